@@ -205,6 +205,92 @@ int pasa_shift_keys_matrix_mfma(const void* k, void* kprime, int B, int Hkv, int
 int pasa_shift_keys_direct(const void* k, void* kprime, void* k0, int B, int Hkv, int N, int d,
                            double beta, double kscale, void* stream);
 
+/* ---- A cache of keys and values in 8 bits, in pages, and attention that reads it ----
+ *
+ * For servers whose sequences grow token by token and differ in length: S sequences share a pool of `pages` pages of `page`
+ * tokens each; table[b][i] is the page in the pool that holds the tokens i * page .. i * page + page - 1 of sequence b (sequences
+ * may share pages that neither writes).  A token takes d bytes and a scale for its key and for its value, per KV head; what is
+ * held stands for code * scale.  Scales belong to a token and head, so a token that enters changes nothing that is there.
+ *
+ * Eq. (9) of the paper: a vector taken from every key leaves softmax unchanged.  kshift is such a vector per KV head (the bias
+ * of the key projection, or a mean over a prompt): it is taken off before keys are rounded to 8 bits, which then need not cover
+ * the bias, and attention and the choice of pages never add it back; pasa_cache_read does.
+ *
+ * kmean holds the mean of the tokens' (shifted, rounded) keys of every page and head: by Eq. (12) a query's product with it is
+ * the pseudo-average of the query's scores over that page, which is what pasa_cache_choose ranks pages by.
+ *
+ * length[b] counts the tokens of sequence b with the ones of the current step: a call that is given rows takes rows
+ * row_start[b] .. row_start[b + 1] - 1 as the last ones of sequence b, so row row_start[b] + t of n_b sits at position
+ * length[b] - n_b + t.  A step is: length += n, pasa_cache_write, then pasa_attn_cache (after pasa_cache_choose, where not all
+ * keys are wanted).  Sequences without rows (n_b = 0) are left alone, as are rows from row_start[S] on.  A step that is taken back
+ * (drafted tokens that were not accepted) is a smaller length at the next call; what was written behind it is overwritten.
+ *
+ * table, length and row_start are read on the device, so that a captured graph follows them; they are not checked by the host.
+ * The kernels keep to the buffers whatever they hold: lengths are taken as at most table_width * page and at least 0, row_start as
+ * between 0 and R; positions before 0 and pages outside the pool are not there (nothing is written to them, they read as zeros
+ * and no row sees them).  row_start has to ascend. */
+typedef enum {
+    PASA_CACHE_I8 = 0,    /* bytes hold value + 128, value = -127 .. 127; scale = largest magnitude / 127 */
+    PASA_CACHE_E4M3 = 1   /* OCP 8-bit floats, 4 exponent bits; scale = largest magnitude / 448 */
+} pasa_cache_format;
+
+typedef struct {
+    void* k;              /* DEVICE [pages][Hkv][page][d] bytes, 16-byte aligned, as v */
+    void* v;
+    float* kscale;        /* DEVICE [pages][Hkv][page], 16-byte aligned, as vscale */
+    float* vscale;
+    float* kmean;         /* DEVICE [pages][Hkv][d], 16-byte aligned, or NULL: not kept (pasa_cache_choose needs it) */
+    const float* kshift;  /* DEVICE [Hkv][d], 16-byte aligned, or NULL: zero.  Constant over the life of the cache's contents */
+    const int* table;     /* DEVICE [S][table_width] */
+    const int* length;    /* DEVICE [S] */
+    int S, Hkv, d;        /* d = 64 or 128 */
+    int page;             /* tokens of a page: 16, 32, 64 or 128 */
+    int pages, table_width;   /* table_width * page <= 262144 */
+    int format;           /* a pasa_cache_format */
+} pasa_cache;
+
+/* Tokens enter the cache.  k, v: rows of [Hkv][d] (fp16 or bf16, see pasa_io_dtype), `row_stride` elements apart (at least
+ * Hkv * d, a multiple of 8: slices of a joint projection are taken as they are), 16-byte aligned, R rows in all.  Per token and head:
+ * scale = fp32(largest magnitude / 127 or 448), 1 where that magnitude is below 2^-100, and codes the nearest of
+ * value / scale (ties to even), exactly.  A token with a value that is not finite gets the scale NaN, and so does whoever sees it.
+ * kmean != NULL: the means of the pages that are written to are made again, over all their tokens below length[b].
+ * PASA_EINVAL also for R <= 0. */
+int pasa_cache_write(const pasa_cache* cache, const void* k, const void* v, int R, long long row_stride, const int* row_start,
+                     int io_dtype, void* stream);
+
+/* Positions first[b] .. first[b] + N - 1 of every sequence (first: DEVICE [S], NULL: zeros) as fp16 or bf16 in k, v:
+ * [S, Hkv, N, d], 16-byte aligned, what pasa_prepare_kv takes with B = S: a long chunk of a prompt is attended to that way.  code * scale
+ * + kshift, rounded to fp32 and then to the type.  Zeros where a sequence has no such position. */
+int pasa_cache_read(const pasa_cache* cache, void* k, void* v, const int* first, int N, int io_dtype, void* stream);
+
+/* For every sequence and KV head the pages that its rows' queries point at: the first `head` and the last `tail` pages always (the
+ * first ones where they exceed `count`), and of the others those with the largest pseudo-average, max over the rows of the sequence and the query heads of
+ * the KV head of q . kmean, in 64 bits; of equal ones the first; NaN counts as the largest.  q: rows of [Hq][d] as k above.  blocks: DEVICE
+ * [S][Hkv][count], the places in the sequence's row of the table, ascending, -1 behind the last.  All pages where there are
+ * no more than count; none for a sequence without rows.  One row per sequence (Nq = 1 of a decoding step) makes it a choice per
+ * query; rows that are to have choices of their own go in as sequences of one row each.  `tail` should cover the pages that the rows themselves lie in.
+ * workspace: DEVICE, 256-byte aligned, pasa_cache_choose_workspace() bytes.  PASA_EINVAL also for count < 1, head or tail < 0. */
+size_t pasa_cache_choose_workspace(const pasa_cache* cache);
+int pasa_cache_choose(const pasa_cache* cache, const void* q, int R, long long row_stride, const int* row_start, int Hq, int* blocks,
+                      int count, int head, int tail, int io_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* softmax(scale * Q K^T) V of the rows against the cache: decoding steps, chains and trees of drafted tokens.  q: rows of [Hq][d]
+ * as above; o: [R][Hq][d], contiguous, 16-byte aligned, not q.  Query head h reads KV head h / (Hq / Hkv).
+ * tree == NULL: a row sees the positions up to its own.  tree: DEVICE [R] words of 64 bits: a row sees the positions before its
+ * sequence's first row, and that of the sequence's row t iff bit t of its word is set (its own bit among them, if it is to see
+ * itself); rows from the 64th on are seen by none.
+ * blocks == NULL: all pages.  blocks: DEVICE [S][Hkv][count] as pasa_cache_choose leaves it: only keys of these pages, of those that
+ * the row sees; ascending without repeats, -1 behind the last.
+ * Scores, statistics and output are held in fp32, P is rounded to fp16 (relative to its row's largest), bf16 queries are converted to
+ * fp16 as they are loaded.  A row that sees no key, or whose scores are all -inf, is zeros.
+ * Meant for rows up to some hundred per sequence; more are correct, but long chunks are faster through pasa_cache_read.
+ * workspace: DEVICE, 256-byte aligned, pasa_attn_cache_workspace() bytes; calls that share one must not overlap in time.
+ * PASA_EUNSUPPORTED also where the keys of all row blocks come to 2^37 or more. */
+size_t pasa_attn_cache_workspace(const pasa_cache* cache, int R, int Hq);
+int pasa_attn_cache(const pasa_cache* cache, const void* q, void* o, int R, long long row_stride, const int* row_start, int Hq,
+                    float scale, const unsigned long long* tree, const int* blocks, int count, int io_dtype, void* workspace,
+                    size_t workspace_bytes, void* stream);
+
 /* Host-only, fp64: solves the optimal accuracy condition beta/(1-beta) = f(beta) (Eq. (16), (20)-(22)) by
  * fixed-point iteration from beta0, for a shifting matrix of size n rounded to format tp
  * (0 = fp16, 1 = bf16).  Returns NaN for invalid arguments. */

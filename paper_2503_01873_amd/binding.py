@@ -15,6 +15,7 @@ import os
 MIXED, STRICT16, NAIVE16, S16, DIRECT = 0, 1, 2, 3, 4
 SHIFT_MEAN, SHIFT_MATRIX, SHIFT_MATRIX_MFMA = 0, 1, 2
 IO_F16, IO_BF16 = 0, 1
+CACHE_I8, CACHE_E4M3 = 0, 1
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.environ.get("PASA_LIB") or os.path.join(_PKG, "libpasa.so")
@@ -37,6 +38,21 @@ class pasa_opts(ctypes.Structure):
         ("shift_mode", ctypes.c_int),
         ("io_dtype", ctypes.c_int),
     ]
+
+
+class pasa_cache(ctypes.Structure):
+    """A paged 8-bit cache: where its buffers are and what they hold, kept by the caller from call to call.  Buffers are tensors or addresses, as in
+    the calls; tensors are held on to."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "kscale", "vscale", "kmean", "kshift", "table", "length")] + \
+               [(n, ctypes.c_int) for n in ("S", "Hkv", "d", "page", "pages", "table_width", "format")]
+
+    def __init__(self, k, v, kscale, vscale, table, length, S, Hkv, d, page, pages, table_width, format=CACHE_I8, kmean=None, kshift=None):
+        self.buffers = (k, v, kscale, vscale, kmean, kshift, table, length)
+        super().__init__(*(_ptr(x) for x in self.buffers), S, Hkv, d, page, pages, table_width, format)
+        self.address = ctypes.addressof(self)
+
+    def data_ptr(self):
+        return self.address
 
 
 def lib_path() -> str:
@@ -80,6 +96,19 @@ def lib() -> ctypes.CDLL:
     L.pasa_shift_keys_matrix_mfma.restype = ci
     L.pasa_shift_keys_direct.argtypes = [vp, vp, vp, ci, ci, ci, ci, cd, cd, vp]
     L.pasa_shift_keys_direct.restype = ci
+    ll = ctypes.c_longlong
+    L.pasa_cache_write.argtypes = [vp, vp, vp, ci, ll, vp, ci, vp]
+    L.pasa_cache_write.restype = ci
+    L.pasa_cache_read.argtypes = [vp, vp, vp, vp, ci, ci, vp]
+    L.pasa_cache_read.restype = ci
+    L.pasa_cache_choose_workspace.argtypes = [vp]
+    L.pasa_cache_choose_workspace.restype = sz
+    L.pasa_cache_choose.argtypes = [vp, vp, ci, ll, vp, ci, vp, ci, ci, ci, ci, vp, sz, vp]
+    L.pasa_cache_choose.restype = ci
+    L.pasa_attn_cache_workspace.argtypes = [vp, ci, ci]
+    L.pasa_attn_cache_workspace.restype = sz
+    L.pasa_attn_cache.argtypes = [vp, vp, vp, ci, ll, vp, ci, cf, vp, vp, ci, ci, vp, sz, vp]
+    L.pasa_attn_cache.restype = ci
     L.pasa_optimal_beta.argtypes = [cd, ci, ci]
     L.pasa_optimal_beta.restype = cd
     L.pasa_invariance_rounded.argtypes = [cd, ci, ci]
@@ -257,3 +286,35 @@ def pasa_attn_fwd_adaptive(q, k, v, o, B, Hq, Hkv, N, d, causal, scale, workspac
     st = (_lib or lib()).call_pasa_attn_fwd_adaptive(q, k, v, o, B, Hq, Hkv, N, d, causal, scale, workspace, workspace_bytes, stream,
                                  beta, variant, shift_tile, overflow_s, nonfinite_o, shift_mode, io_dtype, opts_null)
     return _check(st, "pasa_attn_fwd_adaptive", check)
+
+
+def pasa_cache_write(cache, k, v, R, row_stride, row_start, stream=None, io_dtype=IO_F16, check=True) -> int:
+    st = lib().pasa_cache_write(_ptr(cache), _ptr(k), _ptr(v), R, row_stride, _ptr(row_start), int(io_dtype), _stream(stream))
+    return _check(st, "pasa_cache_write", check)
+
+
+def pasa_cache_read(cache, k, v, first, N, stream=None, io_dtype=IO_F16, check=True) -> int:
+    st = lib().pasa_cache_read(_ptr(cache), _ptr(k), _ptr(v), _ptr(first), N, int(io_dtype), _stream(stream))
+    return _check(st, "pasa_cache_read", check)
+
+
+def pasa_cache_choose_workspace(cache) -> int:
+    return lib().pasa_cache_choose_workspace(_ptr(cache))
+
+
+def pasa_cache_choose(cache, q, R, row_stride, row_start, Hq, blocks, count, head, tail, workspace, workspace_bytes, stream=None,
+                      io_dtype=IO_F16, check=True) -> int:
+    st = lib().pasa_cache_choose(_ptr(cache), _ptr(q), R, row_stride, _ptr(row_start), Hq, _ptr(blocks), count, head, tail, int(io_dtype),
+                                 _ptr(workspace), int(workspace_bytes), _stream(stream))
+    return _check(st, "pasa_cache_choose", check)
+
+
+def pasa_attn_cache_workspace(cache, R, Hq) -> int:
+    return lib().pasa_attn_cache_workspace(_ptr(cache), R, Hq)
+
+
+def pasa_attn_cache(cache, q, o, R, row_stride, row_start, Hq, scale, workspace, workspace_bytes, stream=None, tree=None, blocks=None,
+                    count=0, io_dtype=IO_F16, check=True) -> int:
+    st = lib().pasa_attn_cache(_ptr(cache), _ptr(q), _ptr(o), R, row_stride, _ptr(row_start), Hq, float(scale), _ptr(tree), _ptr(blocks), count,
+                               int(io_dtype), _ptr(workspace), int(workspace_bytes), _stream(stream))
+    return _check(st, "pasa_attn_cache", check)

@@ -1,0 +1,136 @@
+// Host layer of the paged 8-bit cache: the entry points of include/pasa.h that take a pasa_cache.  Argument validation and dispatch.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "pasa.h"
+#include "pasa_cache.h"
+
+namespace {
+
+constexpr long long kMaxTokens = 262144;         // of a sequence, as in the other entry points
+constexpr long long kMaxGrid = 0x7fffffff;       // workgroups of a launch
+
+bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+bool buffer(const void* p, uintptr_t a) { return p != nullptr && aligned(p, a); }
+
+int check_cache(const pasa_cache* c)
+{
+    if (c == nullptr) return PASA_EINVAL;
+    if (!buffer(c->k, 16) || !buffer(c->v, 16) || c->k == c->v || !buffer(c->kscale, 16) || !buffer(c->vscale, 16) ||
+        c->kscale == c->vscale || !aligned(c->kmean, 16) || !aligned(c->kshift, 16) || !buffer(c->table, 4) || !buffer(c->length, 4))
+        return PASA_EINVAL;
+    if (c->S <= 0 || c->Hkv <= 0 || c->pages <= 0 || c->table_width <= 0 || c->d <= 0 || c->page <= 0) return PASA_EINVAL;
+    if (c->format != PASA_CACHE_I8 && c->format != PASA_CACHE_E4M3) return PASA_EINVAL;
+    if (c->d != 64 && c->d != 128) return PASA_EUNSUPPORTED;
+    if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return PASA_EUNSUPPORTED;
+    if ((long long)c->table_width * c->page > kMaxTokens || (long long)c->S * c->Hkv > kMaxGrid) return PASA_EUNSUPPORTED;
+    return PASA_OK;
+}
+
+// R rows of `heads` heads at p
+int check_rows(const pasa_cache* c, const void* p, int R, long long row_stride, const int* row_start, int heads, int io_dtype)
+{
+    if (!buffer(p, 16) || !buffer(row_start, 4) || R <= 0 || heads <= 0) return PASA_EINVAL;
+    if (row_stride < (long long)heads * c->d || row_stride % 8 != 0) return PASA_EINVAL;
+    if (io_dtype != PASA_IO_F16 && io_dtype != PASA_IO_BF16) return PASA_EINVAL;
+    if (R > kMaxGrid - 1) return PASA_EUNSUPPORTED;
+    return PASA_OK;
+}
+
+int check_workspace(const void* ws, size_t bytes, size_t need) { return buffer(ws, 256) && bytes >= need ? PASA_OK : PASA_EWORKSPACE; }
+
+// Rows per workgroup: 16 where the rows of a KV head fill no more on average, 32 otherwise.  Workgroups: as many as are resident at once, of 16 rows three
+// to a compute unit, of 32 two, and no more than leave each wavefront a unit.  False where the units do not fit 31 bits.
+bool plan_of(const pasa_cache& c, int R, int Hq, CachePlan* plan)
+{
+    const long long G = Hq / c.Hkv;
+    plan->row_blocks = (long long)R * G <= 16LL * c.S ? 1 : 2;
+    const long long units = ((long long)c.table_width * c.page + kUnit - 1) / kUnit;
+    const long long blocks = (long long)R * G / (16 * plan->row_blocks) + c.S;      // of rows, at most
+    if (R * G > kMaxGrid || blocks > kMaxGrid / c.Hkv || blocks * c.Hkv > kMaxGrid / units) return false;
+    const long long all = (blocks * c.Hkv * units + kUnitsAtOnce - 1) / kUnitsAtOnce, resident = plan->row_blocks == 1 ? 768 : 512;
+    plan->grid = (int)(all < resident ? all : resident);
+    return true;
+}
+
+size_t attn_workspace_bytes(const pasa_cache& c, const CachePlan& plan)
+{
+    return ((size_t)2 * plan.grid * cache_slot_floats(plan.row_blocks, c.d) * 4 + 255) / 256 * 256;
+}
+
+size_t choose_workspace_bytes(const pasa_cache& c) { return ((size_t)8 * c.S * c.Hkv * c.table_width + 255) / 256 * 256; }
+
+int status(hipError_t e) { return e == hipSuccess ? PASA_OK : PASA_ELAUNCH; }
+
+}  // namespace
+
+extern "C" {
+
+int pasa_cache_write(const pasa_cache* cache, const void* k, const void* v, int R, long long row_stride, const int* row_start, int io_dtype,
+                     void* stream)
+{
+    int st = check_cache(cache);
+    if (st != PASA_OK) return st;
+    st = check_rows(cache, k, R, row_stride, row_start, cache->Hkv, io_dtype);
+    if (st != PASA_OK) return st;
+    if (!buffer(v, 16)) return PASA_EINVAL;
+    if (((long long)R / cache->page + 2LL * cache->S) * cache->Hkv > kMaxGrid) return PASA_EUNSUPPORTED;
+    return status(pasa_launch_cache_write(*cache, k, v, R, row_stride, row_start, io_dtype == PASA_IO_BF16, static_cast<hipStream_t>(stream)));
+}
+
+int pasa_cache_read(const pasa_cache* cache, void* k, void* v, const int* first, int N, int io_dtype, void* stream)
+{
+    const int st = check_cache(cache);
+    if (st != PASA_OK) return st;
+    if (!buffer(k, 16) || !buffer(v, 16) || k == v || !aligned(first, 4) || N <= 0) return PASA_EINVAL;
+    if (io_dtype != PASA_IO_F16 && io_dtype != PASA_IO_BF16) return PASA_EINVAL;
+    if (N > kMaxTokens || (((long long)N + 127) / 128) * cache->S > kMaxGrid / cache->Hkv) return PASA_EUNSUPPORTED;
+    return status(pasa_launch_cache_read(*cache, k, v, first, N, io_dtype == PASA_IO_BF16, static_cast<hipStream_t>(stream)));
+}
+
+size_t pasa_cache_choose_workspace(const pasa_cache* cache) { return check_cache(cache) == PASA_OK ? choose_workspace_bytes(*cache) : 0; }
+
+int pasa_cache_choose(const pasa_cache* cache, const void* q, int R, long long row_stride, const int* row_start, int Hq, int* blocks, int count,
+                      int head, int tail, int io_dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    int st = check_cache(cache);
+    if (st != PASA_OK) return st;
+    st = check_rows(cache, q, R, row_stride, row_start, Hq, io_dtype);
+    if (st != PASA_OK) return st;
+    if (Hq % cache->Hkv != 0 || cache->kmean == nullptr || !buffer(blocks, 4) || count < 1 || head < 0 || tail < 0) return PASA_EINVAL;
+    if (count > kMaxTokens || ((long long)cache->table_width + 63) / 64 * cache->S > kMaxGrid / cache->Hkv || (long long)R * (Hq / cache->Hkv) > kMaxGrid)
+        return PASA_EUNSUPPORTED;
+    st = check_workspace(workspace, workspace_bytes, choose_workspace_bytes(*cache));
+    if (st != PASA_OK) return st;
+    return status(pasa_launch_cache_choose(*cache, q, R, row_stride, row_start, Hq, count, head, tail, blocks, io_dtype == PASA_IO_BF16,
+                                           static_cast<unsigned long long*>(workspace), static_cast<hipStream_t>(stream)));
+}
+
+size_t pasa_attn_cache_workspace(const pasa_cache* cache, int R, int Hq)
+{
+    CachePlan plan;
+    if (check_cache(cache) != PASA_OK || R <= 0 || Hq <= 0 || Hq % cache->Hkv != 0 || !plan_of(*cache, R, Hq, &plan)) return 0;
+    return attn_workspace_bytes(*cache, plan);
+}
+
+int pasa_attn_cache(const pasa_cache* cache, const void* q, void* o, int R, long long row_stride, const int* row_start, int Hq, float scale,
+                    const unsigned long long* tree, const int* blocks, int count, int io_dtype, void* workspace, size_t workspace_bytes,
+                    void* stream)
+{
+    int st = check_cache(cache);
+    if (st != PASA_OK) return st;
+    st = check_rows(cache, q, R, row_stride, row_start, Hq, io_dtype);
+    if (st != PASA_OK) return st;
+    if (Hq % cache->Hkv != 0 || !buffer(o, 16) || o == q || !isfinite(scale) || !(scale > 0.f)) return PASA_EINVAL;
+    if (!aligned(tree, 8) || !aligned(blocks, 4) || (blocks != nullptr && count < 1)) return PASA_EINVAL;
+    if (blocks != nullptr && count > kMaxTokens) return PASA_EUNSUPPORTED;
+    CachePlan plan;
+    if (!plan_of(*cache, R, Hq, &plan)) return PASA_EUNSUPPORTED;
+    st = check_workspace(workspace, workspace_bytes, attn_workspace_bytes(*cache, plan));
+    if (st != PASA_OK) return st;
+    return status(pasa_launch_attn_cache(*cache, q, o, R, row_stride, row_start, Hq, scale, tree, blocks, count, io_dtype == PASA_IO_BF16, plan,
+                                         static_cast<float*>(workspace), static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"
