@@ -16,9 +16,13 @@ struct CachePlan {
     int row_blocks, grid;
 };
 constexpr int kUnit = 64;              // keys of a unit of work (of one wavefront)
-constexpr int kUnitsAtOnce = 4;        // wavefronts of a workgroup: units that it sweeps at a time
+constexpr int kUnitsAtOnce = 8;        // wavefronts of a workgroup: units that it sweeps at a time
 
-// Per slot and row: sum of P and level, then the stored output; two slots per workgroup.
+// Workspace: per workgroup a record of what is to be merged, then two slots; in a slot sum of P and level per row, then the rows' stored output.
+struct MergeRecord {
+    int pieces;                        // 0: none
+    int slot, p0, list, row0, hk, unused[2];
+};
 __host__ __device__ inline size_t cache_slot_floats(int row_blocks, int d) { return (size_t)16 * row_blocks * (d + 2); }
 
 hipError_t pasa_launch_cache_write(const pasa_cache& c, const void* k, const void* v, int R, long long row_stride, const int* row_start,
@@ -29,7 +33,7 @@ hipError_t pasa_launch_cache_choose(const pasa_cache& c, const void* q, int R, l
                                     int count, int head, int tail, int* blocks, int io_bf16, unsigned long long* scores, hipStream_t stream);
 hipError_t pasa_launch_attn_cache(const pasa_cache& c, const void* q, void* o, int R, long long row_stride, const int* row_start, int Hq,
                                   float scale, const unsigned long long* tree, const int* blocks, int count, int io_bf16,
-                                  const CachePlan& plan, float* slots, hipStream_t stream);
+                                  const CachePlan& plan, void* workspace, hipStream_t stream);
 
 #ifdef __HIPCC__
 namespace {
@@ -50,38 +54,43 @@ __device__ inline Sequence sequence_at(const int* __restrict__ length, const int
     return s;
 }
 
-// A workgroup's place in work that is shared out over the sequences: sequence b has count(b) pieces, and piece `at(total)` of all
-// lies in sequence `b`, the `rest`-th there.  b < 0 where there is no such piece.  All threads call it; every thread counts its own share of the sequences,
-// one scan over the threads finds who has the piece, and that one walks its share.
+// A workgroup's place in work that is shared out over the sequences: sequence b has count(sequence) pieces, and piece `at(total)` of all
+// lies in sequence `b`, the `rest`-th there.  b < 0 where there is no such piece.  All NT threads call it; every thread counts its own
+// share of the sequences, one scan over the threads finds who has the piece, and that one walks its share (which is a single one up to NT sequences)
+// and leaves what it has read: nothing is waited for twice.
 struct Place {
     int b;
     unsigned rest, total;
+    Sequence s;
 };
-template <class Count, class At>
-__device__ inline Place find_place(int S, Count count, At at)
+template <int NT, class Count, class At>
+__device__ inline Place find_place(const int* __restrict__ length, const int* __restrict__ row_start, int S, int R, int most, Count count, At at)
 {
-    __shared__ unsigned sums[kCacheThreads / 64];
-    __shared__ int found_b;
-    __shared__ unsigned found_rest;
+    __shared__ unsigned sums[NT / 64];
+    __shared__ int found[5];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int each = (S + kCacheThreads - 1) / kCacheThreads, b0 = tid * each;
+    const int each = (S + NT - 1) / NT, b0 = tid * each;
+    Sequence s = {0, 0, 0};
     unsigned mine = 0;
     for (int i = 0; i < each; ++i)
-        if (b0 + i < S) mine += count(b0 + i);
+        if (b0 + i < S) {
+            s = sequence_at(length, row_start, b0 + i, R, most);
+            mine += count(s);
+        }
     unsigned upto = mine;              // inclusive scan over the wavefront
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
         const unsigned x = __shfl_up(upto, o);
         if (lane >= o) upto += x;
     }
-    if (tid == 0) found_b = -1;
+    if (tid == 0) found[0] = -1;
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
     Place p;
     p.total = 0;
     unsigned before = upto - mine;
 #pragma unroll
-    for (int w = 0; w < kCacheThreads / 64; ++w) {
+    for (int w = 0; w < NT / 64; ++w) {
         if (w < wave) before += sums[w];
         p.total += sums[w];
     }
@@ -89,17 +98,30 @@ __device__ inline Place find_place(int S, Count count, At at)
     if (want >= before && want < before + mine) {
         int b = b0;
         unsigned left = want - before;
-        for (unsigned c = count(b); left >= c && b < b0 + each; c = count(b)) {
-            left -= c;
-            if (++b >= S) break;
-        }
-        found_b = b < S && b < b0 + each ? b : -1;
-        found_rest = left;
+        if (each > 1)
+            for (;; ++b) {
+                if (b >= S || b >= b0 + each) {      // not as it was counted: somebody writes to length or row_start meanwhile
+                    b = -1;
+                    break;
+                }
+                s = sequence_at(length, row_start, b, R, most);
+                const unsigned c = count(s);
+                if (left < c) break;
+                left -= c;
+            }
+        found[0] = b;
+        found[1] = (int)left;
+        found[2] = s.length;
+        found[3] = s.row0;
+        found[4] = s.rows;
     }
     __syncthreads();
-    p.b = __builtin_amdgcn_readfirstlane(found_b);
-    p.rest = __builtin_amdgcn_readfirstlane(found_rest);
-    p.total = __builtin_amdgcn_readfirstlane(p.total);
+    p.b = __builtin_amdgcn_readfirstlane(found[0]);
+    p.rest = (unsigned)__builtin_amdgcn_readfirstlane(found[1]);
+    p.total = (unsigned)__builtin_amdgcn_readfirstlane((int)p.total);
+    p.s.length = __builtin_amdgcn_readfirstlane(found[2]);
+    p.s.row0 = __builtin_amdgcn_readfirstlane(found[3]);
+    p.s.rows = __builtin_amdgcn_readfirstlane(found[4]);
     return p;
 }
 

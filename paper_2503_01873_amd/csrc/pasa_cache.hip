@@ -73,12 +73,11 @@ void pasa_cache_write_k(pasa_cache c, const unsigned short* __restrict__ k, cons
     const unsigned piece = heads.quotient(blockIdx.x);
     const int hk = (int)heads.rest(blockIdx.x, piece);
     auto first_page = [&](const Sequence& s) { return (s.length > s.rows ? s.length - s.rows : 0) / c.page; };
-    const Place at = find_place(c.S, [&](int b) {
-        const Sequence s = sequence_at(c.length, row_start, b, R, most);
+    const Place at = find_place<kCacheThreads>(c.length, row_start, c.S, R, most, [&](const Sequence& s) {
         return s.rows == 0 || s.length == 0 ? 0u : (unsigned)((s.length - 1) / c.page - first_page(s) + 1);
     }, [&](unsigned) { return piece; });
     if (at.b < 0) return;
-    const Sequence s = sequence_at(c.length, row_start, at.b, R, most);
+    const Sequence s = at.s;
     const int place = first_page(s) + (int)at.rest, pos0 = place * c.page;
     const int id = c.table[(size_t)at.b * c.table_width + place];
     if (id < 0 || id >= c.pages) return;

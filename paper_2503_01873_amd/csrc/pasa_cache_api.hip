@@ -40,8 +40,8 @@ int check_rows(const pasa_cache* c, const void* p, int R, long long row_stride, 
 
 int check_workspace(const void* ws, size_t bytes, size_t need) { return buffer(ws, 256) && bytes >= need ? PASA_OK : PASA_EWORKSPACE; }
 
-// Rows per workgroup: 16 where the rows of a KV head fill no more on average, 32 otherwise.  Workgroups: as many as are resident at once, of 16 rows three
-// to a compute unit, of 32 two, and no more than leave each wavefront a unit.  False where the units do not fit 31 bits.
+// Rows per workgroup: 16 where the rows of a KV head fill no more on average, 32 otherwise.  Workgroups: one to a compute unit (their eight wavefronts take
+// its registers), and no more than leave each wavefront a unit.  False where the units do not fit 31 bits.
 bool plan_of(const pasa_cache& c, int R, int Hq, CachePlan* plan)
 {
     const long long G = Hq / c.Hkv;
@@ -49,14 +49,14 @@ bool plan_of(const pasa_cache& c, int R, int Hq, CachePlan* plan)
     const long long units = ((long long)c.table_width * c.page + kUnit - 1) / kUnit;
     const long long blocks = (long long)R * G / (16 * plan->row_blocks) + c.S;      // of rows, at most
     if (R * G > kMaxGrid || blocks > kMaxGrid / c.Hkv || blocks * c.Hkv > kMaxGrid / units) return false;
-    const long long all = (blocks * c.Hkv * units + kUnitsAtOnce - 1) / kUnitsAtOnce, resident = plan->row_blocks == 1 ? 768 : 512;
+    const long long all = (blocks * c.Hkv * units + kUnitsAtOnce - 1) / kUnitsAtOnce, resident = 256;
     plan->grid = (int)(all < resident ? all : resident);
     return true;
 }
 
 size_t attn_workspace_bytes(const pasa_cache& c, const CachePlan& plan)
 {
-    return ((size_t)2 * plan.grid * cache_slot_floats(plan.row_blocks, c.d) * 4 + 255) / 256 * 256;
+    return (plan.grid * (sizeof(MergeRecord) + 2 * cache_slot_floats(plan.row_blocks, c.d) * sizeof(float)) + 255) / 256 * 256;
 }
 
 size_t choose_workspace_bytes(const pasa_cache& c) { return ((size_t)8 * c.S * c.Hkv * c.table_width + 255) / 256 * 256; }
@@ -130,7 +130,7 @@ int pasa_attn_cache(const pasa_cache* cache, const void* q, void* o, int R, long
     st = check_workspace(workspace, workspace_bytes, attn_workspace_bytes(*cache, plan));
     if (st != PASA_OK) return st;
     return status(pasa_launch_attn_cache(*cache, q, o, R, row_stride, row_start, Hq, scale, tree, blocks, count, io_dtype == PASA_IO_BF16, plan,
-                                         static_cast<float*>(workspace), static_cast<hipStream_t>(stream)));
+                                         workspace, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"
