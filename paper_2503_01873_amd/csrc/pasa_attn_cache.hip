@@ -1,6 +1,7 @@
 // Attention of a few rows per sequence over the paged 8-bit cache: pasa_cache_rows, and the merge of what its workgroups leave.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 #include "pasa_cache.h"
 
@@ -38,8 +39,8 @@ struct RowsArgs {
     FastDiv G;
 };
 
-// What the workgroups share out is units of 64 keys, over sequences, KV heads and blocks of rows; so many a workgroup.
-__device__ inline unsigned share_of(unsigned total, unsigned grid) { return (total + kUnitsAtOnce * grid - 1) / (kUnitsAtOnce * grid) * kUnitsAtOnce; }
+// What the workgroups share out is units of 64 keys, over sequences, KV heads and blocks of rows.  A multiple of what a workgroup sweeps at once:
+__device__ inline unsigned whole_units(unsigned units) { return (units + kUnitsAtOnce - 1) / kUnitsAtOnce * kUnitsAtOnce; }
 
 // Keys that a sequence's rows are swept over, in the order of the list where there is one; its units, at least one (rows without keys
 // are written too); its blocks of rows
@@ -61,11 +62,79 @@ __device__ inline Extent extent_of(const RowsArgs& a, const Sequence& s)
     return x;
 }
 
-template <int ROWS>
-__device__ inline unsigned units_of(const RowsArgs& a, const Sequence& s)
+// What a workgroup sweeps first: units `us` on of block of rows `pair` (of all heads) of sequence b, and how many from there on; b < 0: nothing.
+struct Start {
+    int b, us;
+    unsigned pair, left, per;
+    Sequence s;
+};
+
+// Two ways to share out.  Few (sequence, head, row block)s, half as many as there are workgroups at most: each is cut into ranges of `per` units,
+// one a workgroup, with `per` the least of eight sizes (one a wavefront tries) that gives no more ranges than workgroups: between an even share of the whole and
+// that share for the workgroups that are left when every row block has one range that is not full, with which it always fits.  Many: the units of all are one line that is cut evenly, and a
+// workgroup's range may end inside one block and begin inside the next.  That costs it what a range costs beside its keys, twice: 6 us (4 heads of 4999 keys 14.7 us,
+// so 10.5).
+template <int ROWS, int NT>
+__device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid, int most)
 {
-    const Extent x = extent_of<ROWS>(a, s);
-    return (unsigned)x.units * (unsigned)x.row_blocks * (unsigned)a.c.Hkv;
+    constexpr int NW = NT / 64;
+    __shared__ unsigned lds_units[NT], lds_pairs[NT], lds_sum[2][NW], lds_try[NW];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    Start st;
+    unsigned per = 0;
+    if (a.c.S <= NT) {
+        unsigned units = 1, pairs = 0;
+        Sequence s = {0, 0, 0};
+        if (tid < a.c.S) {
+            s = sequence_at(a.c.length, a.row_start, tid, a.R, most);
+            const Extent x = extent_of<ROWS>(a, s);
+            units = (unsigned)x.units;
+            pairs = (unsigned)x.row_blocks * (unsigned)a.c.Hkv;
+        }
+        lds_units[tid] = units;
+        lds_pairs[tid] = pairs;
+        const unsigned u = scan64(units * pairs), p = scan64(pairs);
+        if (lane == 63) lds_sum[0][wave] = u, lds_sum[1][wave] = p;
+        __syncthreads();
+        unsigned total = 0, all = 0;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) total += lds_sum[0][i], all += lds_sum[1][i];
+        if (2 * all <= grid) {
+            const unsigned least = whole_units((total + grid - 1) / grid), sure = whole_units((total + grid - all - 1) / (grid - all));
+            auto size = [&](unsigned i) { return whole_units(least + (sure - least) * i / (NW - 1)); };
+            const unsigned mine = size((unsigned)wave);
+            unsigned ranges = 0;
+            for (int i = lane; i < a.c.S; i += 64) ranges += lds_pairs[i] * ((lds_units[i] + mine - 1) / (mine > 0 ? mine : 1));
+            ranges = scan64(ranges);
+            if (lane == 63) lds_try[wave] = ranges;
+            __syncthreads();
+            per = sure;
+#pragma unroll
+            for (int i = NW - 2; i >= 0; --i)
+                if (lds_try[i] <= grid) per = size((unsigned)i);
+            per = (unsigned)__builtin_amdgcn_readfirstlane((int)per);
+        }
+    }
+    const bool ranges = per > 0;
+    const Place at = find_place<NT>(a.c.length, a.row_start, a.c.S, a.R, most, [&](const Sequence& s) {
+        const Extent x = extent_of<ROWS>(a, s);
+        return (unsigned)x.row_blocks * (unsigned)a.c.Hkv * (ranges ? ((unsigned)x.units + per - 1) / per : (unsigned)x.units);
+    }, [&](unsigned total) {
+        if (!ranges) per = whole_units((total + grid - 1) / grid);
+        return ranges ? w : w * per;
+    });
+    per = (unsigned)__builtin_amdgcn_readfirstlane((int)per);
+    st.b = at.b;
+    st.s = at.s;
+    st.per = per;
+    if (at.b < 0) return st;
+    const Extent x = extent_of<ROWS>(a, at.s);
+    const unsigned of_pair = ranges ? ((unsigned)x.units + per - 1) / per : (unsigned)x.units;
+    st.pair = at.rest / of_pair;
+    st.us = (int)((at.rest - st.pair * of_pair) * (ranges ? per : 1u));
+    st.left = ranges ? (unsigned)(x.units - st.us) : at.total - w * per;
+    if (st.left > per) st.left = per;
+    return st;
 }
 
 // Workgroups are dealt round-robin to the 8 XCDs; each XCD gets a contiguous range of the work, so that blocks of rows that read the
@@ -102,7 +171,7 @@ __device__ inline void store_row(const RowsArgs& a, int row0, int hk, int p, int
 // The value's scale is not applied to values (there are 128 of them per key, and one P per row): it goes into the exponent.  With
 // t = score + log2(vscale), M the running maximum of t and P = 2^(t - M): O = sum P y, and the sum of the softmax is sum P / vscale.
 // P is at most 1 (2^8 between moves of the level), so fp16 holds what matters of it whatever the scales.
-template <int D, int RB, bool E4M3>
+template <int D, int RB, bool E4M3, bool LISTED>
 __global__ __launch_bounds__(64 * kUnitsAtOnce, 2)
 void pasa_cache_rows(RowsArgs a)
 {
@@ -121,21 +190,15 @@ void pasa_cache_rows(RowsArgs a)
     const int G = (int)a.G.d, most = a.c.table_width << a.page_log2, lg = a.page_log2;
     const unsigned w = logical_workgroup(blockIdx.x, gridDim.x);
 
-    const Place at = find_place<NT>(a.c.length, a.row_start, a.c.S, a.R, most, [&](const Sequence& s) { return units_of<ROWS>(a, s); },
-                                    [&](unsigned total) { return w * share_of(total, gridDim.x); });
+    const Start at = find_start<ROWS, NT>(a, w, gridDim.x, most);
     if (at.b < 0) {
         if (tid == 0) a.records[w].pieces = 0;
         return;
     }
-    const unsigned per = share_of(at.total, gridDim.x);
-    unsigned left = at.total - w * per;          // units of this workgroup still to be swept
-    if (left > per) left = per;
-
-    int b = at.b;
+    unsigned left = at.left, pair = at.pair;     // units of this workgroup still to be swept
+    int b = at.b, us = at.us;
     Sequence s = at.s;
     Extent x = extent_of<ROWS>(a, s);
-    unsigned pair = at.rest / (unsigned)x.units;
-    int us = (int)(at.rest - pair * (unsigned)x.units);
     bool first_piece = true;
     float* const key_f = lds_key[wave];
 
@@ -171,20 +234,18 @@ void pasa_cache_rows(RowsArgs a)
         if (units > 0) {
             // Places of the blocks of 16 keys, lane group g that of block g, by way of the list where there is one.  Three steps, each an
             // iteration ahead of the next: the list's entry, the table's, the keys.  Entries are read at index 0 where there is no block, and not
-            // used; without a list the first entry of the table stands in for one.  No load hangs on a branch: where ways
-            // with and without one meet, the compiler waits for all that is on its way.
-            const bool listed = a.blocks != nullptr;
+            // used.  No load hangs on a branch: where ways with and without one meet, the compiler waits for all that is on its way.
             const int* const table = a.c.table + (size_t)b * a.c.table_width;
-            const int* const chosen = listed ? a.blocks + ((size_t)b * a.c.Hkv + hk) * a.count : table;
+            const int* const chosen = LISTED ? a.blocks + ((size_t)b * a.c.Hkv + hk) * a.count : nullptr;
             int listed_a, place_b, entry_b;      // of the unit after the next two; of the one after the next
             int pos_next = 0, page_next = -1, pos_now = 0, page_now = -1;
             auto first_key = [&](int n) { return (us + wave + NW * n) * kUnit + 16 * g; };
             auto read_list = [&](int n) {
                 const int vk = first_key(n);
-                listed_a = chosen[listed && n < units && vk < x.keys ? vk >> lg : 0];
+                listed_a = LISTED ? chosen[n < units && vk < x.keys ? vk >> lg : 0] : 0;
             };
             auto read_entry = [&](int n) {
-                const int vk = first_key(n), place = listed ? listed_a : vk >> lg;
+                const int vk = first_key(n), place = LISTED ? listed_a : vk >> lg;
                 const bool in = n < units && vk < x.keys && place >= 0 && place < a.c.table_width;
                 place_b = in ? place : -1;
                 entry_b = table[in ? place : 0];
@@ -327,7 +388,7 @@ void pasa_cache_rows(RowsArgs a)
                 unsigned seen[RB];               // bit 4 blk + i, where not all keys are
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb) seen[rb] = 0xffffu;
-                if (!whole) {
+                if (__builtin_expect(!whole, 0)) {
 #pragma unroll
                     for (int rb = 0; rb < RB; ++rb) seen[rb] = 0;
 #pragma unroll
@@ -474,7 +535,7 @@ void pasa_cache_rows(RowsArgs a)
             // begun here, and goes on in the ranges behind
             if (tid == 0) {
                 MergeRecord m = {0, (int)my_slot, p0, list, s.row0, hk, {0, 0}};
-                if (us == 0 && ue < x.units) m.pieces = 1 + (int)(((unsigned)(x.units - ue) + per - 1) / per);
+                if (us == 0 && ue < x.units) m.pieces = clamp_int(1 + (int)(((unsigned)(x.units - ue) + at.per - 1) / at.per), 0, (int)(gridDim.x - w));
                 a.records[w] = m;
             }
             return;
@@ -496,42 +557,85 @@ void pasa_cache_rows(RowsArgs a)
     }
 }
 
-// A row block that several workgroups have swept: pieces from the slot of the one that began it and the first slots of those behind it, added
-// in the order of the keys, so that the result does not depend on which was done first.  Workgroup (w, part) adds what workgroup w of the sweep
-// has begun, a wavefront a row: 64 / (D / 8) lanes share a chunk of eight channels and take every so many pieces each.
+// A row block that several workgroups have swept: pieces from the slot of the one that began it and the first slots of those behind it.
+// Workgroup (w, r) adds row r of what workgroup w of the sweep has begun: D / 8 neighbouring lanes take a piece, eight channels each, and the
+// groups of lanes are added at the end, always in the same order.
 template <int D, int RB>
 __global__ __launch_bounds__(kCacheThreads)
-void pasa_cache_merge(RowsArgs a)
+void pasa_cache_merge(RowsArgs a, FastDiv rows)
 {
-    constexpr int ROWS = 16 * RB, PARTS = ROWS / 4, CHUNKS = D / 8, LANES = 64 / CHUNKS;
-    const unsigned w = blockIdx.x / PARTS;
+    constexpr int ROWS = 16 * RB, CHUNKS = D / 8, LANES = kCacheThreads / CHUNKS, AT = 4;
+    __shared__ float lds_acc[4][D];
+    __shared__ float lds_state[4][2];
+    const unsigned w = rows.quotient(blockIdx.x);
     const MergeRecord m = a.records[w];
-    const int r = (int)(blockIdx.x % PARTS) * 4 + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63, p = m.p0 + r;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = (int)rows.rest(blockIdx.x, w), p = m.p0 + r;
     if (m.pieces == 0 || p >= m.list) return;
-    const int c8 = lane % CHUNKS * 8, first = lane / CHUNKS;
-    auto slot_of = [&](int i) { return a.slots + (size_t)(i == 0 ? (unsigned)m.slot : 2u * (w + (unsigned)i)) * cache_slot_floats(RB, D); };
-    float level = kNoLevel;
-    for (int i = lane; i < m.pieces; i += 64) level = __builtin_fmaxf(level, slot_of(i)[2 * r + 1]);
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) level = __builtin_fmaxf(level, __shfl_xor(level, o));
-    float sum = 0.f;
+    const int c8 = tid % CHUNKS * 8;
+    float level = kNoLevel, sum = 0.f;
     f4 acc[2] = {(f4)0.f, (f4)0.f};
-#pragma unroll 4
-    for (int i = first; i < m.pieces; i += LANES) {
-        const float* slot = slot_of(i);
-        const f4 lo = *reinterpret_cast<const f4*>(slot + 2 * ROWS + (size_t)r * D + c8), hi = *reinterpret_cast<const f4*>(slot + 2 * ROWS + (size_t)r * D + c8 + 4);
-        const float f = __builtin_amdgcn_exp2f(slot[2 * r + 1] - level);
-        sum += f * slot[2 * r];
-        acc[0] += f * lo;
-        acc[1] += f * hi;
+    for (int i0 = tid / CHUNKS; i0 < m.pieces; i0 += AT * LANES) {
+        f2 state[AT];
+        f4 part[AT][2];
+#pragma unroll
+        for (int j = 0; j < AT; ++j) {           // all loads at once; behind the last piece the first one of the lane again, for nothing
+            const int i = i0 + j * LANES < m.pieces ? i0 + j * LANES : i0;
+            const float* slot = a.slots + (size_t)(i == 0 ? (unsigned)m.slot : 2u * (w + (unsigned)i)) * cache_slot_floats(RB, D);
+            state[j] = *reinterpret_cast<const f2*>(slot + 2 * r);
+            part[j][0] = *reinterpret_cast<const f4*>(slot + 2 * ROWS + (size_t)r * D + c8);
+            part[j][1] = *reinterpret_cast<const f4*>(slot + 2 * ROWS + (size_t)r * D + c8 + 4);
+        }
+        float top = level;
+#pragma unroll
+        for (int j = 0; j < AT; ++j) top = __builtin_fmaxf(top, state[j][1]);
+        const float keep = __builtin_amdgcn_exp2f(level - top);
+        sum *= keep;
+        acc[0] *= keep;
+        acc[1] *= keep;
+#pragma unroll
+        for (int j = 0; j < AT; ++j)
+            if (i0 + j * LANES < m.pieces) {
+                const float f = __builtin_amdgcn_exp2f(state[j][1] - top);
+                sum += f * state[j][0];
+                acc[0] += f * part[j][0];
+                acc[1] += f * part[j][1];
+            }
+        level = top;
     }
+    // the groups of lanes of a wavefront, then the wavefronts
+    float top = level;
+#pragma unroll
+    for (int o = CHUNKS; o < 64; o <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, o));
+    const float f = __builtin_amdgcn_exp2f(level - top);
+    sum *= f;
+    acc[0] *= f;
+    acc[1] *= f;
 #pragma unroll
     for (int o = CHUNKS; o < 64; o <<= 1) {
         sum += __shfl_xor(sum, o);
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i >> 2][i & 3] += __shfl_xor(acc[i >> 2][i & 3], o);
     }
-    if (first == 0) store_row(a, m.row0, m.hk, p, D, c8, acc, sum);
+    if (lane < CHUNKS) {
+        *reinterpret_cast<f4*>(&lds_acc[wave][c8]) = acc[0];
+        *reinterpret_cast<f4*>(&lds_acc[wave][c8 + 4]) = acc[1];
+        if (lane == 0) lds_state[wave][0] = sum, lds_state[wave][1] = top;
+    }
+    __syncthreads();
+    if (tid >= CHUNKS) return;
+    top = lds_state[0][1];
+#pragma unroll
+    for (int i = 1; i < 4; ++i) top = __builtin_fmaxf(top, lds_state[i][1]);
+    sum = 0.f;
+    acc[0] = acc[1] = (f4)0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float e = __builtin_amdgcn_exp2f(lds_state[i][1] - top);
+        sum += e * lds_state[i][0];
+        acc[0] += e * *reinterpret_cast<const f4*>(&lds_acc[i][c8]);
+        acc[1] += e * *reinterpret_cast<const f4*>(&lds_acc[i][c8 + 4]);
+    }
+    store_row(a, m.row0, m.hk, p, D, c8, acc, sum);
 }
 
 }  // namespace
@@ -562,14 +666,19 @@ hipError_t pasa_launch_attn_cache(const pasa_cache& c, const void* q, void* o, i
         rows<<<plan.grid, 64 * kUnitsAtOnce, 0, stream>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || plan.grid == 1) return e;
-        merge<<<plan.grid * 4 * plan.row_blocks, kCacheThreads, 0, stream>>>(a);
+        const long long most = (long long)R * (Hq / c.Hkv);          // rows of a block
+        const unsigned each = (unsigned)(most < 16 * plan.row_blocks ? most : 16 * plan.row_blocks);
+        merge<<<(unsigned)plan.grid * each, kCacheThreads, 0, stream>>>(a, fast_div(each));
         return hipGetLastError();
     };
-    const bool e = c.format == PASA_CACHE_E4M3;
-    if (c.d == 128) {
-        if (plan.row_blocks == 1) return e ? go(pasa_cache_rows<128, 1, true>, pasa_cache_merge<128, 1>) : go(pasa_cache_rows<128, 1, false>, pasa_cache_merge<128, 1>);
-        return e ? go(pasa_cache_rows<128, 2, true>, pasa_cache_merge<128, 2>) : go(pasa_cache_rows<128, 2, false>, pasa_cache_merge<128, 2>);
-    }
-    if (plan.row_blocks == 1) return e ? go(pasa_cache_rows<64, 1, true>, pasa_cache_merge<64, 1>) : go(pasa_cache_rows<64, 1, false>, pasa_cache_merge<64, 1>);
-    return e ? go(pasa_cache_rows<64, 2, true>, pasa_cache_merge<64, 2>) : go(pasa_cache_rows<64, 2, false>, pasa_cache_merge<64, 2>);
+    const bool e = c.format == PASA_CACHE_E4M3, l = blocks != nullptr;
+    auto of_format = [&](auto d, auto rb) {
+        constexpr int D = decltype(d)::value, RB = decltype(rb)::value;
+        if (e) return l ? go(pasa_cache_rows<D, RB, true, true>, pasa_cache_merge<D, RB>) : go(pasa_cache_rows<D, RB, true, false>, pasa_cache_merge<D, RB>);
+        return l ? go(pasa_cache_rows<D, RB, false, true>, pasa_cache_merge<D, RB>) : go(pasa_cache_rows<D, RB, false, false>, pasa_cache_merge<D, RB>);
+    };
+    auto of_rows = [&](auto d) {
+        return plan.row_blocks == 1 ? of_format(d, std::integral_constant<int, 1>{}) : of_format(d, std::integral_constant<int, 2>{});
+    };
+    return c.d == 128 ? of_rows(std::integral_constant<int, 128>{}) : of_rows(std::integral_constant<int, 64>{});
 }

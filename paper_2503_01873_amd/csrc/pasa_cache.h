@@ -54,9 +54,21 @@ __device__ inline Sequence sequence_at(const int* __restrict__ length, const int
     return s;
 }
 
+// Sum over the lanes of a wavefront up to and with one's own
+__device__ inline unsigned scan64(unsigned x)
+{
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false);       // row_shr 1, 2, 4, 8: within 16 lanes
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false);
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false);
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false);
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);       // lane 15 to the second 16 lanes, 47 to the fourth
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);       // lane 31 to the upper half
+    return x;
+}
+
 // A workgroup's place in work that is shared out over the sequences: sequence b has count(sequence) pieces, and piece `at(total)` of all
-// lies in sequence `b`, the `rest`-th there.  b < 0 where there is no such piece.  All NT threads call it; every thread counts its own
-// share of the sequences, one scan over the threads finds who has the piece, and that one walks its share (which is a single one up to NT sequences)
+// lies in sequence `b`, the `rest`-th there.  b < 0 where there is no such piece.  All NT threads call it (at with the same result in all); every
+// thread counts its own share of the sequences, one scan over the threads finds who has the piece, and that one walks its share (which is a single one up to NT sequences)
 // and leaves what it has read: nothing is waited for twice.
 struct Place {
     int b;
@@ -77,12 +89,7 @@ __device__ inline Place find_place(const int* __restrict__ length, const int* __
             s = sequence_at(length, row_start, b0 + i, R, most);
             mine += count(s);
         }
-    unsigned upto = mine;              // inclusive scan over the wavefront
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const unsigned x = __shfl_up(upto, o);
-        if (lane >= o) upto += x;
-    }
+    const unsigned upto = scan64(mine);
     if (tid == 0) found[0] = -1;
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
