@@ -78,11 +78,20 @@ template <int ROWS, int NT>
 __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid, int most)
 {
     constexpr int NW = NT / 64;
-    __shared__ unsigned lds_units[NT], lds_pairs[NT], lds_sum[2][NW], lds_try[NW];
+    __shared__ unsigned lds_units[NT], lds_pairs[NT], lds_sum[3][NW], lds_try[NW];
+    __shared__ Start found;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    Start st;
-    unsigned per = 0;
-    if (a.c.S <= NT) {
+    // Place `rest` of a sequence's ranges (or units, where the line is cut)
+    auto start_at = [&](int b, const Sequence& s, unsigned rest, unsigned total, unsigned per, bool ranges) {
+        const Extent x = extent_of<ROWS>(a, s);
+        const unsigned of_pair = ranges ? ((unsigned)x.units + per - 1) / per : (unsigned)x.units;
+        Start st = {b, 0, rest / of_pair, 0, per, s};
+        st.us = (int)((rest - st.pair * of_pair) * (ranges ? per : 1u));
+        st.left = ranges ? (unsigned)(x.units - st.us) : total - w * per;
+        if (st.left > per) st.left = per;
+        return st;
+    };
+    if (a.c.S <= NT) {                           // a sequence a thread: what is read of it once is enough
         unsigned units = 1, pairs = 0;
         Sequence s = {0, 0, 0};
         if (tid < a.c.S) {
@@ -93,47 +102,65 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
         }
         lds_units[tid] = units;
         lds_pairs[tid] = pairs;
-        const unsigned u = scan64(units * pairs), p = scan64(pairs);
-        if (lane == 63) lds_sum[0][wave] = u, lds_sum[1][wave] = p;
+        const unsigned upto_u = scan64(units * pairs), upto_p = scan64(pairs);
+        if (lane == 63) lds_sum[0][wave] = upto_u, lds_sum[1][wave] = upto_p;
+        if (tid == 0) found.b = -1;
         __syncthreads();
-        unsigned total = 0, all = 0;
+        unsigned total = 0, all = 0, before = upto_u - units * pairs, mine = units * pairs;
 #pragma unroll
-        for (int i = 0; i < NW; ++i) total += lds_sum[0][i], all += lds_sum[1][i];
-        if (2 * all <= grid) {
-            const unsigned least = whole_units((total + grid - 1) / grid), sure = whole_units((total + grid - all - 1) / (grid - all));
+        for (int i = 0; i < NW; ++i) {
+            if (i < wave) before += lds_sum[0][i];
+            total += lds_sum[0][i];
+            all += lds_sum[1][i];
+        }
+        const bool ranges = 2 * all <= grid;
+        unsigned per = whole_units((total + grid - 1) / grid), want = w * per;
+        if (ranges) {
+            const unsigned least = per, sure = whole_units((total + grid - all - 1) / (grid - all));
             auto size = [&](unsigned i) { return whole_units(least + (sure - least) * i / (NW - 1)); };
-            const unsigned mine = size((unsigned)wave);
-            unsigned ranges = 0;
-            for (int i = lane; i < a.c.S; i += 64) ranges += lds_pairs[i] * ((lds_units[i] + mine - 1) / (mine > 0 ? mine : 1));
-            ranges = scan64(ranges);
-            if (lane == 63) lds_try[wave] = ranges;
+            const unsigned size_of_wave = size((unsigned)wave);
+            unsigned sum = 0;
+            for (int i = lane; i < a.c.S; i += 64) sum += size_of_wave > 0 ? lds_pairs[i] * ((lds_units[i] + size_of_wave - 1) / size_of_wave) : 0;
+            sum = scan64(sum);
+            if (lane == 63) lds_try[wave] = sum;
             __syncthreads();
             per = sure;
 #pragma unroll
             for (int i = NW - 2; i >= 0; --i)
                 if (lds_try[i] <= grid) per = size((unsigned)i);
-            per = (unsigned)__builtin_amdgcn_readfirstlane((int)per);
+            mine = per > 0 ? pairs * ((units + per - 1) / per) : 0;
+            before = scan64(mine);
+            if (lane == 63) lds_sum[2][wave] = before;
+            __syncthreads();
+            before -= mine;
+#pragma unroll
+            for (int i = 0; i < NW; ++i)
+                if (i < wave) before += lds_sum[2][i];
+            want = w;
         }
+        if (want >= before && want < before + mine) found = start_at(tid, s, want - before, total, per, ranges);
+        __syncthreads();
+    } else {
+        unsigned per = 0;
+        const Place at = find_place<NT>(a.c.length, a.row_start, a.c.S, a.R, most, [&](const Sequence& s) {
+            const Extent x = extent_of<ROWS>(a, s);
+            return (unsigned)x.row_blocks * (unsigned)a.c.Hkv * (unsigned)x.units;
+        }, [&](unsigned total) { return w * (per = whole_units((total + grid - 1) / grid)); });
+        if (tid == 0) {
+            if (at.b < 0) found.b = -1;
+            else found = start_at(at.b, at.s, at.rest, at.total, per, false);
+        }
+        __syncthreads();
     }
-    const bool ranges = per > 0;
-    const Place at = find_place<NT>(a.c.length, a.row_start, a.c.S, a.R, most, [&](const Sequence& s) {
-        const Extent x = extent_of<ROWS>(a, s);
-        return (unsigned)x.row_blocks * (unsigned)a.c.Hkv * (ranges ? ((unsigned)x.units + per - 1) / per : (unsigned)x.units);
-    }, [&](unsigned total) {
-        if (!ranges) per = whole_units((total + grid - 1) / grid);
-        return ranges ? w : w * per;
-    });
-    per = (unsigned)__builtin_amdgcn_readfirstlane((int)per);
-    st.b = at.b;
-    st.s = at.s;
-    st.per = per;
-    if (at.b < 0) return st;
-    const Extent x = extent_of<ROWS>(a, at.s);
-    const unsigned of_pair = ranges ? ((unsigned)x.units + per - 1) / per : (unsigned)x.units;
-    st.pair = at.rest / of_pair;
-    st.us = (int)((at.rest - st.pair * of_pair) * (ranges ? per : 1u));
-    st.left = ranges ? (unsigned)(x.units - st.us) : at.total - w * per;
-    if (st.left > per) st.left = per;
+    Start st;
+    st.b = __builtin_amdgcn_readfirstlane(found.b);
+    st.us = __builtin_amdgcn_readfirstlane(found.us);
+    st.pair = (unsigned)__builtin_amdgcn_readfirstlane((int)found.pair);
+    st.left = (unsigned)__builtin_amdgcn_readfirstlane((int)found.left);
+    st.per = (unsigned)__builtin_amdgcn_readfirstlane((int)found.per);
+    st.s.length = __builtin_amdgcn_readfirstlane(found.s.length);
+    st.s.row0 = __builtin_amdgcn_readfirstlane(found.s.row0);
+    st.s.rows = __builtin_amdgcn_readfirstlane(found.s.rows);
     return st;
 }
 
@@ -659,8 +686,7 @@ hipError_t pasa_launch_attn_cache(const pasa_cache& c, const void* q, void* o, i
     a.Hq = Hq;
     a.count = count;
     a.io_bf16 = io_bf16;
-    a.page_log2 = 0;
-    while ((1 << a.page_log2) < c.page) ++a.page_log2;
+    a.page_log2 = log2_of(c.page);
     a.G = fast_div((unsigned)(Hq / c.Hkv));
     auto go = [&](auto rows, auto merge) {
         rows<<<plan.grid, 64 * kUnitsAtOnce, 0, stream>>>(a);

@@ -8,8 +8,13 @@
 #include "pasa.h"
 #include "pasa_device.h"
 
-constexpr int kCacheThreads = 256;     // of a workgroup, in all the cache's kernels but the one that picks pages
-constexpr int kPickThreads = 1024;
+constexpr int kCacheThreads = 256;     // of a workgroup
+inline int log2_of(int page)
+{
+    int n = 0;
+    while ((1 << n) < page) ++n;
+    return n;
+}
 
 // The kernels of attention over the cache: rows per workgroup are 16 * row_blocks, `grid` workgroups share the units of work.
 struct CachePlan {

@@ -1,6 +1,7 @@
 // The paged 8-bit cache: tokens enter (write), come back (read), and pages are chosen by their pseudo-averages (score, pick).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 #include "pasa_cache.h"
 
@@ -22,29 +23,66 @@ __device__ inline float sticky_quotient(float x, float scale, float inverse)
     return __uint_as_float(bits);
 }
 
-// Eight values of a token -> eight bytes.  `top`: the largest magnitude of the token as bits (a NaN is above all others).
+constexpr float kRound = 12582912.f + 128.f;     // 1.5 2^23: a sum with it is rounded to whole numbers, and its low byte is number + 128
+
+// Eight values of a token -> eight bytes, and the numbers that they hold.  `top`: the largest magnitude of the token, NaN where one is.
+// x * (1 / scale) is off by two steps of fp32 at most, which matters next to a tie only: one wavefront in ten finds such a value among its
+// 512 and takes the exact quotient.  (Exact ones for all: 28 instructions a value instead of 10; four prompts of 20000 tokens in all 32.7 us.)
 template <bool E4M3>
-__device__ inline uint2 encode8(const float (&x)[8], unsigned top, float& scale)
+__device__ inline uint2 encode8(const float (&x)[8], float top, float& scale, float (&held)[8])
 {
     constexpr float most = E4M3 ? 448.f : 127.f;
-    const bool finite = top < 0x7f800000u;
-    scale = __uint_as_float(top) / most;
-    if (top < 0x0d800000u) scale = 1.f;          // below 2^-100
+    const bool finite = top < __builtin_inff();
+    scale = top / most;
+    if (top < 0x1p-100f) scale = 1.f;
     if (!finite) scale = __builtin_nanf("");
     const float inverse = 1.f / scale;
+    float q[8];
+    bool near = false;
+    if constexpr (E4M3) {
+        // borders: the 20 bits of the quotient behind e4m3's three are a half; below 2^-6 the steps no longer shrink
+        unsigned border = ~0u, small = ~0u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            q[i] = x[i] * inverse;
+            const unsigned u = __float_as_uint(q[i]), d = (u - 0x7fffcu) & 0xfffffu, s = 2u * u - 1u;
+            border = d < border ? d : border;
+            small = s < small ? s : small;
+        }
+        near = border <= 8u || small < 2u * 0x3c800000u - 1u;
+    } else {
+        float off = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            q[i] = __builtin_fmaf(x[i], inverse, kRound);
+            held[i] = q[i] - kRound;
+            off = __builtin_fmaxf(off, __builtin_fabsf(__builtin_fmaf(x[i], inverse, -held[i])));
+        }
+        near = off > 0.5f - 0x1p-15f;
+    }
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(near && finite) != 0ull, 0)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float e = __builtin_fminf(__builtin_fmaxf(sticky_quotient(x[i], scale, inverse), -most), most);
+            q[i] = E4M3 ? e : e + kRound;        // the sum rounds the sticky quotient once
+            if (!E4M3) held[i] = q[i] - kRound;
+        }
+    }
     unsigned w[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        float q[4];
+        if constexpr (E4M3) {
+            const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * h], q[4 * h + 1], 0, false);
+            w[h] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(q[4 * h + 2], q[4 * h + 3], lo, true);
+            if (!finite) w[h] = 0u;
+            float z[4];
+            widen4<true>(w[h], z);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = finite ? __builtin_fminf(__builtin_fmaxf(sticky_quotient(x[4 * h + i], scale, inverse), -most), most) : 0.f;
-        if (E4M3) {
-            const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
-            w[h] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], lo, true);
+            for (int i = 0; i < 4; ++i) held[4 * h + i] = z[i];
         } else {
-            w[h] = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[h] |= (unsigned)((int)__builtin_rintf(q[i]) + 128) << (8 * i);
+            const unsigned lo = __builtin_amdgcn_perm(__float_as_uint(q[4 * h + 1]), __float_as_uint(q[4 * h]), 0x0c0c0400u);
+            w[h] = lo | __builtin_amdgcn_perm(__float_as_uint(q[4 * h + 3]), __float_as_uint(q[4 * h + 2]), 0x04000c0cu);
+            if (!finite) w[h] = 0x80808080u;
         }
     }
     return make_uint2(w[0], w[1]);
@@ -52,33 +90,58 @@ __device__ inline uint2 encode8(const float (&x)[8], unsigned top, float& scale)
 
 __device__ inline void widen_io(u16x8 raw, int io_bf16, float (&x)[8])
 {
+    if (io_bf16) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        x[i] = io_bf16 ? __uint_as_float((unsigned)raw[i] << 16) : (float)__builtin_bit_cast(_Float16, (unsigned short)raw[i]);
+        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float((unsigned)raw[i] << 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = (float)__builtin_bit_cast(_Float16, (unsigned short)raw[i]);
+    }
+}
+
+// Largest of x over LANES neighbouring lanes (8 or 16), NaN where one is
+template <int LANES>
+__device__ inline float largest(float x)
+{
+    auto with = [&](auto control) {
+        const float y = __uint_as_float((unsigned)__builtin_amdgcn_update_dpp((int)__float_as_uint(x), (int)__float_as_uint(x), decltype(control)::value, 0xf, 0xf, false));
+        x = __builtin_elementwise_maximum(x, y);
+    };
+    with(std::integral_constant<int, 0xb1>{});       // lane ^ 1, ^ 2 (quads), 7 - lane of 8, 15 - lane of 16
+    with(std::integral_constant<int, 0x4e>{});
+    with(std::integral_constant<int, 0x141>{});
+    if (LANES == 16) with(std::integral_constant<int, 0x140>{});
+    return x;
 }
 
 // One workgroup per page that is written to and KV head: D / 8 neighbouring lanes take a token.  Where means are kept, the page's
 // older tokens are read too: a mean made from all tokens is the same whatever the steps that brought them, and writing a
 // token again corrects it.  Partial sums of the lanes that share channels are added in a fixed order.
+// What bounds it: a step, what hangs on one another (lengths, table, tokens; 5 us); prompts, memory.
 template <int D, bool E4M3>
 __global__ __launch_bounds__(kCacheThreads)
 void pasa_cache_write_k(pasa_cache c, const unsigned short* __restrict__ k, const unsigned short* __restrict__ v, int R, long long row_stride,
-                        const int* __restrict__ row_start, int io_bf16, FastDiv heads)
+                        const int* __restrict__ row_start, int io_bf16, int page_log2, FastDiv heads)
 {
-    constexpr int LT = D / 8, AT = kCacheThreads / LT;           // lanes of a token, tokens at a time
-    __shared__ float sums[AT][D];
+    constexpr int LT = D / 8, AT = kCacheThreads / LT, BATCH = 4;        // lanes of a token, tokens at a time, of which so many are on their way
+    __shared__ __attribute__((aligned(16))) float sums[AT][D];
     const int tid = threadIdx.x, lt = tid % LT, t0 = tid / LT;
-    const int most = c.table_width * c.page;
+    const int most = c.table_width << page_log2;
     // workgroups of a page's heads follow one another
     const unsigned piece = heads.quotient(blockIdx.x);
     const int hk = (int)heads.rest(blockIdx.x, piece);
-    auto first_page = [&](const Sequence& s) { return (s.length > s.rows ? s.length - s.rows : 0) / c.page; };
+    f4 shift[2] = {(f4)0.f, (f4)0.f};
+    if (c.kshift != nullptr) {
+        shift[0] = *reinterpret_cast<const f4*>(c.kshift + hk * D + 8 * lt);
+        shift[1] = *reinterpret_cast<const f4*>(c.kshift + hk * D + 8 * lt + 4);
+    }
+    auto first_page = [&](const Sequence& s) { return (s.length > s.rows ? s.length - s.rows : 0) >> page_log2; };
     const Place at = find_place<kCacheThreads>(c.length, row_start, c.S, R, most, [&](const Sequence& s) {
-        return s.rows == 0 || s.length == 0 ? 0u : (unsigned)((s.length - 1) / c.page - first_page(s) + 1);
+        return s.rows == 0 || s.length == 0 ? 0u : (unsigned)(((s.length - 1) >> page_log2) - first_page(s) + 1);
     }, [&](unsigned) { return piece; });
     if (at.b < 0) return;
     const Sequence s = at.s;
-    const int place = first_page(s) + (int)at.rest, pos0 = place * c.page;
+    const int place = first_page(s) + (int)at.rest, pos0 = place << page_log2;
     const int id = c.table[(size_t)at.b * c.table_width + place];
     if (id < 0 || id >= c.pages) return;
     const int tokens = s.length - pos0 < c.page ? s.length - pos0 : c.page;      // of the page
@@ -86,60 +149,66 @@ void pasa_cache_write_k(pasa_cache c, const unsigned short* __restrict__ k, cons
     const size_t slot = ((size_t)id * c.Hkv + hk) * c.page;
     unsigned char* kc = static_cast<unsigned char*>(c.k) + slot * D;
     unsigned char* vc = static_cast<unsigned char*>(c.v) + slot * D;
-    float shift[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) shift[i] = c.kshift != nullptr ? c.kshift[hk * D + 8 * lt + i] : 0.f;
+    const bool means = c.kmean != nullptr;
 
-    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const int start = c.kmean != nullptr || fresh < 0 ? 0 : fresh / AT * AT;
-    for (int t = start + t0; t - t0 < tokens; t += AT) {                         // all lanes of a token go round together
-        if (t >= tokens) continue;
-        uint2 code;
-        float scale;
-        if (t >= fresh) {
-            const size_t row = (size_t)(s.row0 + t - fresh) * (size_t)row_stride + (size_t)hk * D + 8 * lt;
-            float x[8], y[8];
-            widen_io(*reinterpret_cast<const u16x8*>(k + row), io_bf16, x);
-            widen_io(*reinterpret_cast<const u16x8*>(v + row), io_bf16, y);
-            unsigned top_k = 0, top_v = 0;
+    f4 sum[2] = {(f4)0.f, (f4)0.f};
+    for (int begin = means || fresh < 0 ? 0 : fresh / AT * AT; begin < tokens; begin += BATCH * AT) {
+        u16x8 kraw[BATCH], vraw[BATCH];
+        uint2 older[BATCH];
+        float older_scale[BATCH];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[i] -= shift[i];
-                const unsigned a = __float_as_uint(x[i]) & 0x7fffffffu, b = __float_as_uint(y[i]) & 0x7fffffffu;
-                top_k = a > top_k ? a : top_k;
-                top_v = b > top_v ? b : top_v;
+        for (int j = 0; j < BATCH; ++j) {
+            const int t = begin + j * AT + t0;
+            if (t < tokens && t >= fresh) {
+                const size_t row = (size_t)(s.row0 + t - fresh) * (size_t)row_stride + (size_t)hk * D + 8 * lt;
+                kraw[j] = *reinterpret_cast<const u16x8*>(k + row);
+                vraw[j] = *reinterpret_cast<const u16x8*>(v + row);
             }
-#pragma unroll
-            for (int o = 1; o < LT; o <<= 1) {
-                const unsigned a = __shfl_xor(top_k, o), b = __shfl_xor(top_v, o);
-                top_k = a > top_k ? a : top_k;
-                top_v = b > top_v ? b : top_v;
+            if (t < tokens && t < fresh && means) {
+                older[j] = *reinterpret_cast<const uint2*>(kc + (size_t)t * D + 8 * lt);
+                older_scale[j] = c.kscale[slot + t];
             }
-            float vscale;
-            const uint2 vcode = encode8<E4M3>(y, top_v, vscale);
-            code = encode8<E4M3>(x, top_k, scale);
-            *reinterpret_cast<uint2*>(kc + (size_t)t * D + 8 * lt) = code;
-            *reinterpret_cast<uint2*>(vc + (size_t)t * D + 8 * lt) = vcode;
-            if (lt == 0) {
-                c.kscale[slot + t] = scale;
-                c.vscale[slot + t] = vscale;
-            }
-        } else {
-            if (c.kmean == nullptr) continue;
-            code = *reinterpret_cast<const uint2*>(kc + (size_t)t * D + 8 * lt);
-            scale = c.kscale[slot + t];
         }
-        float z[4];
-        widen4<E4M3>(code.x, z);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf(z[i], scale, sum[i]);
-        widen4<E4M3>(code.y, z);
+        for (int j = 0; j < BATCH; ++j) {
+            const int t = begin + j * AT + t0;
+            if (t >= tokens) continue;                           // all lanes of a token go the same way
+            float held[8], scale;
+            if (t >= fresh) {
+                float x[8], y[8], unused[8], vscale;
+                widen_io(kraw[j], io_bf16, x);
+                widen_io(vraw[j], io_bf16, y);
+                float top_k = 0.f, top_v = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[4 + i] = __builtin_fmaf(z[i], scale, sum[4 + i]);
+                for (int i = 0; i < 8; ++i) {
+                    x[i] -= shift[i >> 2][i & 3];
+                    top_k = __builtin_elementwise_maximum(top_k, __builtin_fabsf(x[i]));
+                    top_v = __builtin_elementwise_maximum(top_v, __builtin_fabsf(y[i]));
+                }
+                const uint2 vcode = encode8<E4M3>(y, largest<LT>(top_v), vscale, unused);
+                const uint2 code = encode8<E4M3>(x, largest<LT>(top_k), scale, held);
+                *reinterpret_cast<uint2*>(kc + (size_t)t * D + 8 * lt) = code;
+                *reinterpret_cast<uint2*>(vc + (size_t)t * D + 8 * lt) = vcode;
+                if (lt == 0) {
+                    c.kscale[slot + t] = scale;
+                    c.vscale[slot + t] = vscale;
+                }
+            } else {
+                if (!means) continue;
+                float lo[4], hi[4];
+                widen4<E4M3>(older[j].x, lo);
+                widen4<E4M3>(older[j].y, hi);
+                scale = older_scale[j];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) held[i] = lo[i], held[4 + i] = hi[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i >> 2][i & 3] = __builtin_fmaf(held[i], scale, sum[i >> 2][i & 3]);
+        }
     }
-    if (c.kmean == nullptr) return;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sums[t0][8 * lt + i] = sum[i];
+    if (!means) return;
+    *reinterpret_cast<f4*>(&sums[t0][8 * lt]) = sum[0];
+    *reinterpret_cast<f4*>(&sums[t0][8 * lt + 4]) = sum[1];
     __syncthreads();
     if (tid < D) {
         float total = 0.f;
@@ -151,58 +220,64 @@ void pasa_cache_write_k(pasa_cache c, const unsigned short* __restrict__ k, cons
 
 // ---- tokens come back ----
 
-// D / 16 neighbouring lanes take a token, 16 channels each; a workgroup takes kReadTokens positions of one sequence and head.
+// D / 8 neighbouring lanes take a token, eight channels each, so that a wavefront's stores are 1 KiB of neighbouring bytes; a workgroup takes
+// kReadTokens positions of one sequence and head.  The loads of a step are asked for together: places, then codes and scales.
 constexpr int kReadTokens = 128;
 template <int D, bool E4M3>
 __global__ __launch_bounds__(kCacheThreads)
 void pasa_cache_read_k(pasa_cache c, unsigned short* __restrict__ k, unsigned short* __restrict__ v, const int* __restrict__ first, int N,
-                       int io_bf16, FastDiv heads, FastDiv chunks)
+                       int io_bf16, int page_log2, FastDiv heads, FastDiv chunks)
 {
-    constexpr int LT = D / 16, AT = kCacheThreads / LT, PASSES = kReadTokens / AT;
+    constexpr int LT = D / 8, AT = kCacheThreads / LT, BATCH = 4;
     const int tid = threadIdx.x, lt = tid % LT, t0 = tid / LT;
     const unsigned up = chunks.quotient(blockIdx.x);
     const int n0 = (int)chunks.rest(blockIdx.x, up) * kReadTokens;
     const int b = (int)heads.quotient(up), hk = (int)heads.rest(up, (unsigned)b);
-    const int length = clamp_int(c.length[b], 0, c.table_width * c.page), begin = first != nullptr ? first[b] : 0;
-    float shift[16];
+    const int length = clamp_int(c.length[b], 0, c.table_width << page_log2), begin = first != nullptr ? first[b] : 0;
+    f4 shift[2] = {(f4)0.f, (f4)0.f};
+    if (c.kshift != nullptr) {
+        shift[0] = *reinterpret_cast<const f4*>(c.kshift + hk * D + 8 * lt);
+        shift[1] = *reinterpret_cast<const f4*>(c.kshift + hk * D + 8 * lt + 4);
+    }
+    for (int n1 = n0; n1 < n0 + kReadTokens && n1 < N; n1 += BATCH * AT) {
+        int id[BATCH], pos[BATCH];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) shift[i] = c.kshift != nullptr ? c.kshift[hk * D + 16 * lt + i] : 0.f;
-#pragma unroll
-    for (int p = 0; p < PASSES; ++p) {
-        const int n = n0 + p * AT + t0;
-        if (n >= N) break;
-        const long long pos = (long long)begin + n;
-        uint4 code[2];
-        float scale[2] = {0.f, 0.f};
-        bool there = pos >= 0 && pos < length;
-        if (there) {
-            const int place = (int)pos / c.page, id = c.table[(size_t)b * c.table_width + place];
-            there = id >= 0 && id < c.pages;
-            if (there) {
-                const size_t slot = ((size_t)id * c.Hkv + hk) * c.page + (size_t)((int)pos - place * c.page);
-                code[0] = *reinterpret_cast<const uint4*>(static_cast<const unsigned char*>(c.k) + slot * D + 16 * lt);
-                code[1] = *reinterpret_cast<const uint4*>(static_cast<const unsigned char*>(c.v) + slot * D + 16 * lt);
-                scale[0] = c.kscale[slot];
-                scale[1] = c.vscale[slot];
-            }
+        for (int j = 0; j < BATCH; ++j) {
+            const long long p = (long long)begin + n1 + j * AT + t0;
+            const bool in = n1 + j * AT + t0 < N && p >= 0 && p < length;
+            pos[j] = in ? (int)p : -1;
+            id[j] = c.table[(size_t)b * c.table_width + (in ? (int)p >> page_log2 : 0)];
         }
-        const size_t to = (((size_t)b * heads.d + hk) * N + n) * D + 16 * lt;
+        uint2 code[BATCH][2];
+        float scale[BATCH][2];
 #pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            unsigned out[8];
-            const unsigned w[4] = {code[which].x, code[which].y, code[which].z, code[which].w};
+        for (int j = 0; j < BATCH; ++j) {
+            if (pos[j] < 0 || id[j] < 0 || id[j] >= c.pages) pos[j] = -1;
+            const size_t slot = pos[j] < 0 ? 0 : (((size_t)id[j] * c.Hkv + hk) << page_log2) + (size_t)(pos[j] & (c.page - 1));
+            code[j][0] = *reinterpret_cast<const uint2*>(static_cast<const unsigned char*>(c.k) + slot * D + 8 * lt);
+            code[j][1] = *reinterpret_cast<const uint2*>(static_cast<const unsigned char*>(c.v) + slot * D + 8 * lt);
+            scale[j][0] = c.kscale[slot];
+            scale[j][1] = c.vscale[slot];
+        }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float x[4];
-                widen4<E4M3>(w[j], x);
+        for (int j = 0; j < BATCH; ++j) {
+            const int n = n1 + j * AT + t0;
+            if (n >= N) break;
+            const size_t to = (((size_t)b * heads.d + hk) * N + n) * D + 8 * lt;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = there ? __builtin_fmaf(x[i], scale[which], which == 0 ? shift[4 * j + i] : 0.f) : 0.f;
-                out[2 * j] = io_bf16 ? pack_bf16(x[0], x[1]) : pack_f16(x[0], x[1]);
-                out[2 * j + 1] = io_bf16 ? pack_bf16(x[2], x[3]) : pack_f16(x[2], x[3]);
+            for (int which = 0; which < 2; ++which) {
+                unsigned out[4];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float x[4];
+                    widen4<E4M3>(h == 0 ? code[j][which].x : code[j][which].y, x);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = pos[j] >= 0 ? __builtin_fmaf(x[i], scale[j][which], which == 0 ? shift[h][i] : 0.f) : 0.f;
+                    out[2 * h] = io_bf16 ? pack_bf16(x[0], x[1]) : pack_f16(x[0], x[1]);
+                    out[2 * h + 1] = io_bf16 ? pack_bf16(x[2], x[3]) : pack_f16(x[2], x[3]);
+                }
+                *reinterpret_cast<uint4*>((which == 0 ? k : v) + to) = make_uint4(out[0], out[1], out[2], out[3]);
             }
-            uint4* dst = reinterpret_cast<uint4*>((which == 0 ? k : v) + to);
-            dst[0] = make_uint4(out[0], out[1], out[2], out[3]);
-            dst[1] = make_uint4(out[4], out[5], out[6], out[7]);
         }
     }
 }
@@ -219,143 +294,177 @@ __device__ inline unsigned long long order_of(double x)
     return (u >> 63) != 0 ? ~u : u | 0x8000000000000000ull;
 }
 
-// Four neighbouring lanes take a page, a quarter of the channels each; a workgroup takes 64 pages of one sequence and head.
+// One wavefront takes 16 pages of a sequence and head, on v_mfma_f64_16x16x4f64: rows of queries times means, lane l with g = l / 16 holding
+// a quarter of the channels (D / 4 from D / 4 * g on; which channels a k-step consists of is free) of query row and of page l % 16.
 // The products of fp16 queries and fp32 means are exact in 64 bits, and so, nearly, are their sums: which pages are chosen does
-// not depend on an order of additions unless two scores agree to 15 digits.
+// not depend on an order of additions unless two scores agree to 15 digits.  The matrix unit's rate in 64 bits is far from bounding it (16 steps of
+// 16 sequences of 512 pages on 4 heads: 1 us of it); what hangs on one another does: lengths, table, means.
+typedef double d4 __attribute__((ext_vector_type(4)));
 template <int D>
 __global__ __launch_bounds__(kCacheThreads)
 void pasa_cache_score_k(pasa_cache c, const unsigned short* __restrict__ q, int R, long long row_stride, const int* __restrict__ row_start,
-                        int G, int head, int tail, int io_bf16, FastDiv heads, FastDiv chunks, unsigned long long* __restrict__ scores)
+                        int head, int tail, int io_bf16, int page_log2, FastDiv G, FastDiv heads, FastDiv chunks, unsigned long long* __restrict__ scores)
 {
-    constexpr int CH = D / 4, ROWS = 8;          // channels of a lane, rows that wait in LDS at a time
-    __shared__ double rows[ROWS][D + 2];
-    const int tid = threadIdx.x, quarter = tid & 3;
+    constexpr int CH = D / 4;                    // channels of a lane
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
     const unsigned up = chunks.quotient(blockIdx.x);
     const int b = (int)heads.quotient(up), hk = (int)heads.rest(up, (unsigned)b);
-    const int p = (int)chunks.rest(blockIdx.x, up) * (kCacheThreads / 4) + tid / 4;
-    const Sequence s = sequence_at(c.length, row_start, b, R, c.table_width * c.page);
-    const int pages = (s.length + c.page - 1) / c.page;
-    if ((int)chunks.rest(blockIdx.x, up) * (kCacheThreads / 4) >= pages || s.rows == 0) return;      // nobody reads these words
-    const int id = p < pages ? c.table[(size_t)b * c.table_width + p] : -1;
-    const bool there = id >= 0 && id < c.pages;
-    double mean[CH];
+    const int p0 = (int)chunks.rest(blockIdx.x, up) * 64 + 16 * (int)(threadIdx.x >> 6), p = p0 + l16;
+    const int wanted = p < c.table_width ? p : c.table_width - 1;
+    const int id_read = c.table[(size_t)b * c.table_width + wanted];
+    const Sequence s = sequence_at(c.length, row_start, b, R, c.table_width << page_log2);
+    const int pages = (s.length + c.page - 1) >> page_log2;
+    if (p0 >= pages || s.rows == 0) return;      // nobody reads these words
+    const bool there = p < pages && id_read >= 0 && id_read < c.pages;
+    const float* mean = c.kmean + ((size_t)(there ? id_read : 0) * c.Hkv + hk) * D + CH * g;
+    f4 m[CH / 4];
 #pragma unroll
-    for (int i = 0; i < CH; i += 4) {
-        f4 x = (f4)0.f;
-        if (there) x = *reinterpret_cast<const f4*>(c.kmean + ((size_t)id * c.Hkv + hk) * D + CH * quarter + i);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) mean[i + e] = (double)x[e];
-    }
+    for (int i = 0; i < CH / 4; ++i) m[i] = *reinterpret_cast<const f4*>(mean + 4 * i);
     double best = -__builtin_inf();
     bool nan = false;
-    const int all = s.rows * G;
-    for (int r0 = 0; r0 < all; r0 += ROWS) {
-        __syncthreads();
-        for (int i = tid; i < ROWS * D; i += kCacheThreads) {
-            const int r = r0 + i / D, ch = i % D;
-            if (r < all) {
-                const unsigned short raw = q[(size_t)(s.row0 + r / G) * (size_t)row_stride + (size_t)(hk * G + r % G) * D + ch];
-                rows[i / D][ch] = io_bf16 ? (double)__uint_as_float((unsigned)raw << 16) : (double)__builtin_bit_cast(_Float16, raw);
-            }
-        }
-        __syncthreads();
-        const int here = all - r0 < ROWS ? all - r0 : ROWS;
-        for (int r = 0; r < here; ++r) {
-            double x = 0.0;
+    const int all = s.rows * (int)G.d;
+    for (int r0 = 0; r0 < all; r0 += 16) {
+        const int r = r0 + l16 < all ? r0 + l16 : all - 1;       // the last one again: the maximum is the same
+        const int t = (int)G.quotient((unsigned)r), h = (int)G.rest((unsigned)r, (unsigned)t);
+        const unsigned short* row = q + (size_t)(s.row0 + t) * (size_t)row_stride + (size_t)(hk * (int)G.d + h) * D + CH * g;
+        u16x8 raw[CH / 8];
 #pragma unroll
-            for (int i = 0; i < CH; ++i) x = __builtin_fma(mean[i], rows[r][CH * quarter + i], x);
-            x += __shfl_xor(x, 1);
-            x += __shfl_xor(x, 2);
-            nan |= x != x;
-            best = __builtin_fmax(best, x);
+        for (int i = 0; i < CH / 8; ++i) raw[i] = *reinterpret_cast<const u16x8*>(row + 8 * i);
+        d4 x = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+        for (int i = 0; i < CH / 8; ++i) {
+            float y[8];
+            widen_io(raw[i], io_bf16, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x = __builtin_amdgcn_mfma_f64_16x16x4f64((double)y[e], (double)m[2 * i + (e >> 2)][e & 3], x, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {            // rows, of page l % 16
+            nan |= x[i] != x[i];
+            best = __builtin_fmax(best, x[i]);
         }
     }
-    if (quarter == 0 && p < pages) {
+    best = __builtin_fmax(best, __shfl_xor(best, 16));
+    best = __builtin_fmax(best, __shfl_xor(best, 32));
+    const unsigned long long nans = __builtin_amdgcn_ballot_w64(nan);
+    nan = ((nans | nans >> 16 | nans >> 32 | nans >> 48) >> l16 & 1ull) != 0ull;
+    if (g == 0 && p < pages) {
         const bool always = p < head || p >= pages - tail;
         scores[((size_t)b * c.Hkv + hk) * c.table_width + p] = always ? kAlways : !there ? 1ull : nan ? kAlways - 1 : order_of(best);
     }
 }
 
-// One workgroup per sequence and head.  The count-th largest word is found digit by digit (8 bits at a time, from the top; done as soon
-// as the words that share the digits so far are all taken); words above it are taken, and of its equals the first.  They leave in order.
-template <int EACH>
-__global__ __launch_bounds__(kPickThreads)
-void pasa_cache_pick_k(pasa_cache c, const int* __restrict__ row_start, int R, int count, FastDiv heads,
+// One workgroup per sequence and head.  The pages that are always taken leave first; of the others the want-th largest word is found
+// digit by digit, 8 bits at a time, from the first bit on that they differ in (sign and exponents of scores are much alike), until
+// the words that share the digits so far are all taken.  Words above it are taken, and of its equals the first.  They leave in order.
+// NT threads of EACH words: 256 of 4 for tables up to 1024 pages.
+template <int NT, int EACH>
+__global__ __launch_bounds__(NT)
+void pasa_cache_pick_k(pasa_cache c, const int* __restrict__ row_start, int R, int count, int page_log2, FastDiv heads,
                        const unsigned long long* __restrict__ scores, int* __restrict__ blocks)
 {
+    constexpr int NW = NT / 64;
     __shared__ unsigned bins[256];
-    __shared__ unsigned sums[kPickThreads / 64][2];
+    __shared__ unsigned sums[NW][2];
+    __shared__ unsigned long long differ[NW][2];
     __shared__ unsigned digit_found, above_found, done;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int b = (int)heads.quotient(blockIdx.x);
-    const Sequence s = sequence_at(c.length, row_start, b, R, c.table_width * c.page);
-    const int pages = s.rows == 0 ? 0 : (s.length + c.page - 1) / c.page;
-    int* out = blocks + (size_t)blockIdx.x * count;
     const unsigned long long* in = scores + (size_t)blockIdx.x * c.table_width;
-    const int taken = pages < count ? pages : count;
-    for (int i = taken + tid; i < count; i += kPickThreads) out[i] = -1;
-    if (pages <= count) {
-        for (int i = tid; i < pages; i += kPickThreads) out[i] = i;
-        return;
-    }
-    // thread t has the words t * EACH .. : in order
+    // thread t has the words t * EACH .. : in order.  Read before the length is there; words behind the last page hold anything.
     unsigned long long word[EACH];
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) word[i] = tid * EACH + i < pages ? in[tid * EACH + i] : 0ull;
-    unsigned long long prefix = 0;               // digits of the count-th largest so far
-    unsigned want = (unsigned)count;             // of the words that share them, so many are taken
-    int shift = 56;
-    for (;; shift -= 8) {
-        if (tid < 256) bins[tid] = 0;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < EACH; ++i)
-            if (shift == 56 || (word[i] >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&bins[(word[i] >> shift) & 255u], 1u);
-        __syncthreads();
-        if (tid < 64) {                          // four bins a lane, from the top: lane 0 has 255 .. 252
-            unsigned mine[4], total = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) total += mine[i] = bins[255 - 4 * lane - i];
-            unsigned upto = total;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const unsigned x = __shfl_up(upto, o);
-                if (lane >= o) upto += x;
-            }
-            unsigned above = upto - total;
-            if (above < want && want <= upto) {
-                int i = 0;
-                while (above + mine[i] < want) above += mine[i++];
-                digit_found = 255u - 4u * lane - i;
-                above_found = above;
-                done = above + mine[i] == want;
-            }
-        }
-        __syncthreads();
-        prefix |= (unsigned long long)digit_found << shift;
-        want -= above_found;
-        if (done || shift == 0) break;
+    for (int i = 0; i < EACH; ++i) word[i] = in[tid * EACH + i < c.table_width ? tid * EACH + i : 0];
+    const Sequence s = sequence_at(c.length, row_start, b, R, c.table_width << page_log2);
+    const int pages = s.rows == 0 ? 0 : (s.length + c.page - 1) >> page_log2;
+    int* out = blocks + (size_t)blockIdx.x * count;
+    const int taken = pages < count ? pages : count;
+    for (int i = taken + tid; i < count; i += NT) out[i] = -1;
+    if (pages <= count) {
+        for (int i = tid; i < pages; i += NT) out[i] = i;
+        return;
     }
-    // words whose digits are above the prefix, and `want` of those that share it
+    unsigned always = 0;
+    unsigned long long ones = ~0ull, any = 0;    // bits that all words have, that one has; of those that are not always taken
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        if (tid * EACH + i >= pages) word[i] = 0ull;
+        else if (word[i] == kAlways) ++always;
+        else ones &= word[i], any |= word[i];
+    }
+    unsigned n_always = scan64(always);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) ones &= __shfl_xor(ones, o), any |= __shfl_xor(any, o);
+    if (lane == 63) sums[wave][0] = n_always, differ[wave][0] = ones, differ[wave][1] = any;
+    __syncthreads();
+    n_always = 0;
+    ones = ~0ull, any = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) n_always += sums[w][0], ones &= differ[w][0], any |= differ[w][1];
+    // `limit`: words above it are taken, of its equals `want`; both seen from bit `shift` on
+    unsigned long long limit = kAlways;
+    unsigned want = (unsigned)count;
+    int shift = 0;
+    if (n_always < want) {
+        want -= n_always;
+        const unsigned long long mixed = ones ^ any;
+        const int top = mixed == 0ull ? 0 : 63 - __builtin_clzll(mixed);         // the first bit that words differ in
+        shift = top < 7 ? 0 : top - 7;
+        limit = any & ~(shift + 8 < 64 ? (1ull << (shift + 8)) - 1ull : ~0ull);  // what they share above it
+        for (;;) {
+            for (int i = tid; i < 256; i += NT) bins[i] = 0;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < EACH; ++i)
+                if (tid * EACH + i < pages && word[i] != kAlways && (shift + 8 >= 64 || (word[i] >> (shift + 8)) == (limit >> (shift + 8))))
+                    atomicAdd(&bins[(word[i] >> shift) & 255u], 1u);
+            __syncthreads();
+            if (tid < 64) {                      // four bins a lane, from the top: lane 0 has 255 .. 252
+                unsigned mine[4], total = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) total += mine[i] = bins[255 - 4 * lane - i];
+                const unsigned upto = scan64(total);
+                unsigned above = upto - total;
+                if (above < want && want <= upto) {
+                    int i = 0;
+#pragma unroll
+                    for (int j = 0; j < 3; ++j)
+                        if (i == j && above + mine[j] < want) above += mine[j], ++i;
+                    const unsigned here = i == 0 ? mine[0] : i == 1 ? mine[1] : i == 2 ? mine[2] : mine[3];
+                    digit_found = 255u - 4u * lane - i;
+                    above_found = above;
+                    done = above + here == want;
+                }
+            }
+            __syncthreads();
+            limit |= (unsigned long long)digit_found << shift;
+            want -= above_found;
+            if (done || shift == 0) break;
+            shift = shift < 8 ? 0 : shift - 8;
+            limit &= ~((1ull << (shift + 8)) - 1ull);            // digits overlap where fewer than 8 bits are left
+        }
+    }
+    // pages that are always taken count as above, or, where there are more of them than wanted, as the equals
+    const bool room = n_always < (unsigned)count;
+    auto is_above = [&](unsigned long long x) { return x == kAlways ? room : (x >> shift) > (limit >> shift); };
+    auto is_equal = [&](unsigned long long x) { return x == kAlways ? !room : (x >> shift) == (limit >> shift); };
     unsigned above = 0, equal = 0;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-        above += (word[i] >> shift) > (prefix >> shift);
-        equal += (word[i] >> shift) == (prefix >> shift);
+        above += is_above(word[i]);
+        equal += is_equal(word[i]);
     }
-    unsigned up_a = above, up_e = equal;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const unsigned x = __shfl_up(up_a, o), y = __shfl_up(up_e, o);
-        if (lane >= o) up_a += x, up_e += y;
-    }
-    if (lane == 63) sums[wave][0] = up_a, sums[wave][1] = up_e;
+    unsigned at_a = scan64(above), at_e = scan64(equal);
     __syncthreads();
-    unsigned at_a = up_a - above, at_e = up_e - equal;
-    for (int w = 0; w < wave; ++w) at_a += sums[w][0], at_e += sums[w][1];
+    if (lane == 63) sums[wave][0] = at_a, sums[wave][1] = at_e;
+    __syncthreads();
+    at_a -= above, at_e -= equal;
+#pragma unroll
+    for (int w = 0; w < NW; ++w)
+        if (w < wave) at_a += sums[w][0], at_e += sums[w][1];
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-        const bool a = (word[i] >> shift) > (prefix >> shift), e = (word[i] >> shift) == (prefix >> shift);
+        const bool a = is_above(word[i]), e = is_equal(word[i]);
         if (a || (e && at_e < want)) out[at_a + (at_e < want ? at_e : want)] = tid * EACH + i;
         at_a += a;
         at_e += e;
@@ -372,7 +481,7 @@ hipError_t pasa_launch_cache_write(const pasa_cache& c, const void* k, const voi
     const unsigned grid = (unsigned)((pages < R ? pages : R) * c.Hkv);
     auto go = [&](auto kernel) {
         kernel<<<grid, kCacheThreads, 0, stream>>>(c, static_cast<const unsigned short*>(k), static_cast<const unsigned short*>(v), R, row_stride,
-                                                   row_start, io_bf16, fast_div(c.Hkv));
+                                                   row_start, io_bf16, log2_of(c.page), fast_div(c.Hkv));
     };
     const bool e = c.format == PASA_CACHE_E4M3;
     if (c.d == 128) e ? go(pasa_cache_write_k<128, true>) : go(pasa_cache_write_k<128, false>);
@@ -384,7 +493,7 @@ hipError_t pasa_launch_cache_read(const pasa_cache& c, void* k, void* v, const i
 {
     const unsigned chunks = (unsigned)((N + kReadTokens - 1) / kReadTokens), grid = chunks * (unsigned)c.S * (unsigned)c.Hkv;
     auto go = [&](auto kernel) {
-        kernel<<<grid, kCacheThreads, 0, stream>>>(c, static_cast<unsigned short*>(k), static_cast<unsigned short*>(v), first, N, io_bf16,
+        kernel<<<grid, kCacheThreads, 0, stream>>>(c, static_cast<unsigned short*>(k), static_cast<unsigned short*>(v), first, N, io_bf16, log2_of(c.page),
                                                    fast_div(c.Hkv), fast_div(chunks));
     };
     const bool e = c.format == PASA_CACHE_E4M3;
@@ -399,18 +508,18 @@ hipError_t pasa_launch_cache_choose(const pasa_cache& c, const void* q, int R, l
     if (c.table_width > count) {                 // otherwise all pages are taken
         const unsigned chunks = (unsigned)((c.table_width + 63) / 64), grid = chunks * (unsigned)c.S * (unsigned)c.Hkv;
         auto score = [&](auto kernel) {
-            kernel<<<grid, kCacheThreads, 0, stream>>>(c, static_cast<const unsigned short*>(q), R, row_stride, row_start, Hq / c.Hkv, head, tail,
-                                                       io_bf16, fast_div(c.Hkv), fast_div(chunks), scores);
+            kernel<<<grid, kCacheThreads, 0, stream>>>(c, static_cast<const unsigned short*>(q), R, row_stride, row_start, head, tail, io_bf16, log2_of(c.page),
+                                                       fast_div((unsigned)(Hq / c.Hkv)), fast_div(c.Hkv), fast_div(chunks), scores);
         };
         c.d == 128 ? score(pasa_cache_score_k<128>) : score(pasa_cache_score_k<64>);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    auto pick = [&](auto kernel) {
-        kernel<<<(unsigned)c.S * (unsigned)c.Hkv, kPickThreads, 0, stream>>>(c, row_start, R, count, fast_div(c.Hkv), scores, blocks);
+    auto pick = [&](auto kernel, int threads) {
+        kernel<<<(unsigned)c.S * (unsigned)c.Hkv, threads, 0, stream>>>(c, row_start, R, count, log2_of(c.page), fast_div(c.Hkv), scores, blocks);
     };
-    if (c.table_width <= kPickThreads) pick(pasa_cache_pick_k<1>);
-    else if (c.table_width <= 4 * kPickThreads) pick(pasa_cache_pick_k<4>);
-    else pick(pasa_cache_pick_k<16>);            // the largest table: 262144 tokens in pages of 16
+    if (c.table_width <= 1024) pick(pasa_cache_pick_k<256, 4>, 256);
+    else if (c.table_width <= 4096) pick(pasa_cache_pick_k<1024, 4>, 1024);
+    else pick(pasa_cache_pick_k<1024, 16>, 1024);            // the largest table: 262144 tokens in pages of 16
     return hipGetLastError();
 }
