@@ -123,7 +123,9 @@ def lib() -> ctypes.CDLL:
         calls = None
     for name, in_c, in_ctypes in (("pasa_attn_fwd", "plain", _plain), ("pasa_attn_fwd_ex", "whole", _whole),
                                   ("pasa_attn_fwd_adaptive", "whole", _whole), ("pasa_prepare_kv", "prepare", _prepare),
-                                  ("pasa_attn_fwd_chunk", "chunk", _chunk)):
+                                  ("pasa_attn_fwd_chunk", "chunk", _chunk), ("pasa_cache_write", "cache_write", _cache_write),
+                                  ("pasa_cache_read", "cache_read", _cache_read), ("pasa_cache_choose", "cache_choose", _cache_choose),
+                                  ("pasa_attn_cache", "attn_cache", _attn_cache)):
         f = getattr(L, name)
         call = functools.partial(in_ctypes, f)
         if calls is not None:
@@ -174,6 +176,24 @@ def _chunk(f, q, o, B, Hq, Hkv, Nq, row0, N, d, causal, scale, workspace, worksp
     opts = _opts(*opts)
     return f(_ptr(q), _ptr(o), B, Hq, Hkv, Nq, row0, N, d, int(causal), float(scale), opts, _ptr(workspace), int(workspace_bytes),
              _stream(stream))
+
+
+def _cache_write(f, cache, k, v, R, row_stride, row_start, stream, io_dtype):
+    return f(_ptr(cache), _ptr(k), _ptr(v), R, row_stride, _ptr(row_start), int(io_dtype), _stream(stream))
+
+
+def _cache_read(f, cache, k, v, first, N, stream, io_dtype):
+    return f(_ptr(cache), _ptr(k), _ptr(v), _ptr(first), N, int(io_dtype), _stream(stream))
+
+
+def _cache_choose(f, cache, q, R, row_stride, row_start, Hq, blocks, count, head, tail, workspace, workspace_bytes, stream, io_dtype):
+    return f(_ptr(cache), _ptr(q), R, row_stride, _ptr(row_start), Hq, _ptr(blocks), count, head, tail, int(io_dtype), _ptr(workspace),
+             int(workspace_bytes), _stream(stream))
+
+
+def _attn_cache(f, cache, q, o, R, row_stride, row_start, Hq, scale, workspace, workspace_bytes, stream, tree, blocks, count, io_dtype):
+    return f(_ptr(cache), _ptr(q), _ptr(o), R, row_stride, _ptr(row_start), Hq, float(scale), _ptr(tree), _ptr(blocks), count, int(io_dtype),
+             _ptr(workspace), int(workspace_bytes), _stream(stream))
 
 
 def _check(status: int, what: str, check: bool):
@@ -289,12 +309,12 @@ def pasa_attn_fwd_adaptive(q, k, v, o, B, Hq, Hkv, N, d, causal, scale, workspac
 
 
 def pasa_cache_write(cache, k, v, R, row_stride, row_start, stream=None, io_dtype=IO_F16, check=True) -> int:
-    st = lib().pasa_cache_write(_ptr(cache), _ptr(k), _ptr(v), R, row_stride, _ptr(row_start), int(io_dtype), _stream(stream))
+    st = (_lib or lib()).call_pasa_cache_write(cache, k, v, R, row_stride, row_start, stream, io_dtype)
     return _check(st, "pasa_cache_write", check)
 
 
 def pasa_cache_read(cache, k, v, first, N, stream=None, io_dtype=IO_F16, check=True) -> int:
-    st = lib().pasa_cache_read(_ptr(cache), _ptr(k), _ptr(v), _ptr(first), N, int(io_dtype), _stream(stream))
+    st = (_lib or lib()).call_pasa_cache_read(cache, k, v, first, N, stream, io_dtype)
     return _check(st, "pasa_cache_read", check)
 
 
@@ -304,8 +324,8 @@ def pasa_cache_choose_workspace(cache) -> int:
 
 def pasa_cache_choose(cache, q, R, row_stride, row_start, Hq, blocks, count, head, tail, workspace, workspace_bytes, stream=None,
                       io_dtype=IO_F16, check=True) -> int:
-    st = lib().pasa_cache_choose(_ptr(cache), _ptr(q), R, row_stride, _ptr(row_start), Hq, _ptr(blocks), count, head, tail, int(io_dtype),
-                                 _ptr(workspace), int(workspace_bytes), _stream(stream))
+    st = (_lib or lib()).call_pasa_cache_choose(cache, q, R, row_stride, row_start, Hq, blocks, count, head, tail, workspace, workspace_bytes,
+                                                stream, io_dtype)
     return _check(st, "pasa_cache_choose", check)
 
 
@@ -315,6 +335,6 @@ def pasa_attn_cache_workspace(cache, R, Hq) -> int:
 
 def pasa_attn_cache(cache, q, o, R, row_stride, row_start, Hq, scale, workspace, workspace_bytes, stream=None, tree=None, blocks=None,
                     count=0, io_dtype=IO_F16, check=True) -> int:
-    st = lib().pasa_attn_cache(_ptr(cache), _ptr(q), _ptr(o), R, row_stride, _ptr(row_start), Hq, float(scale), _ptr(tree), _ptr(blocks), count,
-                               int(io_dtype), _ptr(workspace), int(workspace_bytes), _stream(stream))
+    st = (_lib or lib()).call_pasa_attn_cache(cache, q, o, R, row_stride, row_start, Hq, scale, workspace, workspace_bytes, stream, tree, blocks,
+                                              count, io_dtype)
     return _check(st, "pasa_attn_cache", check)

@@ -196,11 +196,83 @@ static PyObject* chunk(PyObject* self, PyObject* const* a, Py_ssize_t n)
     return PyLong_FromLong(status);
 }
 
+/* 64 bits, as ctypes takes them for a long long */
+static int get_long(PyObject* x, long long* out)
+{
+    if (!PyLong_Check(x)) return 0;
+    *out = (long long)PyLong_AsUnsignedLongLongMask(x);
+    return !PyErr_Occurred();
+}
+
+/* address, ctypes, cache, k, v, R, row stride, row_start, stream, type */
+static PyObject* cache_write(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    void *f, *p[3], *rows, *stream;
+    int R, status;
+    long long stride;
+    unsigned long long type;
+    if (n != 10 || !get_ptr(a[0], &f) || !get_ptrs(a + 2, 3, p) || !get_size(a[5], &R) || !get_long(a[6], &stride) || !get_ptr(a[7], &rows) ||
+        !get_stream(a[8], &stream) || !get_int(a[9], &type))
+        return through_ctypes(a, n);
+    CALL(status, ((int (*)(const void*, const void*, const void*, int, long long, const void*, int, void*))f)(p[0], p[1], p[2], R, stride, rows,
+                                                                                                         (int)(unsigned)type, stream));
+    return PyLong_FromLong(status);
+}
+
+/* address, ctypes, cache, k, v, first, N, stream, type */
+static PyObject* cache_read(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    void *f, *p[4], *stream;
+    int N, status;
+    unsigned long long type;
+    if (n != 9 || !get_ptr(a[0], &f) || !get_ptrs(a + 2, 4, p) || !get_size(a[6], &N) || !get_stream(a[7], &stream) || !get_int(a[8], &type))
+        return through_ctypes(a, n);
+    CALL(status, ((int (*)(const void*, void*, void*, const void*, int, int, void*))f)(p[0], p[1], p[2], p[3], N, (int)(unsigned)type, stream));
+    return PyLong_FromLong(status);
+}
+
+/* address, ctypes, cache, q, R, row stride, row_start, Hq, blocks, count, head, tail, workspace, bytes, stream, type */
+static PyObject* cache_choose(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    void *f, *p[2], *rows, *blocks, *ws, *stream;
+    int R, Hq, s[3], status;
+    long long stride;
+    unsigned long long bytes, type;
+    if (n != 16 || !get_ptr(a[0], &f) || !get_ptrs(a + 2, 2, p) || !get_size(a[4], &R) || !get_long(a[5], &stride) || !get_ptr(a[6], &rows) ||
+        !get_size(a[7], &Hq) || !get_ptr(a[8], &blocks) || !get_sizes(a + 9, 3, s) || !get_ptr(a[12], &ws) || !get_int(a[13], &bytes) ||
+        !get_stream(a[14], &stream) || !get_int(a[15], &type))
+        return through_ctypes(a, n);
+    CALL(status, ((int (*)(const void*, const void*, int, long long, const void*, int, void*, int, int, int, int, void*, size_t, void*))f)(
+                     p[0], p[1], R, stride, rows, Hq, blocks, s[0], s[1], s[2], (int)(unsigned)type, ws, (size_t)bytes, stream));
+    return PyLong_FromLong(status);
+}
+
+/* address, ctypes, cache, q, o, R, row stride, row_start, Hq, scale, workspace, bytes, stream, tree, blocks, count, type */
+static PyObject* attn_cache(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    void *f, *p[3], *rows, *ws, *stream, *tree, *blocks;
+    int R, Hq, count, status;
+    long long stride;
+    unsigned long long bytes, type;
+    float scale;
+    if (n != 17 || !get_ptr(a[0], &f) || !get_ptrs(a + 2, 3, p) || !get_size(a[5], &R) || !get_long(a[6], &stride) || !get_ptr(a[7], &rows) ||
+        !get_size(a[8], &Hq) || !get_float(a[9], &scale) || !get_ptr(a[10], &ws) || !get_int(a[11], &bytes) || !get_stream(a[12], &stream) ||
+        !get_ptr(a[13], &tree) || !get_ptr(a[14], &blocks) || !get_size(a[15], &count) || !get_int(a[16], &type))
+        return through_ctypes(a, n);
+    CALL(status, ((int (*)(const void*, const void*, void*, int, long long, const void*, int, float, const void*, const void*, int, int, void*, size_t,
+                           void*))f)(p[0], p[1], p[2], R, stride, rows, Hq, scale, tree, blocks, count, (int)(unsigned)type, ws, (size_t)bytes, stream));
+    return PyLong_FromLong(status);
+}
+
 static PyMethodDef methods[] = {
     {"plain", (PyCFunction)(void (*)(void))plain, METH_FASTCALL, NULL},
     {"whole", (PyCFunction)(void (*)(void))whole, METH_FASTCALL, NULL},
     {"prepare", (PyCFunction)(void (*)(void))prepare, METH_FASTCALL, NULL},
     {"chunk", (PyCFunction)(void (*)(void))chunk, METH_FASTCALL, NULL},
+    {"cache_write", (PyCFunction)(void (*)(void))cache_write, METH_FASTCALL, NULL},
+    {"cache_read", (PyCFunction)(void (*)(void))cache_read, METH_FASTCALL, NULL},
+    {"cache_choose", (PyCFunction)(void (*)(void))cache_choose, METH_FASTCALL, NULL},
+    {"attn_cache", (PyCFunction)(void (*)(void))attn_cache, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL},
 };
 

@@ -118,12 +118,12 @@ __device__ inline float largest(float x)
 // older tokens are read too: a mean made from all tokens is the same whatever the steps that brought them, and writing a
 // token again corrects it.  Partial sums of the lanes that share channels are added in a fixed order.
 // What bounds it: a step, what hangs on one another (lengths, table, tokens; 5 us); prompts, memory.
-template <int D, bool E4M3>
-__global__ __launch_bounds__(kCacheThreads)
+template <int D, bool E4M3, int NT>
+__global__ __launch_bounds__(NT)
 void pasa_cache_write_k(pasa_cache c, const unsigned short* __restrict__ k, const unsigned short* __restrict__ v, int R, long long row_stride,
                         const int* __restrict__ row_start, int io_bf16, int page_log2, FastDiv heads)
 {
-    constexpr int LT = D / 8, AT = kCacheThreads / LT, BATCH = 4;        // lanes of a token, tokens at a time, of which so many are on their way
+    constexpr int LT = D / 8, AT = NT / LT, BATCH = 2;   // lanes of a token, tokens at a time, of which so many are on their way
     __shared__ __attribute__((aligned(16))) float sums[AT][D];
     const int tid = threadIdx.x, lt = tid % LT, t0 = tid / LT;
     const int most = c.table_width << page_log2;
@@ -136,7 +136,7 @@ void pasa_cache_write_k(pasa_cache c, const unsigned short* __restrict__ k, cons
         shift[1] = *reinterpret_cast<const f4*>(c.kshift + hk * D + 8 * lt + 4);
     }
     auto first_page = [&](const Sequence& s) { return (s.length > s.rows ? s.length - s.rows : 0) >> page_log2; };
-    const Place at = find_place<kCacheThreads>(c.length, row_start, c.S, R, most, [&](const Sequence& s) {
+    const Place at = find_place<NT>(c.length, row_start, c.S, R, most, [&](const Sequence& s) {
         return s.rows == 0 || s.length == 0 ? 0u : (unsigned)(((s.length - 1) >> page_log2) - first_page(s) + 1);
     }, [&](unsigned) { return piece; });
     if (at.b < 0) return;
@@ -479,13 +479,24 @@ hipError_t pasa_launch_cache_write(const pasa_cache& c, const void* k, const voi
     // a sequence of n rows writes to (n - 1) / page + 2 pages at most, and to n at most
     const long pages = (long)R / c.page + 2 * (long)c.S;
     const unsigned grid = (unsigned)((pages < R ? pages : R) * c.Hkv);
-    auto go = [&](auto kernel) {
-        kernel<<<grid, kCacheThreads, 0, stream>>>(c, static_cast<const unsigned short*>(k), static_cast<const unsigned short*>(v), R, row_stride,
-                                                   row_start, io_bf16, log2_of(c.page), fast_div(c.Hkv));
+    // Threads that take a page in four steps of d / 8 lanes a token, 256 at least: two on their way at a time, and several workgroups to a compute unit.  us in
+    // four steps / two / eight: 14000 tokens, 4 heads, d = 128, pages of 128 tokens, e4m3 18.7 / 21.2 / 21.2, of 64, integers 13.0 / 14.7 / 13.0;
+    // 777 tokens in pages of 128 7.4 / 7.2 / 9.8
+    const int lanes = c.page * (c.d / 8);
+    auto go = [&](auto kernel, int threads) {
+        kernel<<<grid, threads, 0, stream>>>(c, static_cast<const unsigned short*>(k), static_cast<const unsigned short*>(v), R, row_stride, row_start,
+                                             io_bf16, log2_of(c.page), fast_div(c.Hkv));
     };
     const bool e = c.format == PASA_CACHE_E4M3;
-    if (c.d == 128) e ? go(pasa_cache_write_k<128, true>) : go(pasa_cache_write_k<128, false>);
-    else e ? go(pasa_cache_write_k<64, true>) : go(pasa_cache_write_k<64, false>);
+    auto of_threads = [&](auto d, auto nt) {
+        constexpr int D = decltype(d)::value, NT = decltype(nt)::value;
+        e ? go(pasa_cache_write_k<D, true, NT>, NT) : go(pasa_cache_write_k<D, false, NT>, NT);
+    };
+    auto of_size = [&](auto d) {
+        if (lanes <= 1024) of_threads(d, std::integral_constant<int, 256>{});
+        else of_threads(d, std::integral_constant<int, 512>{});
+    };
+    c.d == 128 ? of_size(std::integral_constant<int, 128>{}) : of_size(std::integral_constant<int, 64>{});
     return hipGetLastError();
 }
 
