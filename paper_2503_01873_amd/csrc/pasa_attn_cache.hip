@@ -35,7 +35,7 @@ struct RowsArgs {
     float* slots;
     long long row_stride;
     float scale2;                                // scale * log2(e)
-    int R, Hq, count, io_bf16, page_log2;
+    int R, Hq, count, io_bf16, page_log2, never_cut;
     FastDiv G;
 };
 
@@ -63,104 +63,174 @@ __device__ inline Extent extent_of(const RowsArgs& a, const Sequence& s)
 }
 
 // What a workgroup sweeps first: units `us` on of block of rows `pair` (of all heads) of sequence b, and how many from there on; b < 0: nothing.
+// Then, its wavefronts one by one, whole blocks of rows of short sequences: `shorts` of them in all, of which the first ones go to workgroup `used`.
 struct Start {
     int b, us;
     unsigned pair, left, per;
     Sequence s;
+    unsigned shorts, used;
+    int longest_short;
 };
 
-// Two ways to share out.  Few (sequence, head, row block)s, half as many as there are workgroups at most: each is cut into ranges of `per` units,
-// one a workgroup, with `per` the least of eight sizes (one a wavefront tries) that gives no more ranges than workgroups: between an even share of the whole and
-// that share for the workgroups that are left when every row block has one range that is not full, with which it always fits.  Many: the units of all are one line that is cut evenly, and a
-// workgroup's range may end inside one block and begin inside the next.  That costs it what a range costs beside its keys, twice: 6 us (4 heads of 4999 keys 14.7 us,
-// so 10.5).
-template <int ROWS, int NT>
-__device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid, int most)
+// What a workgroup keeps of the sequences for its shorts, where there are as many threads: each one, and how many blocks of rows of short sequences there
+// are up to and with it.
+template <int NT>
+struct Known {
+    Sequence s[NT];
+    unsigned shorts[NT];
+};
+
+// units / size, rounded up; both below 2^13, where the quotient with a half added is off by far less than keeps it from the next whole number
+__device__ inline unsigned ranges_of(unsigned units, unsigned size)
 {
-    constexpr int NW = NT / 64;
-    __shared__ unsigned lds_units[NT], lds_pairs[NT], lds_sum[3][NW], lds_try[NW];
+    return (unsigned)(((float)(units + size - 1) + 0.5f) * __builtin_amdgcn_rcpf((float)size));
+}
+
+// How the work is shared out.  A block of rows (of a sequence and head) costs a workgroup about 5 us beside its keys: lengths, places, queries, the first keys'
+// way from memory, the wavefronts' states brought together.
+// - No more blocks than workgroups: each is cut into ranges of `per` units, one a workgroup, with `per` the least of eight sizes
+//   that gives no more ranges than workgroups; the largest of the eight always does: the longest sequence, or the share of the workgroups that are
+//   left when every block has one range that is not full.
+// - More: the units of all are one line that is cut evenly, and a workgroup's range may end inside one block and begin inside the next, as
+//   often as it has to.  Sequences so short that this would leave wavefronts idle (a wavefront takes 5 + units us for a block, a workgroup that time for
+//   each of its blocks) stay out of the line: wavefronts take their blocks whole.
+// Never cut (where the host knows that no sequence is long): ranges are whole sequences, and there is no line.
+// Up to 64 sequences a wavefront has one a lane and needs no other; up to as many as threads the wavefronts exchange their sums; beyond, the line alone.
+template <int ROWS, int NT>
+__device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid, int most, Known<NT>& known)
+{
+    constexpr int NW = NT / 64, SIZES = 8;
+    __shared__ unsigned lds_sum[4][NW], lds_try[SIZES][NW];
     __shared__ Start found;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     // Place `rest` of a sequence's ranges (or units, where the line is cut)
-    auto start_at = [&](int b, const Sequence& s, unsigned rest, unsigned total, unsigned per, bool ranges) {
+    auto start_at = [&](int b, const Sequence& s, unsigned rest, unsigned line, unsigned per, bool ranges) {
         const Extent x = extent_of<ROWS>(a, s);
-        const unsigned of_pair = ranges ? ((unsigned)x.units + per - 1) / per : (unsigned)x.units;
-        Start st = {b, 0, rest / of_pair, 0, per, s};
+        const unsigned of_pair = ranges ? ranges_of((unsigned)x.units, per) : (unsigned)x.units;
+        Start st = {b, 0, rest / of_pair, 0, per, s, 0, 0, 0};
         st.us = (int)((rest - st.pair * of_pair) * (ranges ? per : 1u));
-        st.left = ranges ? (unsigned)(x.units - st.us) : total - w * per;
+        st.left = ranges ? (unsigned)(x.units - st.us) : line - w * per;
         if (st.left > per) st.left = per;
         return st;
     };
-    if (a.c.S <= NT) {                           // a sequence a thread: what is read of it once is enough
-        unsigned units = 1, pairs = 0;
-        Sequence s = {0, 0, 0};
-        if (tid < a.c.S) {
-            s = sequence_at(a.c.length, a.row_start, tid, a.R, most);
-            const Extent x = extent_of<ROWS>(a, s);
-            units = (unsigned)x.units;
-            pairs = (unsigned)x.row_blocks * (unsigned)a.c.Hkv;
-        }
-        lds_units[tid] = units;
-        lds_pairs[tid] = pairs;
-        const unsigned upto_u = scan64(units * pairs), upto_p = scan64(pairs);
-        if (lane == 63) lds_sum[0][wave] = upto_u, lds_sum[1][wave] = upto_p;
-        if (tid == 0) found.b = -1;
-        __syncthreads();
-        unsigned total = 0, all = 0, before = upto_u - units * pairs, mine = units * pairs;
-#pragma unroll
-        for (int i = 0; i < NW; ++i) {
-            if (i < wave) before += lds_sum[0][i];
-            total += lds_sum[0][i];
-            all += lds_sum[1][i];
-        }
-        const bool ranges = 2 * all <= grid;
-        unsigned per = whole_units((total + grid - 1) / grid), want = w * per;
-        if (ranges) {
-            const unsigned least = per, sure = whole_units((total + grid - all - 1) / (grid - all));
-            auto size = [&](unsigned i) { return whole_units(least + (sure - least) * i / (NW - 1)); };
-            const unsigned size_of_wave = size((unsigned)wave);
-            unsigned sum = 0;
-            for (int i = lane; i < a.c.S; i += 64) sum += size_of_wave > 0 ? lds_pairs[i] * ((lds_units[i] + size_of_wave - 1) / size_of_wave) : 0;
-            sum = scan64(sum);
-            if (lane == 63) lds_try[wave] = sum;
-            __syncthreads();
-            per = sure;
-#pragma unroll
-            for (int i = NW - 2; i >= 0; --i)
-                if (lds_try[i] <= grid) per = size((unsigned)i);
-            mine = per > 0 ? pairs * ((units + per - 1) / per) : 0;
-            before = scan64(mine);
-            if (lane == 63) lds_sum[2][wave] = before;
-            __syncthreads();
-            before -= mine;
-#pragma unroll
-            for (int i = 0; i < NW; ++i)
-                if (i < wave) before += lds_sum[2][i];
-            want = w;
-        }
-        if (want >= before && want < before + mine) found = start_at(tid, s, want - before, total, per, ranges);
-        __syncthreads();
-    } else {
+    if (a.c.S > NT) {
         unsigned per = 0;
         const Place at = find_place<NT>(a.c.length, a.row_start, a.c.S, a.R, most, [&](const Sequence& s) {
             const Extent x = extent_of<ROWS>(a, s);
             return (unsigned)x.row_blocks * (unsigned)a.c.Hkv * (unsigned)x.units;
         }, [&](unsigned total) { return w * (per = whole_units((total + grid - 1) / grid)); });
-        if (tid == 0) {
-            if (at.b < 0) found.b = -1;
-            else found = start_at(at.b, at.s, at.rest, at.total, per, false);
+        if (at.b >= 0) return start_at(at.b, at.s, at.rest, at.total, (unsigned)__builtin_amdgcn_readfirstlane((int)per), false);
+        return Start{-1, 0, 0, 0, 0, {0, 0, 0}, 0, 0, 0};
+    }
+    const bool one_wave = a.c.S <= 64;
+    const int b = one_wave ? lane : tid;
+    unsigned units = 1, pairs = 0;
+    Sequence s = {0, 0, 0};
+    if (b < a.c.S) {
+        s = sequence_at(a.c.length, a.row_start, b, a.R, most);
+        const Extent x = extent_of<ROWS>(a, s);
+        units = (unsigned)x.units;
+        pairs = (unsigned)x.row_blocks * (unsigned)a.c.Hkv;
+    }
+    // Sums over the sequences up to and with one's own, and over all
+    auto sums = [&](int n, const unsigned (&x)[2], unsigned (&upto)[2], unsigned (&all)[2]) {
+        unsigned sum[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            upto[i] = scan64(x[i]);
+            sum[i] = (unsigned)__builtin_amdgcn_readlane((int)upto[i], 63);
+            all[i] = sum[i];
+        }
+        if (one_wave) return;
+        if (lane == 0) lds_sum[2 * n][wave] = sum[0], lds_sum[2 * n + 1][wave] = sum[1];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            all[i] = 0;
+            for (int j = 0; j < NW; ++j) {
+                if (j < wave) upto[i] += lds_sum[2 * n + i][j];
+                all[i] += lds_sum[2 * n + i][j];
+            }
+        }
+    };
+    unsigned upto[2], all[2];
+    sums(0, {units * pairs, pairs}, upto, all);
+    const unsigned total = all[0], blocks = all[1];
+    const bool ranges = blocks <= grid;
+    const unsigned longest_short = ranges ? 0u : a.never_cut ? 0x7fffffffu : min(32u, 5u * ((blocks - 1) / grid));
+    unsigned per = 0;
+    if (ranges) {
+        unsigned longest = largest64(pairs > 0 ? units : 0);
+        if (!one_wave) {
+            __syncthreads();
+            if (lane == 0) lds_sum[0][wave] = longest;
+            __syncthreads();
+            for (int j = 0; j < NW; ++j) longest = max(longest, lds_sum[0][j]);
+        }
+        per = whole_units(longest);
+        if (!a.never_cut && longest > 0) {
+            unsigned sure = per;
+            if (blocks < grid) sure = min(sure, whole_units((total + grid - blocks - 1) / (grid - blocks)));
+            const unsigned least = min(whole_units((total + grid - 1) / grid), sure);
+            auto size = [&](unsigned i) { return whole_units(least + (sure - least) * i / (SIZES - 1)); };
+            if (one_wave) {                      // the least by halving: more ranges, smaller ones
+                unsigned low = 0, high = SIZES - 1;
+                for (int i = 0; i < 3; ++i) {
+                    const unsigned middle = (low + high) / 2;
+                    const unsigned sum = (unsigned)__builtin_amdgcn_readlane((int)scan64(pairs * ranges_of(units, size(middle))), 63);
+                    if (sum <= grid) high = middle;
+                    else low = middle + 1;
+                }
+                per = size(high);
+            } else {
+                for (unsigned i = 0; i < SIZES; ++i) {
+                    const unsigned sum = scan64(pairs * ranges_of(units, size(i)));
+                    if (lane == 63) lds_try[i][wave] = sum;
+                }
+                __syncthreads();
+                per = sure;
+                for (int i = SIZES - 2; i >= 0; --i) {
+                    unsigned sum = 0;
+                    for (int j = 0; j < NW; ++j) sum += lds_try[i][j];
+                    if (sum <= grid) per = size((unsigned)i);
+                }
+            }
+        }
+    }
+    per = (unsigned)__builtin_amdgcn_readfirstlane((int)per);
+    const bool is_short = units <= longest_short;
+    const unsigned mine = is_short || pairs == 0 ? 0u : ranges ? pairs * ranges_of(units, per) : units * pairs;
+    if (!one_wave) __syncthreads();              // the sums are read
+    sums(1, {mine, is_short ? pairs : 0u}, upto, all);
+    const unsigned line = all[0];
+    if (!ranges) per = whole_units((line + grid - 1) / grid);
+    if (all[1] > 0) {
+        if (one_wave ? wave == 0 : true) {
+            known.s[b] = s;
+            known.shorts[b] = upto[1];
         }
         __syncthreads();
     }
-    Start st;
-    st.b = __builtin_amdgcn_readfirstlane(found.b);
-    st.us = __builtin_amdgcn_readfirstlane(found.us);
-    st.pair = (unsigned)__builtin_amdgcn_readfirstlane((int)found.pair);
-    st.left = (unsigned)__builtin_amdgcn_readfirstlane((int)found.left);
-    st.per = (unsigned)__builtin_amdgcn_readfirstlane((int)found.per);
-    st.s.length = __builtin_amdgcn_readfirstlane(found.s.length);
-    st.s.row0 = __builtin_amdgcn_readfirstlane(found.s.row0);
-    st.s.rows = __builtin_amdgcn_readfirstlane(found.s.rows);
+    const unsigned want = ranges ? w : w * per, before = upto[0] - mine;
+    const bool here = want >= before && want < upto[0];
+    Start st = {-1, 0, 0, 0, per, {0, 0, 0}, 0, 0, 0};
+    if (one_wave) {
+        const unsigned long long who = __builtin_amdgcn_ballot_w64(here);
+        if (who != 0ull) {
+            const int l = __builtin_ctzll(who);
+            const Sequence of = {__builtin_amdgcn_readlane(s.length, l), __builtin_amdgcn_readlane(s.row0, l), __builtin_amdgcn_readlane(s.rows, l)};
+            st = start_at(l, of, want - (unsigned)__builtin_amdgcn_readlane((int)before, l), line, per, ranges);
+        }
+    } else {
+        if (tid == 0) found = st;
+        __syncthreads();
+        if (here) found = start_at(b, s, want - before, line, per, ranges);
+        __syncthreads();
+        st = found;
+    }
+    st.shorts = all[1];
+    st.used = ranges ? line : 0;
+    st.longest_short = (int)longest_short;
     return st;
 }
 
@@ -205,36 +275,64 @@ void pasa_cache_rows(RowsArgs a)
     constexpr int ROWS = 16 * RB, KS = D / 32, CB = D / 16, NW = kUnitsAtOnce, NT = 64 * NW;
     constexpr int LD = D + 4;                    // LDS row of the merge, in floats
     constexpr int VW = CB / 4;                   // words of a key's value that a lane takes
-    __shared__ __attribute__((aligned(16))) float lds_o[NW * ROWS * LD];
-    __shared__ __attribute__((aligned(16))) float lds_key[NW][3 * kUnit];       // per key: score factor, log2 of the value's scale, 1 / it
-    __shared__ float lds_l[NW][ROWS], lds_m[NW][ROWS];
     constexpr bool QLDS = RB > 1;                // the query fragments wait in LDS: the registers are needed for RB blocks
-    __shared__ __attribute__((aligned(16))) h8 lds_q[QLDS ? RB * KS * 64 : 1];
+    // A wavefront's own part: while it sweeps, per key of the unit the score's factor, log2 of the value's scale and 1 / it, and the query fragments;
+    // afterwards its stored output.
+    __shared__ __attribute__((aligned(16))) float lds_o[NW * ROWS * LD];
+    static_assert(3 * kUnit * 4 + (QLDS ? RB * KS * 1024 : 0) <= ROWS * LD * 4, "what a wavefront keeps while it sweeps fits its part");
+    __shared__ float lds_l[NW][ROWS], lds_m[NW][ROWS];
+    __shared__ Known<NT> known;
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lq = lane & 15, g = lane >> 4;
     const int G = (int)a.G.d, most = a.c.table_width << a.page_log2, lg = a.page_log2;
-    const unsigned w = logical_workgroup(blockIdx.x, gridDim.x);
+    const unsigned grid = gridDim.x, w = logical_workgroup(blockIdx.x, grid);
+    float* const key_f = lds_o + wave * ROWS * LD;
+    h8* const lds_q = reinterpret_cast<h8*>(key_f + 3 * kUnit);
 
-    const Start at = find_start<ROWS, NT>(a, w, gridDim.x, most);
-    if (at.b < 0) {
-        if (tid == 0) a.records[w].pieces = 0;
-        return;
-    }
+    Start at = find_start<ROWS, NT>(a, w, grid, most, known);
+    // the same in all lanes, which the compiler does not see on all ways to here: the buffers' descriptions would be taken lane by lane
+    auto uniform = [](auto& v) { v = (std::remove_reference_t<decltype(v)>)__builtin_amdgcn_readfirstlane((int)v); };
+    uniform(at.b), uniform(at.per), uniform(at.shorts), uniform(at.used), uniform(at.longest_short);
     unsigned left = at.left, pair = at.pair;     // units of this workgroup still to be swept
     int b = at.b, us = at.us;
     Sequence s = at.s;
     Extent x = extent_of<ROWS>(a, s);
     bool first_piece = true;
-    float* const key_f = lds_key[wave];
+    // Shorts: neighbours go to different workgroups, the first ones to those without a range
+    unsigned next_short = (w >= at.used ? w - at.used : w + grid - at.used) + grid * (unsigned)wave;
+    auto take_short = [&] {
+        if (next_short >= at.shorts) return false;
+        int n = 0;                               // sequences whose shorts all come before
+        for (int i = 0; i < a.c.S; i += 64) n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i + lane < a.c.S && known.shorts[i + lane] <= next_short));
+        b = __builtin_amdgcn_readfirstlane(n < a.c.S ? n : a.c.S - 1);
+        s.length = __builtin_amdgcn_readfirstlane(known.s[b].length);
+        s.row0 = __builtin_amdgcn_readfirstlane(known.s[b].row0);
+        s.rows = __builtin_amdgcn_readfirstlane(known.s[b].rows);
+        x = extent_of<ROWS>(a, s);
+        pair = next_short - (unsigned)__builtin_amdgcn_readfirstlane(b > 0 ? (int)known.shorts[b - 1] : 0);
+        us = 0;
+        left = (unsigned)x.units;
+        next_short += grid * NW;
+        return true;
+    };
+    bool alone = b < 0;                          // this wavefront sweeps a short by itself
+    if (alone) {
+        if (tid == 0) a.records[w].pieces = 0;
+        if (!take_short()) return;
+    }
 
     for (;;) {
+        uniform(b), uniform(us), uniform(left), uniform(pair);
+        uniform(s.length), uniform(s.row0), uniform(s.rows);
+        uniform(x.keys), uniform(x.units), uniform(x.row_blocks);
         const int ue = (int)((unsigned)(x.units - us) < left ? x.units : us + (int)left);
         const int hk = (int)(pair / (unsigned)x.row_blocks), p0 = (int)(pair - (unsigned)hk * (unsigned)x.row_blocks) * ROWS;
         const int list = s.rows * G;             // rows of the KV head's query heads, by token, then head
         const int new0 = s.length - s.rows;      // position of the sequence's first row
-        const int units = us + wave < ue ? (ue - us - wave + NW - 1) / NW : 0;      // of this wavefront
+        const int begin = __builtin_amdgcn_readfirstlane(alone ? us : us + wave), step = __builtin_amdgcn_readfirstlane(alone ? 1 : NW);
+        const int units = begin < ue ? (ue - begin + step - 1) / step : 0;       // of this wavefront
 
         f4 O[RB][CB];
         float M[RB], l[RB];
@@ -251,13 +349,6 @@ void pasa_cache_rows(RowsArgs a)
             return *reinterpret_cast<const u16x8*>(a.q + (size_t)(s.row0 + t) * (size_t)a.row_stride + (size_t)(hk * G + h) * D + 16 * g +
                                                    64 * (ks / 2) + 8 * (ks & 1));
         };
-        if (QLDS) {
-            for (int f = wave; f < RB * KS; f += NW) {
-                const u16x8 raw = query(row_of(f / KS), f % KS);
-                lds_q[f * 64 + lane] = a.io_bf16 ? bf16x8_to_h8(raw) : __builtin_bit_cast(h8, raw);
-            }
-            __syncthreads();
-        }
         if (units > 0) {
             // Places of the blocks of 16 keys, lane group g that of block g, by way of the list where there is one.  Three steps, each an
             // iteration ahead of the next: the list's entry, the table's, the keys.  Entries are read at index 0 where there is no block, and not
@@ -266,7 +357,7 @@ void pasa_cache_rows(RowsArgs a)
             const int* const chosen = LISTED ? a.blocks + ((size_t)b * a.c.Hkv + hk) * a.count : nullptr;
             int listed_a, place_b, entry_b;      // of the unit after the next two; of the one after the next
             int pos_next = 0, page_next = -1, pos_now = 0, page_now = -1;
-            auto first_key = [&](int n) { return (us + wave + NW * n) * kUnit + 16 * g; };
+            auto first_key = [&](int n) { return (begin + step * n) * kUnit + 16 * g; };
             auto read_list = [&](int n) {
                 const int vk = first_key(n);
                 listed_a = LISTED ? chosen[n < units && vk < x.keys ? vk >> lg : 0] : 0;
@@ -292,7 +383,10 @@ void pasa_cache_rows(RowsArgs a)
             auto buffer_of = [&](void* base, int blk, int pages, int poss) {
                 const int page = __builtin_amdgcn_readlane(pages, 16 * blk), pos = __builtin_amdgcn_readlane(poss, 16 * blk);
                 const size_t slot = ((size_t)(unsigned)(page < 0 ? 0 : page) * (unsigned)a.c.Hkv + (unsigned)hk) * (unsigned)a.c.page + (unsigned)(pos & (a.c.page - 1));
-                return __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(base) + slot * D, 0, page < 0 ? 0 : 16 * D, 0x00020000);
+                const uintptr_t at = reinterpret_cast<uintptr_t>(base) + slot * D;
+                const unsigned lo = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)at), hi = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(at >> 32));
+                return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>((uintptr_t)hi << 32 | lo), 0,
+                                                         __builtin_amdgcn_readfirstlane(page < 0 ? 0 : 16 * D), 0x00020000);
             };
             auto load_k = [&] {
 #pragma unroll
@@ -325,7 +419,7 @@ void pasa_cache_rows(RowsArgs a)
             };
 
             // query rows, and what each sees; rows behind the last one are the last one again, and not stored
-            u16x8 raw[QLDS ? 1 : RB][KS];
+            u16x8 raw[RB][KS];
             int last[RB];
             unsigned long long bits[RB];
             read_list(0);
@@ -334,9 +428,8 @@ void pasa_cache_rows(RowsArgs a)
                 const int p = row_of(rb), t = (int)a.G.quotient((unsigned)p);
                 last[rb] = a.tree != nullptr ? new0 - 1 : new0 + t;
                 bits[rb] = a.tree != nullptr ? a.tree[s.row0 + t] : 0ull;
-                if (!QLDS)
 #pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) raw[rb][ks] = query(p, ks);
+                for (int ks = 0; ks < KS; ++ks) raw[rb][ks] = query(p, ks);
             }
             read_entry(0);
             read_list(1);
@@ -347,20 +440,24 @@ void pasa_cache_rows(RowsArgs a)
             page_now = page_next, pos_now = pos_next;
             load_v();
             PASA_FENCE();
-            h8 Qr[QLDS ? 1 : RB][KS];
-            if (!QLDS) {
+            h8 Qr[RB][KS];
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) Qr[rb][ks] = __builtin_bit_cast(h8, raw[rb][ks]);
+            if (a.io_bf16) {
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) Qr[QLDS ? 0 : rb][ks] = __builtin_bit_cast(h8, raw[QLDS ? 0 : rb][ks]);
-                if (a.io_bf16) {
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-                        for (int ks = 0; ks < KS; ++ks) Qr[QLDS ? 0 : rb][ks] = bf16x8_to_h8(raw[QLDS ? 0 : rb][ks]);
-                }
+                    for (int ks = 0; ks < KS; ++ks) Qr[rb][ks] = bf16x8_to_h8(raw[rb][ks]);
             }
-            auto Q = [&](int rb, int ks) { return QLDS ? lds_q[(rb * KS + ks) * 64 + lane] : Qr[QLDS ? 0 : rb][ks]; };
+            if (QLDS) {
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) lds_q[(rb * KS + ks) * 64 + lane] = Qr[rb][ks];
+            }
+            auto Q = [&](int rb, int ks) { return QLDS ? lds_q[(rb * KS + ks) * 64 + lane] : Qr[rb][ks]; };
 
             int n = 0;
             do {
@@ -510,20 +607,37 @@ void pasa_cache_rows(RowsArgs a)
         }
 
         // ---- the wavefronts' states brought to the highest of their levels and added ----
+        int ln = lane;
+        asm volatile("" : "+v"(ln));             // no address is to be worked out before the main loop and kept through it
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             const float sum = sum_row(l[rb]);
-            if (g == 0) {
-                lds_m[wave][16 * rb + lq] = M[rb];
-                lds_l[wave][16 * rb + lq] = sum;
+            if (ln < 16) {
+                lds_m[wave][16 * rb + ln] = M[rb];
+                lds_l[wave][16 * rb + ln] = sum;
             }
             // element i of block cb is channel CB * (4 g + i) + cb
-            float* dst = lds_o + (wave * ROWS + 16 * rb + lq) * LD + CB * 4 * g;
+            float* dst = lds_o + (wave * ROWS + 16 * rb + (ln & 15)) * LD + CB * 4 * (ln >> 4);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int cb = 0; cb < CB; cb += 4)
                     *reinterpret_cast<f4*>(dst + CB * i + cb) = f4{O[rb][cb][i], O[rb][cb + 1][i], O[rb][cb + 2][i], O[rb][cb + 3][i]};
+        }
+        if (alone) {
+            __builtin_amdgcn_wave_barrier();     // a wavefront's LDS accesses are done in order
+            asm volatile("" ::: "memory");
+            constexpr int STEP = 64 / (D / 8);   // rows at a time, eight channels a lane
+#pragma unroll
+            for (int r0 = 0; r0 < ROWS; r0 += STEP) {
+                const int r = r0 + ln / (D / 8), c8 = ln % (D / 8) * 8, p = p0 + r;
+                const float* src = lds_o + (wave * ROWS + r) * LD + c8;
+                const f4 acc[2] = {*reinterpret_cast<const f4*>(src), *reinterpret_cast<const f4*>(src + 4)};
+                if (p < list) store_row(a, s.row0, hk, p, D, c8, acc, lds_l[wave][r]);
+            }
+            asm volatile("" ::: "memory");
+            if (!take_short()) return;
+            continue;
         }
         __syncthreads();
         const bool complete = us == 0 && ue == x.units;
@@ -532,7 +646,7 @@ void pasa_cache_rows(RowsArgs a)
         constexpr int STEP = NT / (D / 8);       // rows at a time, eight channels a lane
 #pragma unroll
         for (int r0 = 0; r0 < ROWS; r0 += STEP) {
-            const int r = r0 + tid / (D / 8), c8 = tid % (D / 8) * 8, p = p0 + r;
+            const int th = 64 * wave + ln, r = r0 + th / (D / 8), c8 = th % (D / 8) * 8, p = p0 + r;
             if (r >= ROWS || p >= list) break;
             float level = lds_m[0][r], sum = 0.f;
 #pragma unroll
@@ -558,28 +672,31 @@ void pasa_cache_rows(RowsArgs a)
             }
         }
         left -= (unsigned)(ue - us);
-        if (left == 0) {
-            // begun here, and goes on in the ranges behind
-            if (tid == 0) {
-                MergeRecord m = {0, (int)my_slot, p0, list, s.row0, hk, {0, 0}};
-                if (us == 0 && ue < x.units) m.pieces = clamp_int(1 + (int)(((unsigned)(x.units - ue) + at.per - 1) / at.per), 0, (int)(gridDim.x - w));
-                a.records[w] = m;
-            }
-            return;
-        }
-        __syncthreads();                         // the LDS is free again
         first_piece = false;
+        bool more = left > 0;
+        if (!more && tid == 0) {                 // begun here, and goes on in the ranges behind?
+            MergeRecord m = {0, (int)my_slot, p0, list, s.row0, hk, {0, 0}};
+            if (us == 0 && ue < x.units) m.pieces = clamp_int(1 + (int)(((unsigned)(x.units - ue) + at.per - 1) / at.per), 0, (int)(grid - w));
+            a.records[w] = m;
+        }
         us = 0;
-        if (++pair == (unsigned)x.row_blocks * (unsigned)a.c.Hkv) {
+        if (more && ++pair == (unsigned)x.row_blocks * (unsigned)a.c.Hkv) {
             pair = 0;
-            do {
+            do {                                 // the next sequence in the line
                 if (++b >= a.c.S) {
                     if (tid == 0) a.records[w].pieces = 0;
-                    return;
+                    more = false;
+                    break;
                 }
                 s = sequence_at(a.c.length, a.row_start, b, a.R, most);
-            } while (s.rows == 0);
-            x = extent_of<ROWS>(a, s);
+                x = extent_of<ROWS>(a, s);
+            } while (s.rows == 0 || x.units <= (int)at.longest_short);
+        }
+        if (!more && at.shorts == 0) return;
+        __syncthreads();                         // the LDS is free again
+        if (!more) {
+            alone = true;
+            if (!take_short()) return;
         }
     }
 }
@@ -686,12 +803,13 @@ hipError_t pasa_launch_attn_cache(const pasa_cache& c, const void* q, void* o, i
     a.Hq = Hq;
     a.count = count;
     a.io_bf16 = io_bf16;
+    a.never_cut = plan.never_cut;
     a.page_log2 = log2_of(c.page);
     a.G = fast_div((unsigned)(Hq / c.Hkv));
     auto go = [&](auto rows, auto merge) {
         rows<<<plan.grid, 64 * kUnitsAtOnce, 0, stream>>>(a);
         const hipError_t e = hipGetLastError();
-        if (e != hipSuccess || plan.grid == 1) return e;
+        if (e != hipSuccess || plan.grid == 1 || plan.never_cut) return e;
         const long long most = (long long)R * (Hq / c.Hkv);          // rows of a block
         const unsigned each = (unsigned)(most < 16 * plan.row_blocks ? most : 16 * plan.row_blocks);
         merge<<<(unsigned)plan.grid * each, kCacheThreads, 0, stream>>>(a, fast_div(each));

@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 #include "pasa.h"
 #include "pasa_device.h"
@@ -16,9 +17,10 @@ inline int log2_of(int page)
     return n;
 }
 
-// The kernels of attention over the cache: rows per workgroup are 16 * row_blocks, `grid` workgroups share the units of work.
+// The kernels of attention over the cache: rows per workgroup are 16 * row_blocks, `grid` workgroups share the units of work; no block of rows
+// is shared by two of them (and nothing merged) where never_cut.
 struct CachePlan {
-    int row_blocks, grid;
+    int row_blocks, grid, never_cut;
 };
 constexpr int kUnit = 64;              // keys of a unit of work (of one wavefront)
 constexpr int kUnitsAtOnce = 8;        // wavefronts of a workgroup: units that it sweeps at a time
@@ -69,6 +71,22 @@ __device__ inline unsigned scan64(unsigned x)
     x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);       // lane 15 to the second 16 lanes, 47 to the fourth
     x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);       // lane 31 to the upper half
     return x;
+}
+
+// Largest over the lanes of a wavefront, in all
+__device__ inline unsigned largest64(unsigned x)
+{
+    auto with = [&](auto control, auto rows) {
+        const unsigned y = (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, decltype(control)::value, decltype(rows)::value, 0xf, false);
+        x = y > x ? y : x;
+    };
+    with(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});
+    with(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+    with(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+    with(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+    with(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});
+    with(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+    return (unsigned)__builtin_amdgcn_readlane((int)x, 63);
 }
 
 // A workgroup's place in work that is shared out over the sequences: sequence b has count(sequence) pieces, and piece `at(total)` of all

@@ -10,6 +10,7 @@ namespace {
 
 constexpr long long kMaxTokens = 262144;         // of a sequence, as in the other entry points
 constexpr long long kMaxGrid = 0x7fffffff;       // workgroups of a launch
+constexpr int kComputeUnits = 256;               // MI355X
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 bool buffer(const void* p, uintptr_t a) { return p != nullptr && aligned(p, a); }
@@ -41,16 +42,18 @@ int check_rows(const pasa_cache* c, const void* p, int R, long long row_stride, 
 int check_workspace(const void* ws, size_t bytes, size_t need) { return buffer(ws, 256) && bytes >= need ? PASA_OK : PASA_EWORKSPACE; }
 
 // Rows per workgroup: 16 where the rows of a KV head fill no more on average, 32 otherwise.  Workgroups: one to a compute unit (their eight wavefronts take
-// its registers), and no more than leave each wavefront a unit.  False where the units do not fit 31 bits.
-bool plan_of(const pasa_cache& c, int R, int Hq, CachePlan* plan)
+// its registers), and no more than there are blocks of rows or leave each wavefront a unit.  Never cut: up to 1024 keys, where a merge costs what it saves,
+// and as many sequences as the kernel has threads.  False where the units do not fit 31 bits.
+bool plan_of(const pasa_cache& c, int R, int Hq, int count, CachePlan* plan)
 {
     const long long G = Hq / c.Hkv;
     plan->row_blocks = (long long)R * G <= 16LL * c.S ? 1 : 2;
-    const long long units = ((long long)c.table_width * c.page + kUnit - 1) / kUnit;
+    const long long pages = count > 0 && count < c.table_width ? count : c.table_width, units = (pages * c.page + kUnit - 1) / kUnit;
     const long long blocks = (long long)R * G / (16 * plan->row_blocks) + c.S;      // of rows, at most
     if (R * G > kMaxGrid || blocks > kMaxGrid / c.Hkv || blocks * c.Hkv > kMaxGrid / units) return false;
-    const long long all = (blocks * c.Hkv * units + kUnitsAtOnce - 1) / kUnitsAtOnce, resident = 256;
-    plan->grid = (int)(all < resident ? all : resident);
+    const long long pairs = blocks * c.Hkv, filled = (pairs * units + kUnitsAtOnce - 1) / kUnitsAtOnce, all = pairs > filled ? pairs : filled;
+    plan->grid = (int)(all < kComputeUnits ? all : kComputeUnits);
+    plan->never_cut = units <= 16 && c.S <= 64 * kUnitsAtOnce;
     return true;
 }
 
@@ -110,7 +113,7 @@ int pasa_cache_choose(const pasa_cache* cache, const void* q, int R, long long r
 size_t pasa_attn_cache_workspace(const pasa_cache* cache, int R, int Hq)
 {
     CachePlan plan;
-    if (check_cache(cache) != PASA_OK || R <= 0 || Hq <= 0 || Hq % cache->Hkv != 0 || !plan_of(*cache, R, Hq, &plan)) return 0;
+    if (check_cache(cache) != PASA_OK || R <= 0 || Hq <= 0 || Hq % cache->Hkv != 0 || !plan_of(*cache, R, Hq, 0, &plan)) return 0;
     return attn_workspace_bytes(*cache, plan);
 }
 
@@ -126,8 +129,9 @@ int pasa_attn_cache(const pasa_cache* cache, const void* q, void* o, int R, long
     if (!aligned(tree, 8) || !aligned(blocks, 4) || (blocks != nullptr && count < 1)) return PASA_EINVAL;
     if (blocks != nullptr && count > kMaxTokens) return PASA_EUNSUPPORTED;
     CachePlan plan;
-    if (!plan_of(*cache, R, Hq, &plan)) return PASA_EUNSUPPORTED;
+    if (!plan_of(*cache, R, Hq, 0, &plan)) return PASA_EUNSUPPORTED;
     st = check_workspace(workspace, workspace_bytes, attn_workspace_bytes(*cache, plan));
+    if (blocks != nullptr) plan_of(*cache, R, Hq, count, &plan);     // a smaller one
     if (st != PASA_OK) return st;
     return status(pasa_launch_attn_cache(*cache, q, o, R, row_stride, row_start, Hq, scale, tree, blocks, count, io_dtype == PASA_IO_BF16, plan,
                                          workspace, static_cast<hipStream_t>(stream)));
