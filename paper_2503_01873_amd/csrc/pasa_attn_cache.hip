@@ -63,13 +63,13 @@ __device__ inline Extent extent_of(const RowsArgs& a, const Sequence& s)
 }
 
 // What a workgroup sweeps first: units `us` on of block of rows `pair` (of all heads) of sequence b, and how many from there on; b < 0: nothing.
-// Then, its wavefronts one by one, whole blocks of rows of short sequences: `shorts` of them in all, of which the first ones go to workgroup `used`.
+// Then, in groups of `group` wavefronts, whole blocks of rows of short sequences: `shorts` of them in all, of which the first ones go to workgroup `used`.
 struct Start {
     int b, us;
     unsigned pair, left, per;
     Sequence s;
     unsigned shorts, used;
-    int longest_short;
+    int longest_short, group;
 };
 
 // What a workgroup keeps of the sequences for its shorts, where there are as many threads: each one, and how many blocks of rows of short sequences there
@@ -92,8 +92,8 @@ __device__ inline unsigned ranges_of(unsigned units, unsigned size)
 //   that gives no more ranges than workgroups; the largest of the eight always does: the longest sequence, or the share of the workgroups that are
 //   left when every block has one range that is not full.
 // - More: the units of all are one line that is cut evenly, and a workgroup's range may end inside one block and begin inside the next, as
-//   often as it has to.  Sequences so short that this would leave wavefronts idle (a wavefront takes 5 + units us for a block, a workgroup that time for
-//   each of its blocks) stay out of the line: wavefronts take their blocks whole.
+//   often as it has to.  Short sequences, which would leave wavefronts idle, stay out of the line: groups of 1, 2, 4 or 8 wavefronts, as many as there are for
+//   each, take their blocks whole, in 5 us and 1 us a unit and wavefront, while a workgroup would take its blocks one after the other.
 // Never cut (where the host knows that no sequence is long): ranges are whole sequences, and there is no line.
 // Up to 64 sequences a wavefront has one a lane and needs no other; up to as many as threads the wavefronts exchange their sums; beyond, the line alone.
 template <int ROWS, int NT>
@@ -107,7 +107,7 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
     auto start_at = [&](int b, const Sequence& s, unsigned rest, unsigned line, unsigned per, bool ranges) {
         const Extent x = extent_of<ROWS>(a, s);
         const unsigned of_pair = ranges ? ranges_of((unsigned)x.units, per) : (unsigned)x.units;
-        Start st = {b, 0, rest / of_pair, 0, per, s, 0, 0, 0};
+        Start st = {b, 0, rest / of_pair, 0, per, s, 0, 0, 0, 1};
         st.us = (int)((rest - st.pair * of_pair) * (ranges ? per : 1u));
         st.left = ranges ? (unsigned)(x.units - st.us) : line - w * per;
         if (st.left > per) st.left = per;
@@ -120,7 +120,7 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
             return (unsigned)x.row_blocks * (unsigned)a.c.Hkv * (unsigned)x.units;
         }, [&](unsigned total) { return w * (per = whole_units((total + grid - 1) / grid)); });
         if (at.b >= 0) return start_at(at.b, at.s, at.rest, at.total, (unsigned)__builtin_amdgcn_readfirstlane((int)per), false);
-        return Start{-1, 0, 0, 0, 0, {0, 0, 0}, 0, 0, 0};
+        return Start{-1, 0, 0, 0, 0, {0, 0, 0}, 0, 0, 0, 1};
     }
     const bool one_wave = a.c.S <= 64;
     const int b = one_wave ? lane : tid;
@@ -157,7 +157,9 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
     sums(0, {units * pairs, pairs}, upto, all);
     const unsigned total = all[0], blocks = all[1];
     const bool ranges = blocks <= grid;
-    const unsigned longest_short = ranges ? 0u : a.never_cut ? 0x7fffffffu : min(32u, 5u * ((blocks - 1) / grid));
+    unsigned group = NW;
+    while (group > 1 && blocks * group > NW * grid) group /= 2;
+    const unsigned longest_short = ranges ? 0u : a.never_cut ? 0x7fffffffu : min(32u, group * 5u * ((blocks - 1) / grid));
     unsigned per = 0;
     if (ranges) {
         unsigned longest = largest64(pairs > 0 ? units : 0);
@@ -213,7 +215,7 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
     }
     const unsigned want = ranges ? w : w * per, before = upto[0] - mine;
     const bool here = want >= before && want < upto[0];
-    Start st = {-1, 0, 0, 0, per, {0, 0, 0}, 0, 0, 0};
+    Start st = {-1, 0, 0, 0, per, {0, 0, 0}, 0, 0, 0, 1};
     if (one_wave) {
         const unsigned long long who = __builtin_amdgcn_ballot_w64(here);
         if (who != 0ull) {
@@ -231,6 +233,8 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
     st.shorts = all[1];
     st.used = ranges ? line : 0;
     st.longest_short = (int)longest_short;
+    st.group = (int)group;
+    while (st.group < NW && (int)st.shorts * 2 * st.group <= (int)(NW * grid)) st.group *= 2;        // fewer shorts than blocks
     return st;
 }
 
@@ -294,31 +298,37 @@ void pasa_cache_rows(RowsArgs a)
     Start at = find_start<ROWS, NT>(a, w, grid, most, known);
     // the same in all lanes, which the compiler does not see on all ways to here: the buffers' descriptions would be taken lane by lane
     auto uniform = [](auto& v) { v = (std::remove_reference_t<decltype(v)>)__builtin_amdgcn_readfirstlane((int)v); };
-    uniform(at.b), uniform(at.per), uniform(at.shorts), uniform(at.used), uniform(at.longest_short);
+    uniform(at.b), uniform(at.per), uniform(at.shorts), uniform(at.used), uniform(at.longest_short), uniform(at.group);
     unsigned left = at.left, pair = at.pair;     // units of this workgroup still to be swept
     int b = at.b, us = at.us;
     Sequence s = at.s;
     Extent x = extent_of<ROWS>(a, s);
     bool first_piece = true;
-    // Shorts: neighbours go to different workgroups, the first ones to those without a range
-    unsigned next_short = (w >= at.used ? w - at.used : w + grid - at.used) + grid * (unsigned)wave;
+    // Shorts: neighbours go to different workgroups, the first ones to those without a range.  False where the workgroup has no more; a group
+    // for which there is none while the first one still has one goes along with no rows and no keys.
+    int group = NW, lead = wave;                 // wavefronts that share a range or a short, and one's place among them
+    unsigned next_short = w >= at.used ? w - at.used : w + grid - at.used;
     auto take_short = [&] {
-        if (next_short >= at.shorts) return false;
+        const unsigned groups = NW / (unsigned)at.group, first = next_short, mine = first + grid * ((unsigned)wave / (unsigned)at.group);
+        group = at.group;
+        lead = wave & (group - 1);
+        next_short += grid * groups;
+        if ((group > 1 ? first : mine) >= at.shorts) return false;
+        const unsigned want = mine < at.shorts ? mine : at.shorts - 1;
         int n = 0;                               // sequences whose shorts all come before
-        for (int i = 0; i < a.c.S; i += 64) n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i + lane < a.c.S && known.shorts[i + lane] <= next_short));
+        for (int i = 0; i < a.c.S; i += 64) n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i + lane < a.c.S && known.shorts[i + lane] <= want));
         b = __builtin_amdgcn_readfirstlane(n < a.c.S ? n : a.c.S - 1);
         s.length = __builtin_amdgcn_readfirstlane(known.s[b].length);
         s.row0 = __builtin_amdgcn_readfirstlane(known.s[b].row0);
         s.rows = __builtin_amdgcn_readfirstlane(known.s[b].rows);
         x = extent_of<ROWS>(a, s);
-        pair = next_short - (unsigned)__builtin_amdgcn_readfirstlane(b > 0 ? (int)known.shorts[b - 1] : 0);
+        pair = want - (unsigned)__builtin_amdgcn_readfirstlane(b > 0 ? (int)known.shorts[b - 1] : 0);
         us = 0;
-        left = (unsigned)x.units;
-        next_short += grid * NW;
+        left = mine < at.shorts ? (unsigned)x.units : 0u;
         return true;
     };
-    bool alone = b < 0;                          // this wavefront sweeps a short by itself
-    if (alone) {
+    bool whole_blocks = b < 0;                   // shorts, not ranges
+    if (whole_blocks) {
         if (tid == 0) a.records[w].pieces = 0;
         if (!take_short()) return;
     }
@@ -329,9 +339,10 @@ void pasa_cache_rows(RowsArgs a)
         uniform(x.keys), uniform(x.units), uniform(x.row_blocks);
         const int ue = (int)((unsigned)(x.units - us) < left ? x.units : us + (int)left);
         const int hk = (int)(pair / (unsigned)x.row_blocks), p0 = (int)(pair - (unsigned)hk * (unsigned)x.row_blocks) * ROWS;
-        const int list = s.rows * G;             // rows of the KV head's query heads, by token, then head
+        const int list = ue > us ? s.rows * G : 0;      // rows of the KV head's query heads, by token, then head
         const int new0 = s.length - s.rows;      // position of the sequence's first row
-        const int begin = __builtin_amdgcn_readfirstlane(alone ? us : us + wave), step = __builtin_amdgcn_readfirstlane(alone ? 1 : NW);
+        uniform(group), uniform(lead);
+        const int begin = us + lead, step = group;
         const int units = begin < ue ? (ue - begin + step - 1) / step : 0;       // of this wavefront
 
         f4 O[RB][CB];
@@ -624,7 +635,7 @@ void pasa_cache_rows(RowsArgs a)
                 for (int cb = 0; cb < CB; cb += 4)
                     *reinterpret_cast<f4*>(dst + CB * i + cb) = f4{O[rb][cb][i], O[rb][cb + 1][i], O[rb][cb + 2][i], O[rb][cb + 3][i]};
         }
-        if (alone) {
+        if (group == 1) {
             __builtin_amdgcn_wave_barrier();     // a wavefront's LDS accesses are done in order
             asm volatile("" ::: "memory");
             constexpr int STEP = 64 / (D / 8);   // rows at a time, eight channels a lane
@@ -643,33 +654,44 @@ void pasa_cache_rows(RowsArgs a)
         const bool complete = us == 0 && ue == x.units;
         const unsigned my_slot = 2 * w + (first_piece ? 0u : 1u);
         float* slot = a.slots + (size_t)my_slot * cache_slot_floats(RB, D);
-        constexpr int STEP = NT / (D / 8);       // rows at a time, eight channels a lane
+        auto bring_together = [&](auto size) {
+            constexpr int GS = decltype(size)::value, STEP = 64 * GS / (D / 8);      // rows at a time, eight channels a lane
+            const int w0 = wave - lead, th = 64 * lead + ln;
 #pragma unroll
-        for (int r0 = 0; r0 < ROWS; r0 += STEP) {
-            const int th = 64 * wave + ln, r = r0 + th / (D / 8), c8 = th % (D / 8) * 8, p = p0 + r;
-            if (r >= ROWS || p >= list) break;
-            float level = lds_m[0][r], sum = 0.f;
+            for (int r0 = 0; r0 < ROWS; r0 += STEP) {
+                const int r = r0 + th / (D / 8), c8 = th % (D / 8) * 8, p = p0 + r;
+                if (r >= ROWS || p >= list) break;
+                float level = lds_m[w0][r], sum = 0.f;
 #pragma unroll
-            for (int i = 1; i < NW; ++i) level = __builtin_fmaxf(level, lds_m[i][r]);
-            f4 acc[2] = {(f4)0.f, (f4)0.f};
+                for (int i = 1; i < GS; ++i) level = __builtin_fmaxf(level, lds_m[w0 + i][r]);
+                f4 acc[2] = {(f4)0.f, (f4)0.f};
 #pragma unroll
-            for (int i = 0; i < NW; ++i) {
-                const float f = __builtin_amdgcn_exp2f(lds_m[i][r] - level);
-                sum += f * lds_l[i][r];
-                const float* src = lds_o + (i * ROWS + r) * LD + c8;
-                acc[0] += f * *reinterpret_cast<const f4*>(src);
-                acc[1] += f * *reinterpret_cast<const f4*>(src + 4);
-            }
-            if (complete) {
-                store_row(a, s.row0, hk, p, D, c8, acc, sum);
-            } else {
-                if (c8 == 0) {
-                    slot[2 * r] = sum;
-                    slot[2 * r + 1] = level;
+                for (int i = 0; i < GS; ++i) {
+                    const float f = __builtin_amdgcn_exp2f(lds_m[w0 + i][r] - level);
+                    sum += f * lds_l[w0 + i][r];
+                    const float* src = lds_o + ((w0 + i) * ROWS + r) * LD + c8;
+                    acc[0] += f * *reinterpret_cast<const f4*>(src);
+                    acc[1] += f * *reinterpret_cast<const f4*>(src + 4);
                 }
-                *reinterpret_cast<f4*>(slot + 2 * ROWS + (size_t)r * D + c8) = acc[0];
-                *reinterpret_cast<f4*>(slot + 2 * ROWS + (size_t)r * D + c8 + 4) = acc[1];
+                if (complete) {
+                    store_row(a, s.row0, hk, p, D, c8, acc, sum);
+                } else {
+                    if (c8 == 0) {
+                        slot[2 * r] = sum;
+                        slot[2 * r + 1] = level;
+                    }
+                    *reinterpret_cast<f4*>(slot + 2 * ROWS + (size_t)r * D + c8) = acc[0];
+                    *reinterpret_cast<f4*>(slot + 2 * ROWS + (size_t)r * D + c8 + 4) = acc[1];
+                }
             }
+        };
+        if (group == NW) bring_together(std::integral_constant<int, NW>{});
+        else if (group == 4) bring_together(std::integral_constant<int, 4>{});
+        else bring_together(std::integral_constant<int, 2>{});
+        if (whole_blocks) {
+            __syncthreads();                     // the LDS is free again
+            if (!take_short()) return;
+            continue;
         }
         left -= (unsigned)(ue - us);
         first_piece = false;
@@ -695,7 +717,7 @@ void pasa_cache_rows(RowsArgs a)
         if (!more && at.shorts == 0) return;
         __syncthreads();                         // the LDS is free again
         if (!more) {
-            alone = true;
+            whole_blocks = true;
             if (!take_short()) return;
         }
     }

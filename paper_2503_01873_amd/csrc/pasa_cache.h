@@ -104,6 +104,28 @@ __device__ inline Place find_place(const int* __restrict__ length, const int* __
     __shared__ unsigned sums[NT / 64];
     __shared__ int found[5];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    Place p;
+    if (S <= 64) {                     // a sequence a lane: no wavefront needs another
+        Sequence s = {0, 0, 0};
+        unsigned mine = 0;
+        if (lane < S) {
+            s = sequence_at(length, row_start, lane, R, most);
+            mine = count(s);
+        }
+        const unsigned upto = scan64(mine);
+        p.total = (unsigned)__builtin_amdgcn_readlane((int)upto, 63);
+        const unsigned want = at(p.total), before = upto - mine;
+        const unsigned long long who = __builtin_amdgcn_ballot_w64(want >= before && want < upto);
+        p.b = -1;
+        if (who != 0ull) {
+            p.b = __builtin_ctzll(who);
+            p.rest = want - (unsigned)__builtin_amdgcn_readlane((int)before, p.b);
+            p.s.length = __builtin_amdgcn_readlane(s.length, p.b);
+            p.s.row0 = __builtin_amdgcn_readlane(s.row0, p.b);
+            p.s.rows = __builtin_amdgcn_readlane(s.rows, p.b);
+        }
+        return p;
+    }
     const int each = (S + NT - 1) / NT, b0 = tid * each;
     Sequence s = {0, 0, 0};
     unsigned mine = 0;
@@ -116,7 +138,6 @@ __device__ inline Place find_place(const int* __restrict__ length, const int* __
     if (tid == 0) found[0] = -1;
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
-    Place p;
     p.total = 0;
     unsigned before = upto - mine;
 #pragma unroll

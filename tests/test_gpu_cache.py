@@ -348,3 +348,29 @@ def test_bad_pages_are_not_seen():
     ref = co.attend(c, q, row_start, 0.125)
     assert not ref[0][2].any()
     ch.check_attend(c, got, ref, "f16", 320)
+
+
+# Sequences, KV heads, table in pages of 64, and lengths (drawn between the two, some of them the third): a workgroup a block of rows, cut or not;
+# groups of wavefronts; a line that is cut; more sequences than a wavefront has lanes, than a workgroup has threads
+SHARES = [
+    (1, 1, 80, (5000, 5001), 5000), (3, 4, 16, (1, 1024), 900), (40, 8, 16, (1, 700), 1000), (40, 8, 160, (30, 600), 9000), (70, 1, 80, (1000, 5000), 17),
+    (90, 3, 80, (40, 300), 5000), (200, 2, 16, (0, 1000), 0), (300, 2, 40, (0, 100), 2500), (520, 1, 24, (1, 200), 1500), (30, 32, 2, (1, 128), 128),
+    (64, 16, 3, (1, 190), 64), (17, 16, 20, (200, 1280), 64),
+]
+
+
+@pytest.mark.parametrize("S,Hkv,width,between,some", SHARES)
+@pytest.mark.parametrize("rows", [1, 3])
+def test_every_way_to_share_out(S, Hkv, width, between, some, rows):
+    g = np.random.default_rng([S, Hkv, rows])
+    d, Hq = 64, 2 * Hkv
+    lengths = [some if g.random() < 0.06 or b == S // 2 else int(g.integers(*between)) for b in range(S)]
+    c = ch.filled(g, lengths, Hkv, d, 64, "i8", width=width)
+    n = [0 if g.random() < 0.1 else rows for _ in range(S)]
+    n[S // 2] = rows * 9 if rows > 1 else 1                              # more than a block of rows of one sequence
+    R = sum(n)
+    q = _queries(g, R, Hq, d, "f16", 3.0)
+    scale = float(np.float32(d ** -0.5))
+    got = ch.run_attend(_gpu(c), q, ch.starts(n), scale, "f16")
+    ref = co.attend(c, q, ch.starts(n), scale)
+    ch.check_attend(c, got, ref, "f16", max(lengths))
