@@ -62,10 +62,11 @@ __device__ inline Extent extent_of(const RowsArgs& a, const Sequence& s)
     return x;
 }
 
-// What a workgroup sweeps first: units `us` on of block of rows `pair` (of all heads) of sequence b, and how many from there on; b < 0: nothing.
+// What a workgroup sweeps first: from `at` on, block of rows `pair` (of all heads) of sequence b, and how far from there on; b < 0: nothing.  Counted in
+// units, with `beside` for each block before its first one.
 // Then, in groups of `group` wavefronts, whole blocks of rows of short sequences: `shorts` of them in all, of which the first ones go to workgroup `used`.
 struct Start {
-    int b, us;
+    int b, at, beside;
     unsigned pair, left, per;
     Sequence s;
     unsigned shorts, used;
@@ -80,6 +81,9 @@ struct Known {
     unsigned shorts[NT];
 };
 
+// What a block of rows costs a workgroup beside its keys (5 us), in units times rows.
+constexpr unsigned kBeside = 640;
+
 // units / size, rounded up; both below 2^13, where the quotient with a half added is off by far less than keeps it from the next whole number
 __device__ inline unsigned ranges_of(unsigned units, unsigned size)
 {
@@ -91,8 +95,9 @@ __device__ inline unsigned ranges_of(unsigned units, unsigned size)
 // - No more blocks than workgroups: each is cut into ranges of `per` units, one a workgroup, with `per` the least of eight sizes
 //   that gives no more ranges than workgroups; the largest of the eight always does: the longest sequence, or the share of the workgroups that are
 //   left when every block has one range that is not full.
-// - More: the units of all are one line that is cut evenly, and a workgroup's range may end inside one block and begin inside the next, as
-//   often as it has to.  Short sequences, which would leave wavefronts idle, stay out of the line: groups of 1, 2, 4 or 8 wavefronts, as many as there are for
+// - More, or where that gives larger ranges than an even share: the units of all, with what a block costs beside them, are one line that is cut evenly, and a
+//   workgroup's range may end inside one block and begin inside the next, as often as it has to.  (Trees behind 8 sequences, 204 blocks of 128
+//   units at most: ranges of 120 units 61 us; the line, an even share 80, 47 us, but 72 us where it does not count what blocks cost beside their units.)  Short sequences, which would leave wavefronts idle, stay out of the line: groups of 1, 2, 4 or 8 wavefronts, as many as there are for
 //   each, take their blocks whole, in 5 us and 1 us a unit and wavefront, while a workgroup would take its blocks one after the other.
 // Never cut (where the host knows that no sequence is long): ranges are whole sequences, and there is no line.
 // Up to 64 sequences a wavefront has one a lane and needs no other; up to as many as threads the wavefronts exchange their sums; beyond, the line alone.
@@ -100,16 +105,17 @@ template <int ROWS, int NT>
 __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid, int most, Known<NT>& known)
 {
     constexpr int NW = NT / 64, SIZES = 8;
+    constexpr unsigned beside = kBeside / ROWS;
     __shared__ unsigned lds_sum[4][NW], lds_try[SIZES][NW];
     __shared__ Start found;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     // Place `rest` of a sequence's ranges (or units, where the line is cut)
     auto start_at = [&](int b, const Sequence& s, unsigned rest, unsigned line, unsigned per, bool ranges) {
         const Extent x = extent_of<ROWS>(a, s);
-        const unsigned of_pair = ranges ? ranges_of((unsigned)x.units, per) : (unsigned)x.units;
-        Start st = {b, 0, rest / of_pair, 0, per, s, 0, 0, 0, 1};
-        st.us = (int)((rest - st.pair * of_pair) * (ranges ? per : 1u));
-        st.left = ranges ? (unsigned)(x.units - st.us) : line - w * per;
+        const unsigned of_pair = ranges ? ranges_of((unsigned)x.units, per) : (unsigned)x.units + beside;
+        Start st = {b, 0, ranges ? 0 : (int)beside, rest / of_pair, 0, per, s, 0, 0, 0, 1};
+        st.at = (int)((rest - st.pair * of_pair) * (ranges ? per : 1u));
+        st.left = ranges ? (unsigned)(x.units - st.at) : line - w * per;
         if (st.left > per) st.left = per;
         return st;
     };
@@ -117,10 +123,10 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
         unsigned per = 0;
         const Place at = find_place<NT>(a.c.length, a.row_start, a.c.S, a.R, most, [&](const Sequence& s) {
             const Extent x = extent_of<ROWS>(a, s);
-            return (unsigned)x.row_blocks * (unsigned)a.c.Hkv * (unsigned)x.units;
+            return (unsigned)x.row_blocks * (unsigned)a.c.Hkv * ((unsigned)x.units + beside);
         }, [&](unsigned total) { return w * (per = whole_units((total + grid - 1) / grid)); });
         if (at.b >= 0) return start_at(at.b, at.s, at.rest, at.total, (unsigned)__builtin_amdgcn_readfirstlane((int)per), false);
-        return Start{-1, 0, 0, 0, 0, {0, 0, 0}, 0, 0, 0, 1};
+        return Start{-1, 0, 0, 0, 0, 0, {0, 0, 0}, 0, 0, 0, 1};
     }
     const bool one_wave = a.c.S <= 64;
     const int b = one_wave ? lane : tid;
@@ -156,7 +162,7 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
     unsigned upto[2], all[2];
     sums(0, {units * pairs, pairs}, upto, all);
     const unsigned total = all[0], blocks = all[1];
-    const bool ranges = blocks <= grid;
+    bool ranges = blocks <= grid;
     unsigned group = NW;
     while (group > 1 && blocks * group > NW * grid) group /= 2;
     const unsigned longest_short = ranges ? 0u : a.never_cut ? 0x7fffffffu : min(32u, group * 5u * ((blocks - 1) / grid));
@@ -197,11 +203,12 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
                     if (sum <= grid) per = size((unsigned)i);
                 }
             }
+            ranges = per <= whole_units((total + blocks * beside + grid - 1) / grid);
         }
     }
     per = (unsigned)__builtin_amdgcn_readfirstlane((int)per);
     const bool is_short = units <= longest_short;
-    const unsigned mine = is_short || pairs == 0 ? 0u : ranges ? pairs * ranges_of(units, per) : units * pairs;
+    const unsigned mine = is_short || pairs == 0 ? 0u : ranges ? pairs * ranges_of(units, per) : (units + beside) * pairs;
     if (!one_wave) __syncthreads();              // the sums are read
     sums(1, {mine, is_short ? pairs : 0u}, upto, all);
     const unsigned line = all[0];
@@ -215,7 +222,7 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
     }
     const unsigned want = ranges ? w : w * per, before = upto[0] - mine;
     const bool here = want >= before && want < upto[0];
-    Start st = {-1, 0, 0, 0, per, {0, 0, 0}, 0, 0, 0, 1};
+    Start st = {-1, 0, 0, 0, 0, per, {0, 0, 0}, 0, 0, 0, 1};
     if (one_wave) {
         const unsigned long long who = __builtin_amdgcn_ballot_w64(here);
         if (who != 0ull) {
@@ -298,9 +305,9 @@ void pasa_cache_rows(RowsArgs a)
     Start at = find_start<ROWS, NT>(a, w, grid, most, known);
     // the same in all lanes, which the compiler does not see on all ways to here: the buffers' descriptions would be taken lane by lane
     auto uniform = [](auto& v) { v = (std::remove_reference_t<decltype(v)>)__builtin_amdgcn_readfirstlane((int)v); };
-    uniform(at.b), uniform(at.per), uniform(at.shorts), uniform(at.used), uniform(at.longest_short), uniform(at.group);
+    uniform(at.b), uniform(at.per), uniform(at.beside), uniform(at.at), uniform(at.shorts), uniform(at.used), uniform(at.longest_short), uniform(at.group);
     unsigned left = at.left, pair = at.pair;     // units of this workgroup still to be swept
-    int b = at.b, us = at.us;
+    int b = at.b, pos = at.at, beside = at.beside;
     Sequence s = at.s;
     Extent x = extent_of<ROWS>(a, s);
     bool first_piece = true;
@@ -323,7 +330,7 @@ void pasa_cache_rows(RowsArgs a)
         s.rows = __builtin_amdgcn_readfirstlane(known.s[b].rows);
         x = extent_of<ROWS>(a, s);
         pair = want - (unsigned)__builtin_amdgcn_readfirstlane(b > 0 ? (int)known.shorts[b - 1] : 0);
-        us = 0;
+        pos = beside = 0;
         left = mine < at.shorts ? (unsigned)x.units : 0u;
         return true;
     };
@@ -334,10 +341,12 @@ void pasa_cache_rows(RowsArgs a)
     }
 
     for (;;) {
-        uniform(b), uniform(us), uniform(left), uniform(pair);
+        uniform(b), uniform(pos), uniform(left), uniform(pair);
         uniform(s.length), uniform(s.row0), uniform(s.rows);
         uniform(x.keys), uniform(x.units), uniform(x.row_blocks);
-        const int ue = (int)((unsigned)(x.units - us) < left ? x.units : us + (int)left);
+        // the piece's units, [us, ue); none where the range ends before the block's first one, which the next workgroup then has
+        const int end = (int)((unsigned)(x.units + beside - pos) < left ? x.units + beside : pos + (int)left);
+        const int us = pos > beside ? pos - beside : 0, ue = end > beside ? end - beside : 0;
         const int hk = (int)(pair / (unsigned)x.row_blocks), p0 = (int)(pair - (unsigned)hk * (unsigned)x.row_blocks) * ROWS;
         const int list = ue > us ? s.rows * G : 0;      // rows of the KV head's query heads, by token, then head
         const int new0 = s.length - s.rows;      // position of the sequence's first row
@@ -482,26 +491,29 @@ void pasa_cache_rows(RowsArgs a)
 
                 f4 S[RB][4];
 #pragma unroll
-                for (int blk = 0; blk < 4; ++blk) {
+                for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) S[rb][blk] = (f4)0.f;
+                    for (int blk = 0; blk < 4; ++blk) S[rb][blk] = (f4)0.f;
 #pragma unroll
-                    for (int j = 0; j < D / 64; ++j) {
-                        const unsigned kw[4] = {K[blk][j].x, K[blk][j].y, K[blk][j].z, K[blk][j].w};
+                for (int j = 0; j < D / 64; ++j)
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
+                    for (int h = 0; h < 2; ++h) {
+                        h8 q[RB];
+#pragma unroll
+                        for (int rb = 0; rb < RB; ++rb) q[rb] = Q(rb, 2 * j + h);
+#pragma unroll
+                        for (int blk = 0; blk < 4; ++blk) {
+                            const unsigned kw[2] = {h == 0 ? K[blk][j].x : K[blk][j].z, h == 0 ? K[blk][j].y : K[blk][j].w};
                             h8 f;
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
-                                const h2 lo = widen2<E4M3, false>(kw[2 * h + e]), hi = widen2<E4M3, true>(kw[2 * h + e]);
+                                const h2 lo = widen2<E4M3, false>(kw[e]), hi = widen2<E4M3, true>(kw[e]);
                                 f[4 * e] = lo[0]; f[4 * e + 1] = lo[1]; f[4 * e + 2] = hi[0]; f[4 * e + 3] = hi[1];
                             }
 #pragma unroll
-                            for (int rb = 0; rb < RB; ++rb)
-                                S[rb][blk] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, Q(rb, 2 * j + h), S[rb][blk], 0, 0, 0);
+                            for (int rb = 0; rb < RB; ++rb) S[rb][blk] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, q[rb], S[rb][blk], 0, 0, 0);
                         }
                     }
-                }
                 PASA_FENCE();
                 take_entry(n + 1);
                 read_entry(n + 2);
@@ -693,15 +705,15 @@ void pasa_cache_rows(RowsArgs a)
             if (!take_short()) return;
             continue;
         }
-        left -= (unsigned)(ue - us);
-        first_piece = false;
+        left -= (unsigned)(end - pos);
+        first_piece = first_piece && ue == us;
         bool more = left > 0;
         if (!more && tid == 0) {                 // begun here, and goes on in the ranges behind?
             MergeRecord m = {0, (int)my_slot, p0, list, s.row0, hk, {0, 0}};
-            if (us == 0 && ue < x.units) m.pieces = clamp_int(1 + (int)(((unsigned)(x.units - ue) + at.per - 1) / at.per), 0, (int)(grid - w));
+            if (us == 0 && ue > 0 && ue < x.units) m.pieces = clamp_int(1 + (int)(((unsigned)(x.units - ue) + at.per - 1) / at.per), 0, (int)(grid - w));
             a.records[w] = m;
         }
-        us = 0;
+        pos = 0;
         if (more && ++pair == (unsigned)x.row_blocks * (unsigned)a.c.Hkv) {
             pair = 0;
             do {                                 // the next sequence in the line

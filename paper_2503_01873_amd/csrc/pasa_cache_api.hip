@@ -50,7 +50,7 @@ bool plan_of(const pasa_cache& c, int R, int Hq, int count, CachePlan* plan)
     plan->row_blocks = (long long)R * G <= 16LL * c.S ? 1 : 2;
     const long long pages = count > 0 && count < c.table_width ? count : c.table_width, units = (pages * c.page + kUnit - 1) / kUnit;
     const long long blocks = (long long)R * G / (16 * plan->row_blocks) + c.S;      // of rows, at most
-    if (R * G > kMaxGrid || blocks > kMaxGrid / c.Hkv || blocks * c.Hkv > kMaxGrid / units) return false;
+    if (R * G > kMaxGrid || blocks > kMaxGrid / c.Hkv || blocks * c.Hkv > kMaxGrid / (units + 40)) return false;
     const long long pairs = blocks * c.Hkv, filled = (pairs * units + kUnitsAtOnce - 1) / kUnitsAtOnce, all = pairs > filled ? pairs : filled;
     plan->grid = (int)(all < kComputeUnits ? all : kComputeUnits);
     plan->never_cut = units <= 16 && c.S <= 64 * kUnitsAtOnce;
