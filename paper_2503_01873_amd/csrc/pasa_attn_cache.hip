@@ -400,31 +400,30 @@ void pasa_cache_rows(RowsArgs a)
             float ks_raw, vs_raw;
             const int koff = lq * D + 16 * g, voff = 4 * g * D + lq * CB;
             // A block that is not there reads nothing and comes as zeros: its buffer has no bytes.
-            auto buffer_of = [&](void* base, int blk, int pages, int poss) {
-                const int page = __builtin_amdgcn_readlane(pages, 16 * blk), pos = __builtin_amdgcn_readlane(poss, 16 * blk);
-                const size_t slot = ((size_t)(unsigned)(page < 0 ? 0 : page) * (unsigned)a.c.Hkv + (unsigned)hk) * (unsigned)a.c.page + (unsigned)(pos & (a.c.page - 1));
-                const uintptr_t at = reinterpret_cast<uintptr_t>(base) + slot * D;
-                const unsigned lo = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)at), hi = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(at >> 32));
-                return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>((uintptr_t)hi << 32 | lo), 0,
-                                                         __builtin_amdgcn_readfirstlane(page < 0 ? 0 : 16 * D), 0x00020000);
+            unsigned long long at_next = 0, at_now = 0;          // bytes from the first key (value) of the pool to the block's
+            auto buffer_of = [&](void* base, int blk, unsigned long long offsets, int pages) {
+                const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)offsets, 16 * blk), hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(offsets >> 32), 16 * blk);
+                return __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(base) + ((unsigned long long)hi << 32 | lo), 0,
+                                                         __builtin_amdgcn_readlane(pages, 16 * blk) < 0 ? 0 : 16 * D, 0x00020000);
             };
             auto load_k = [&] {
+                const size_t slot = ((size_t)(unsigned)(page_next < 0 ? 0 : page_next) * (unsigned)a.c.Hkv + (unsigned)hk) * (unsigned)a.c.page +
+                                    (unsigned)(pos_next & (a.c.page - 1));
+                at_next = slot * D;
 #pragma unroll
                 for (int blk = 0; blk < 4; ++blk) {
-                    const __amdgpu_buffer_rsrc_t from = buffer_of(a.c.k, blk, page_next, pos_next);
+                    const __amdgpu_buffer_rsrc_t from = buffer_of(a.c.k, blk, at_next, page_next);
 #pragma unroll
                     for (int j = 0; j < D / 64; ++j) K[blk][j] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(from, koff + 64 * j, 0, 0));
                 }
                 // a lane a key
-                const size_t slot = ((size_t)(unsigned)(page_next < 0 ? 0 : page_next) * (unsigned)a.c.Hkv + (unsigned)hk) * (unsigned)a.c.page +
-                                    (unsigned)(pos_next & (a.c.page - 1)) + lq;
-                ks_raw = a.c.kscale[slot];
-                vs_raw = a.c.vscale[slot];
+                ks_raw = a.c.kscale[slot + lq];
+                vs_raw = a.c.vscale[slot + lq];
             };
             auto load_v = [&] {
 #pragma unroll
                 for (int blk = 0; blk < 4; ++blk) {
-                    const __amdgpu_buffer_rsrc_t from = buffer_of(a.c.v, blk, page_now, pos_now);
+                    const __amdgpu_buffer_rsrc_t from = buffer_of(a.c.v, blk, at_now, page_now);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         if constexpr (VW == 2) {
@@ -457,7 +456,7 @@ void pasa_cache_rows(RowsArgs a)
             read_entry(1);
             read_list(2);
             load_k();
-            page_now = page_next, pos_now = pos_next;
+            page_now = page_next, pos_now = pos_next, at_now = at_next;
             load_v();
             PASA_FENCE();
             h8 Qr[RB][KS];
@@ -485,7 +484,8 @@ void pasa_cache_rows(RowsArgs a)
                 // per key: what its score is multiplied by, and the value's scale; in the lanes' order of keys
                 key_f[lane] = ks_raw * a.scale2;
                 key_f[kUnit + lane] = __builtin_amdgcn_logf(vs_raw);
-                key_f[2 * kUnit + lane] = __builtin_amdgcn_rcpf(vs_raw);
+                // finite, so that 0 times it is 0: a key that is not there may have any scale, and a NaN shows in the score of the rows that see it
+                key_f[2 * kUnit + lane] = __builtin_fminf(__builtin_fmaxf(__builtin_amdgcn_rcpf(vs_raw), 0.f), 3e38f);
                 __builtin_amdgcn_wave_barrier();                 // a wavefront's LDS accesses are done in order
                 asm volatile("" ::: "memory");
 
@@ -494,13 +494,16 @@ void pasa_cache_rows(RowsArgs a)
                 for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
                     for (int blk = 0; blk < 4; ++blk) S[rb][blk] = (f4)0.f;
+                h8 q[RB][KS];
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) q[rb][ks] = Q(rb, ks);
+                if (QLDS) PASA_FENCE();          // all asked for before the first is used
 #pragma unroll
                 for (int j = 0; j < D / 64; ++j)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        h8 q[RB];
-#pragma unroll
-                        for (int rb = 0; rb < RB; ++rb) q[rb] = Q(rb, 2 * j + h);
+                    for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int blk = 0; blk < 4; ++blk) {
                             const unsigned kw[2] = {h == 0 ? K[blk][j].x : K[blk][j].z, h == 0 ? K[blk][j].y : K[blk][j].w};
@@ -511,9 +514,8 @@ void pasa_cache_rows(RowsArgs a)
                                 f[4 * e] = lo[0]; f[4 * e + 1] = lo[1]; f[4 * e + 2] = hi[0]; f[4 * e + 3] = hi[1];
                             }
 #pragma unroll
-                            for (int rb = 0; rb < RB; ++rb) S[rb][blk] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, q[rb], S[rb][blk], 0, 0, 0);
+                            for (int rb = 0; rb < RB; ++rb) S[rb][blk] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, q[rb][2 * j + h], S[rb][blk], 0, 0, 0);
                         }
-                    }
                 PASA_FENCE();
                 take_entry(n + 1);
                 read_entry(n + 2);
@@ -532,30 +534,23 @@ void pasa_cache_rows(RowsArgs a)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) S[rb][blk][i] = __builtin_fmaf(S[rb][blk][i], factor[i], lv[i]);
                 }
-                unsigned seen[RB];               // bit 4 blk + i, where not all keys are
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb) seen[rb] = 0xffffu;
                 if (__builtin_expect(!whole, 0)) {
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) seen[rb] = 0;
 #pragma unroll
                     for (int blk = 0; blk < 4; ++blk) {
                         const int pos0 = __builtin_amdgcn_readlane(pos_now, 16 * blk), page = __builtin_amdgcn_readlane(page_now, 16 * blk);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
+                            // selections, no ways: hipcc 7.2 drops the -inf of a way that && and || make
                             const int pos = pos0 + 4 * g + i, nth = pos - new0;
-                            const bool there = page >= 0 && pos < s.length;
+                            const unsigned there = (unsigned)(page >= 0) & (unsigned)(pos < s.length), proposed = (unsigned)((unsigned)nth < 64u);
 #pragma unroll
                             for (int rb = 0; rb < RB; ++rb) {
-                                const bool see = there && (pos <= last[rb] || (nth >= 0 && nth < 64 && (bits[rb] >> (nth & 63) & 1ull) != 0));
-                                seen[rb] |= (unsigned)see << (4 * blk + i);
-                                if (!see) S[rb][blk][i] = -__builtin_inff();
+                                const unsigned see = there & ((unsigned)(pos <= last[rb]) | (proposed & (unsigned)(bits[rb] >> (nth & 63))));
+                                S[rb][blk][i] = (see & 1u) != 0u ? S[rb][blk][i] : -__builtin_inff();
                             }
                             // what is no key may hold anything, NaN among it, and 0 times that is not 0
-                            if (!there) {
 #pragma unroll
-                                for (int d = 0; d < VW; ++d) V[blk >> 1][4 * (blk & 1) + i][d] = 0;
-                            }
+                            for (int d = 0; d < VW; ++d) V[blk >> 1][4 * (blk & 1) + i][d] = there != 0u ? V[blk >> 1][4 * (blk & 1) + i][d] : 0u;
                         }
                     }
                 }
@@ -587,14 +582,8 @@ void pasa_cache_rows(RowsArgs a)
                         P[rb][blk >> 1][4 * (blk & 1) + 1] = lo[1];
                         P[rb][blk >> 1][4 * (blk & 1) + 2] = hi[0];
                         P[rb][blk >> 1][4 * (blk & 1) + 3] = hi[1];
-                        if (whole) {
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) l[rb] = __builtin_fmaf(e[i], inv[blk][i], l[rb]);
-                        } else {                 // the scale of a key that is not seen may be NaN
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                if ((seen[rb] >> (4 * blk + i) & 1u) != 0u) l[rb] = __builtin_fmaf(e[i], inv[blk][i], l[rb]);
-                        }
+                        for (int i = 0; i < 4; ++i) l[rb] = __builtin_fmaf(e[i], inv[blk][i], l[rb]);
                     }
                 }
                 PASA_FENCE();
@@ -623,7 +612,7 @@ void pasa_cache_rows(RowsArgs a)
                         }
                     }
                 PASA_FENCE();
-                page_now = page_next, pos_now = pos_next;
+                page_now = page_next, pos_now = pos_next, at_now = at_next;
                 load_v();
                 PASA_FENCE();
             } while (++n < units);
