@@ -221,17 +221,23 @@ void pasa_cache_write_k(pasa_cache c, const unsigned short* __restrict__ k, cons
 // ---- tokens come back ----
 
 // D / 8 neighbouring lanes take a token, eight channels each, so that a wavefront's stores are 1 KiB of neighbouring bytes; a workgroup takes
-// kReadTokens positions of one sequence and head.  The loads of a step are asked for together: places, then codes and scales.
-constexpr int kReadTokens = 128;
-template <int D, bool E4M3>
+// read_tokens(D) positions of one sequence and head.  The loads are asked for together: places, then codes and scales.
+// STREAM: outputs of which the eight L2s would keep nothing are stored past them (two sequences of 32768 tokens on 4 heads, 134 MB of output:
+// 31.9 us, 6.4 TB/s; through the L2s 42.4); smaller ones stay there for the one who reads them next (14 x 5 heads, d = 64, 2304 tokens, 21 MB each: 11.5 us, past
+// them 11.9).
+constexpr int kReadBatch = 4;
+constexpr int read_tokens(int d) { return kReadBatch * kCacheThreads / (d / 8); }
+constexpr size_t kStreamBytes = (size_t)32 << 20;
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
+template <int D, bool E4M3, bool STREAM>
 __global__ __launch_bounds__(kCacheThreads)
 void pasa_cache_read_k(pasa_cache c, unsigned short* __restrict__ k, unsigned short* __restrict__ v, const int* __restrict__ first, int N,
                        int io_bf16, int page_log2, FastDiv heads, FastDiv chunks)
 {
-    constexpr int LT = D / 8, AT = kCacheThreads / LT, BATCH = 4;
+    constexpr int LT = D / 8, AT = kCacheThreads / LT, BATCH = kReadBatch;
     const int tid = threadIdx.x, lt = tid % LT, t0 = tid / LT;
     const unsigned up = chunks.quotient(blockIdx.x);
-    const int n0 = (int)chunks.rest(blockIdx.x, up) * kReadTokens;
+    const int n1 = (int)chunks.rest(blockIdx.x, up) * read_tokens(D);
     const int b = (int)heads.quotient(up), hk = (int)heads.rest(up, (unsigned)b);
     const int length = clamp_int(c.length[b], 0, c.table_width << page_log2), begin = first != nullptr ? first[b] : 0;
     f4 shift[2] = {(f4)0.f, (f4)0.f};
@@ -239,45 +245,46 @@ void pasa_cache_read_k(pasa_cache c, unsigned short* __restrict__ k, unsigned sh
         shift[0] = *reinterpret_cast<const f4*>(c.kshift + hk * D + 8 * lt);
         shift[1] = *reinterpret_cast<const f4*>(c.kshift + hk * D + 8 * lt + 4);
     }
-    for (int n1 = n0; n1 < n0 + kReadTokens && n1 < N; n1 += BATCH * AT) {
-        int id[BATCH], pos[BATCH];
+    int id[BATCH], pos[BATCH];
 #pragma unroll
-        for (int j = 0; j < BATCH; ++j) {
-            const long long p = (long long)begin + n1 + j * AT + t0;
-            const bool in = n1 + j * AT + t0 < N && p >= 0 && p < length;
-            pos[j] = in ? (int)p : -1;
-            id[j] = c.table[(size_t)b * c.table_width + (in ? (int)p >> page_log2 : 0)];
-        }
-        uint2 code[BATCH][2];
-        float scale[BATCH][2];
+    for (int j = 0; j < BATCH; ++j) {
+        const long long p = (long long)begin + n1 + j * AT + t0;
+        const bool in = n1 + j * AT + t0 < N && p >= 0 && p < length;
+        pos[j] = in ? (int)p : -1;
+        id[j] = c.table[(size_t)b * c.table_width + (in ? (int)p >> page_log2 : 0)];
+    }
+    uint2 code[BATCH][2];
+    float scale[BATCH][2];
 #pragma unroll
-        for (int j = 0; j < BATCH; ++j) {
-            if (pos[j] < 0 || id[j] < 0 || id[j] >= c.pages) pos[j] = -1;
-            const size_t slot = pos[j] < 0 ? 0 : (((size_t)id[j] * c.Hkv + hk) << page_log2) + (size_t)(pos[j] & (c.page - 1));
-            code[j][0] = *reinterpret_cast<const uint2*>(static_cast<const unsigned char*>(c.k) + slot * D + 8 * lt);
-            code[j][1] = *reinterpret_cast<const uint2*>(static_cast<const unsigned char*>(c.v) + slot * D + 8 * lt);
-            scale[j][0] = c.kscale[slot];
-            scale[j][1] = c.vscale[slot];
-        }
+    for (int j = 0; j < BATCH; ++j) {
+        if (pos[j] < 0 || id[j] < 0 || id[j] >= c.pages) pos[j] = -1;
+        const size_t slot = pos[j] < 0 ? 0 : (((size_t)id[j] * c.Hkv + hk) << page_log2) + (size_t)(pos[j] & (c.page - 1));
+        code[j][0] = *reinterpret_cast<const uint2*>(static_cast<const unsigned char*>(c.k) + slot * D + 8 * lt);
+        code[j][1] = *reinterpret_cast<const uint2*>(static_cast<const unsigned char*>(c.v) + slot * D + 8 * lt);
+        scale[j][0] = c.kscale[slot];
+        scale[j][1] = c.vscale[slot];
+    }
 #pragma unroll
-        for (int j = 0; j < BATCH; ++j) {
-            const int n = n1 + j * AT + t0;
-            if (n >= N) break;
-            const size_t to = (((size_t)b * heads.d + hk) * N + n) * D + 8 * lt;
+    for (int j = 0; j < BATCH; ++j) {
+        const int n = n1 + j * AT + t0;
+        if (n >= N) break;
+        const size_t to = (((size_t)b * heads.d + hk) * N + n) * D + 8 * lt;
 #pragma unroll
-            for (int which = 0; which < 2; ++which) {
-                unsigned out[4];
+        for (int which = 0; which < 2; ++which) {
+            unsigned out[4];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float x[4];
-                    widen4<E4M3>(h == 0 ? code[j][which].x : code[j][which].y, x);
+            for (int h = 0; h < 2; ++h) {
+                float x[4];
+                widen4<E4M3>(h == 0 ? code[j][which].x : code[j][which].y, x);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[i] = pos[j] >= 0 ? __builtin_fmaf(x[i], scale[j][which], which == 0 ? shift[h][i] : 0.f) : 0.f;
-                    out[2 * h] = io_bf16 ? pack_bf16(x[0], x[1]) : pack_f16(x[0], x[1]);
-                    out[2 * h + 1] = io_bf16 ? pack_bf16(x[2], x[3]) : pack_f16(x[2], x[3]);
-                }
-                *reinterpret_cast<uint4*>((which == 0 ? k : v) + to) = make_uint4(out[0], out[1], out[2], out[3]);
+                for (int i = 0; i < 4; ++i) x[i] = pos[j] >= 0 ? __builtin_fmaf(x[i], scale[j][which], which == 0 ? shift[h][i] : 0.f) : 0.f;
+                out[2 * h] = io_bf16 ? pack_bf16(x[0], x[1]) : pack_f16(x[0], x[1]);
+                out[2 * h + 1] = io_bf16 ? pack_bf16(x[2], x[3]) : pack_f16(x[2], x[3]);
             }
+            u4* dst = reinterpret_cast<u4*>((which == 0 ? k : v) + to);
+            const u4 x = {out[0], out[1], out[2], out[3]};
+            if (STREAM) __builtin_nontemporal_store(x, dst);
+            else *dst = x;
         }
     }
 }
@@ -502,14 +509,19 @@ hipError_t pasa_launch_cache_write(const pasa_cache& c, const void* k, const voi
 
 hipError_t pasa_launch_cache_read(const pasa_cache& c, void* k, void* v, const int* first, int N, int io_bf16, hipStream_t stream)
 {
-    const unsigned chunks = (unsigned)((N + kReadTokens - 1) / kReadTokens), grid = chunks * (unsigned)c.S * (unsigned)c.Hkv;
+    const int each = read_tokens(c.d);
+    const unsigned chunks = (unsigned)((N + each - 1) / each), grid = chunks * (unsigned)c.S * (unsigned)c.Hkv;
     auto go = [&](auto kernel) {
         kernel<<<grid, kCacheThreads, 0, stream>>>(c, static_cast<unsigned short*>(k), static_cast<unsigned short*>(v), first, N, io_bf16, log2_of(c.page),
                                                    fast_div(c.Hkv), fast_div(chunks));
     };
-    const bool e = c.format == PASA_CACHE_E4M3;
-    if (c.d == 128) e ? go(pasa_cache_read_k<128, true>) : go(pasa_cache_read_k<128, false>);
-    else e ? go(pasa_cache_read_k<64, true>) : go(pasa_cache_read_k<64, false>);
+    const bool e = c.format == PASA_CACHE_E4M3, far = (size_t)4 * c.S * c.Hkv * N * c.d > kStreamBytes;
+    auto of_size = [&](auto d) {
+        constexpr int D = decltype(d)::value;
+        if (e) far ? go(pasa_cache_read_k<D, true, true>) : go(pasa_cache_read_k<D, true, false>);
+        else far ? go(pasa_cache_read_k<D, false, true>) : go(pasa_cache_read_k<D, false, false>);
+    };
+    c.d == 128 ? of_size(std::integral_constant<int, 128>{}) : of_size(std::integral_constant<int, 64>{});
     return hipGetLastError();
 }
 

@@ -88,7 +88,7 @@ int pasa_cache_read(const pasa_cache* cache, void* k, void* v, const int* first,
     if (st != PASA_OK) return st;
     if (!buffer(k, 16) || !buffer(v, 16) || k == v || !aligned(first, 4) || N <= 0) return PASA_EINVAL;
     if (io_dtype != PASA_IO_F16 && io_dtype != PASA_IO_BF16) return PASA_EINVAL;
-    if (N > kMaxTokens || (((long long)N + 127) / 128) * cache->S > kMaxGrid / cache->Hkv) return PASA_EUNSUPPORTED;
+    if (N > kMaxTokens || (((long long)N + 63) / 64) * cache->S > kMaxGrid / cache->Hkv) return PASA_EUNSUPPORTED;
     return status(pasa_launch_cache_read(*cache, k, v, first, N, io_dtype == PASA_IO_BF16, static_cast<hipStream_t>(stream)));
 }
 
