@@ -279,13 +279,14 @@ __device__ inline void store_row(const RowsArgs& a, int row0, int hk, int p, int
 // The value's scale is not applied to values (there are 128 of them per key, and one P per row): it goes into the exponent.  With
 // t = score + log2(vscale), M the running maximum of t and P = 2^(t - M): O = sum P y, and the sum of the softmax is sum P / vscale.
 // P is at most 1 (2^8 between moves of the level), so fp16 holds what matters of it whatever the scales.
-template <int D, int RB, bool E4M3, bool LISTED>
+template <int D, int RB, bool E4M3, bool LISTED, bool FAR>
 __global__ __launch_bounds__(64 * kUnitsAtOnce, 2)
 void pasa_cache_rows(RowsArgs a)
 {
     constexpr int ROWS = 16 * RB, KS = D / 32, CB = D / 16, NW = kUnitsAtOnce, NT = 64 * NW;
     constexpr int LD = D + 4;                    // LDS row of the merge, in floats
     constexpr int VW = CB / 4;                   // words of a key's value that a lane takes
+    constexpr int ONCE = FAR ? 2 : 0;            // non-temporal
     constexpr bool QLDS = RB > 1;                // the query fragments wait in LDS: the registers are needed for RB blocks
     // A wavefront's own part: while it sweeps, per key of the unit the score's factor, log2 of the value's scale and 1 / it, and the query fragments;
     // afterwards its stored output.
@@ -414,7 +415,7 @@ void pasa_cache_rows(RowsArgs a)
                 for (int blk = 0; blk < 4; ++blk) {
                     const __amdgpu_buffer_rsrc_t from = buffer_of(a.c.k, blk, at_next, page_next);
 #pragma unroll
-                    for (int j = 0; j < D / 64; ++j) K[blk][j] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(from, koff + 64 * j, 0, 0));
+                    for (int j = 0; j < D / 64; ++j) K[blk][j] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(from, koff + 64 * j, 0, ONCE));
                 }
                 // a lane a key
                 ks_raw = a.c.kscale[slot + lq];
@@ -427,11 +428,11 @@ void pasa_cache_rows(RowsArgs a)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         if constexpr (VW == 2) {
-                            const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(from, voff + i * D, 0, 0));
+                            const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(from, voff + i * D, 0, ONCE));
                             V[blk >> 1][4 * (blk & 1) + i][0] = y.x;
                             V[blk >> 1][4 * (blk & 1) + i][VW - 1] = y.y;
                         } else {
-                            V[blk >> 1][4 * (blk & 1) + i][0] = __builtin_amdgcn_raw_buffer_load_b32(from, voff + i * D, 0, 0);
+                            V[blk >> 1][4 * (blk & 1) + i][0] = __builtin_amdgcn_raw_buffer_load_b32(from, voff + i * D, 0, ONCE);
                         }
                     }
                 }
@@ -839,10 +840,21 @@ hipError_t pasa_launch_attn_cache(const pasa_cache& c, const void* q, void* o, i
         return hipGetLastError();
     };
     const bool e = c.format == PASA_CACHE_E4M3, l = blocks != nullptr;
-    auto of_format = [&](auto d, auto rb) {
+    auto of_kind = [&](auto d, auto rb, auto far) {
         constexpr int D = decltype(d)::value, RB = decltype(rb)::value;
-        if (e) return l ? go(pasa_cache_rows<D, RB, true, true>, pasa_cache_merge<D, RB>) : go(pasa_cache_rows<D, RB, true, false>, pasa_cache_merge<D, RB>);
-        return l ? go(pasa_cache_rows<D, RB, false, true>, pasa_cache_merge<D, RB>) : go(pasa_cache_rows<D, RB, false, false>, pasa_cache_merge<D, RB>);
+        constexpr bool F = decltype(far)::value;
+        if (e) return l ? go(pasa_cache_rows<D, RB, true, true, F>, pasa_cache_merge<D, RB>) : go(pasa_cache_rows<D, RB, true, false, F>, pasa_cache_merge<D, RB>);
+        return l ? go(pasa_cache_rows<D, RB, false, true, F>, pasa_cache_merge<D, RB>) : go(pasa_cache_rows<D, RB, false, false, F>, pasa_cache_merge<D, RB>);
+    };
+    // Keys and values that are read once and may be more than the last cache's 256 MB are read past the caches.  us, past / through them: 277 MB
+    // (262144 keys, 4 heads) 54.3 / 58.9, 305 MB 63.2 / 65.5; 68 MB, which a program that does little else finds there again, 28.0 / 24.4
+    const long long held = (blocks != nullptr && count < c.table_width ? count : c.table_width);
+    const bool far = (double)held * c.page * c.S * c.Hkv * 2 * c.d > 256e6;
+    auto of_format = [&](auto d, auto rb) {
+        if constexpr (decltype(rb)::value == 1) {
+            if (far) return of_kind(d, rb, std::true_type{});
+        }
+        return of_kind(d, rb, std::false_type{});
     };
     auto of_rows = [&](auto d) {
         return plan.row_blocks == 1 ? of_format(d, std::integral_constant<int, 1>{}) : of_format(d, std::integral_constant<int, 2>{});

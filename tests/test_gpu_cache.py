@@ -374,3 +374,24 @@ def test_every_way_to_share_out(S, Hkv, width, between, some, rows):
     got = ch.run_attend(_gpu(c), q, ch.starts(n), scale, "f16")
     ref = co.attend(c, q, ch.starts(n), scale)
     ch.check_attend(c, got, ref, "f16", max(lengths))
+
+
+@pytest.mark.parametrize("format", FORMATS)
+@pytest.mark.parametrize("Hq,Hkv,d", [(28, 4, 128), (16, 16, 64)])
+@pytest.mark.parametrize("listed", [False, True])
+def test_tables_of_which_little_is_used(Hq, Hkv, d, format, listed):
+    """Tables as wide as they may be (keys that may be more than any cache holds are read another way), short sequences in them."""
+    g = np.random.default_rng([d, listed])
+    lengths = [1500, 3, 400, 0, 65]
+    c = ch.filled(g, lengths, Hkv, d, 64, format, wild=True)
+    table = np.full((5, 4096), -1, np.int32)
+    table[:, :c["table"].shape[1]] = c["table"]
+    c["table"] = table
+    blocks = None
+    if listed:
+        blocks = np.full((5, Hkv, 2000), -1, np.int32)
+        blocks[0, :, :9], blocks[2, :, :3], blocks[4, :, 0] = [0, 2, 3, 5, 7, 11, 13, 17, 23], [0, 4, 6], 1
+    q = _queries(g, 5, Hq, d, "f16")
+    scale = float(np.float32(d ** -0.5))
+    got = ch.run_attend(_gpu(c), q, ch.starts([1] * 5), scale, "f16", blocks=blocks)
+    ch.check_attend(c, got, co.attend(c, q, ch.starts([1] * 5), scale, blocks=blocks), "f16", 1500)
