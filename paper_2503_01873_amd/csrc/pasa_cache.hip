@@ -9,47 +9,47 @@ namespace {
 
 // ---- tokens enter ----
 
-// x / scale for a conversion that rounds to 22 bits or fewer, nearest: the quotient where fp32 holds it, otherwise an fp32 value next
-// to it whose last bit is set, so that no tie and no border of the coarser type is hit that the quotient itself does not hit.
-// The first quotient is off by at most two steps of fp32, the second, from the exact remainder, is the nearest one or next to it,
-// and the sign of its own remainder says on which side the quotient lies.
-__device__ inline float sticky_quotient(float x, float scale, float inverse)
-{
-    float q = x * inverse;
-    q = __builtin_fmaf(__builtin_fmaf(-q, scale, x), inverse, q);
-    const float r = __builtin_fmaf(-q, scale, x);
-    unsigned bits = __float_as_uint(q);
-    if (r != 0.f && q != 0.f && (bits & 1u) == 0u) bits += (r > 0.f) == (q > 0.f) ? 1u : ~0u;
-    return __uint_as_float(bits);
-}
-
 constexpr float kRound = 12582912.f + 128.f;     // 1.5 2^23: a sum with it is rounded to whole numbers, and its low byte is number + 128
 
 // Eight values of a token -> eight bytes, and the numbers that they hold.  `top`: the largest magnitude of the token, NaN where one is.
-// x * (1 / scale) is off by two steps of fp32 at most, which matters next to a tie only: one wavefront in ten finds such a value among its
-// 512 and takes the exact quotient.  (Exact ones for all: 28 instructions a value instead of 10; four prompts of 20000 tokens in all 32.7 us.)
+// Codes are the nearest of the exact quotients.  Products with 1 / scale are off by two steps of fp32 at most, which matters next to a tie only, and
+// ties are common: fp16 and bf16 values over a multiple of one of them.  (Exact quotients as quotients: 28 instructions a value.)
+//  Integers: one multiply-add rounds; where a value of the wavefront is next to a tie, x - number * scale, which fp32 holds exactly, says against scale / 2
+//   whether the number is right, and a tie goes to the even one.  5 instructions a value, 13 then.
+//  e4m3: the product and one correction by the exact remainder give the nearest fp32 value, and a tie of the quotient is one of that value; it
+//   misleads where it is a tie and the quotient is not, as its own remainder shows, one in a million of what is no tie, and there moves by a step.  Ties are
+//   where the 20 bits behind e4m3's three are a half; below 2^-6 steps are those from 2^-6 to 2^-5.  10 instructions a value.
 template <bool E4M3>
 __device__ inline uint2 encode8(const float (&x)[8], float top, float& scale, float (&held)[8])
 {
     constexpr float most = E4M3 ? 448.f : 127.f;
     const bool finite = top < __builtin_inff();
-    scale = top / most;
+    constexpr float part = 1.f / most;           // the quotient by way of it is the rounded one for every mantissa
+    scale = top * part;
+    scale = __builtin_fmaf(__builtin_fmaf(-scale, most, top), part, scale);
     if (top < 0x1p-100f) scale = 1.f;
     if (!finite) scale = __builtin_nanf("");
-    const float inverse = 1.f / scale;
+    const float inverse = __builtin_amdgcn_rcpf(scale);
     float q[8];
-    bool near = false;
     if constexpr (E4M3) {
-        // borders: the 20 bits of the quotient behind e4m3's three are a half; below 2^-6 the steps no longer shrink
-        unsigned border = ~0u, small = ~0u;
+        float left[8];
+        bool misled = false;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             q[i] = x[i] * inverse;
-            const unsigned u = __float_as_uint(q[i]), d = (u - 0x7fffcu) & 0xfffffu, s = 2u * u - 1u;
-            border = d < border ? d : border;
-            small = s < small ? s : small;
+            q[i] = __builtin_fmaf(__builtin_fmaf(-q[i], scale, x[i]), inverse, q[i]);
+            left[i] = __builtin_fmaf(-q[i], scale, x[i]);
+            const float size = __builtin_fabsf(q[i]), as = size < 0x1p-6f ? size + 0x1p-6f : size;
+            misled |= ((__float_as_uint(as) & 0xfffffu) == 0x80000u) & (left[i] != 0.f);
         }
-        near = border <= 8u || small < 2u * 0x3c800000u - 1u;
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(misled && finite) != 0ull, 0)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {        // the quotient where fp32 holds it, otherwise the value next to it whose last bit is set
+                unsigned u = __float_as_uint(q[i]);
+                if (left[i] != 0.f && q[i] != 0.f && (u & 1u) == 0u) u += (left[i] > 0.f) == (q[i] > 0.f) ? 1u : ~0u;
+                q[i] = __uint_as_float(u);
+            }
+        }
     } else {
         float off = 0.f;
 #pragma unroll
@@ -58,14 +58,16 @@ __device__ inline uint2 encode8(const float (&x)[8], float top, float& scale, fl
             held[i] = q[i] - kRound;
             off = __builtin_fmaxf(off, __builtin_fabsf(__builtin_fmaf(x[i], inverse, -held[i])));
         }
-        near = off > 0.5f - 0x1p-15f;
-    }
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(near && finite) != 0ull, 0)) {
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(off > 0.5f - 0x1p-15f && finite) != 0ull, 0)) {
+            const unsigned half = __float_as_uint(0.5f * scale);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float e = __builtin_fminf(__builtin_fmaxf(sticky_quotient(x[i], scale, inverse), -most), most);
-            q[i] = E4M3 ? e : e + kRound;        // the sum rounds the sticky quotient once
-            if (!E4M3) held[i] = q[i] - kRound;
+            for (int i = 0; i < 8; ++i) {
+                const float r = __builtin_fmaf(-held[i], scale, x[i]);
+                const float limit = __uint_as_float(half - (__float_as_uint(q[i]) & 1u));       // odd numbers move at a tie, even ones stay
+                const float step = __builtin_fabsf(r) > limit ? __builtin_copysignf(1.f, r) : 0.f;
+                held[i] += step;
+                q[i] += step;
+            }
         }
     }
     unsigned w[2];
