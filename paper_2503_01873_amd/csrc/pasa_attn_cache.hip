@@ -726,23 +726,24 @@ void pasa_cache_rows(RowsArgs a)
 }
 
 // A row block that several workgroups have swept: pieces from the slot of the one that began it and the first slots of those behind it.
-// Workgroup (w, r) adds row r of what workgroup w of the sweep has begun: D / 8 neighbouring lanes take a piece, eight channels each, and the
-// groups of lanes are added at the end, always in the same order.
-template <int D, int RB>
+// Workgroup (w, part) adds rows of what workgroup w of the sweep has begun: all its wavefronts one row, or (EACH) each a row of its own, for blocks of
+// few pieces.  D / 8 neighbouring lanes take a piece, eight channels each, and the groups of lanes are added at the end, always in the same order.
+template <int D, int RB, bool EACH>
 __global__ __launch_bounds__(kCacheThreads)
-void pasa_cache_merge(RowsArgs a, FastDiv rows)
+void pasa_cache_merge(RowsArgs a, FastDiv parts)
 {
-    constexpr int ROWS = 16 * RB, CHUNKS = D / 8, LANES = kCacheThreads / CHUNKS, AT = 4;
+    constexpr int ROWS = 16 * RB, CHUNKS = D / 8, LANES = (EACH ? 64 : kCacheThreads) / CHUNKS, AT = 4;
     __shared__ float lds_acc[4][D];
     __shared__ float lds_state[4][2];
-    const unsigned w = rows.quotient(blockIdx.x);
+    const unsigned w = parts.quotient(blockIdx.x);
     const MergeRecord m = a.records[w];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = (int)rows.rest(blockIdx.x, w), p = m.p0 + r;
-    if (m.pieces == 0 || p >= m.list) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, part = (int)parts.rest(blockIdx.x, w);
+    const int r = EACH ? 4 * part + wave : part, p = m.p0 + r;
+    if (m.pieces == 0 || r >= ROWS || p >= m.list) return;
     const int c8 = tid % CHUNKS * 8;
     float level = kNoLevel, sum = 0.f;
     f4 acc[2] = {(f4)0.f, (f4)0.f};
-    for (int i0 = tid / CHUNKS; i0 < m.pieces; i0 += AT * LANES) {
+    for (int i0 = (EACH ? lane : tid) / CHUNKS; i0 < m.pieces; i0 += AT * LANES) {
         f2 state[AT];
         f4 part[AT][2];
 #pragma unroll
@@ -783,6 +784,10 @@ void pasa_cache_merge(RowsArgs a, FastDiv rows)
         sum += __shfl_xor(sum, o);
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i >> 2][i & 3] += __shfl_xor(acc[i >> 2][i & 3], o);
+    }
+    if (EACH) {
+        if (lane < CHUNKS) store_row(a, m.row0, m.hk, p, D, c8, acc, sum);
+        return;
     }
     if (lane < CHUNKS) {
         *reinterpret_cast<f4*>(&lds_acc[wave][c8]) = acc[0];
@@ -830,21 +835,23 @@ hipError_t pasa_launch_attn_cache(const pasa_cache& c, const void* q, void* o, i
     a.never_cut = plan.never_cut;
     a.page_log2 = log2_of(c.page);
     a.G = fast_div((unsigned)(Hq / c.Hkv));
-    auto go = [&](auto rows, auto merge) {
+    auto go = [&](auto rows, auto merge, auto merge_each) {
         rows<<<plan.grid, 64 * kUnitsAtOnce, 0, stream>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || plan.grid == 1 || plan.never_cut) return e;
         const long long most = (long long)R * (Hq / c.Hkv);          // rows of a block
         const unsigned each = (unsigned)(most < 16 * plan.row_blocks ? most : 16 * plan.row_blocks);
-        merge<<<(unsigned)plan.grid * each, kCacheThreads, 0, stream>>>(a, fast_div(each));
+        // up to 16 pieces a block on average: a wavefront takes them in one step
+        if ((long long)c.S * c.Hkv * 16 >= plan.grid) merge_each<<<(unsigned)plan.grid * ((each + 3) / 4), kCacheThreads, 0, stream>>>(a, fast_div((each + 3) / 4));
+        else merge<<<(unsigned)plan.grid * each, kCacheThreads, 0, stream>>>(a, fast_div(each));
         return hipGetLastError();
     };
     const bool e = c.format == PASA_CACHE_E4M3, l = blocks != nullptr;
     auto of_kind = [&](auto d, auto rb, auto far) {
         constexpr int D = decltype(d)::value, RB = decltype(rb)::value;
         constexpr bool F = decltype(far)::value;
-        if (e) return l ? go(pasa_cache_rows<D, RB, true, true, F>, pasa_cache_merge<D, RB>) : go(pasa_cache_rows<D, RB, true, false, F>, pasa_cache_merge<D, RB>);
-        return l ? go(pasa_cache_rows<D, RB, false, true, F>, pasa_cache_merge<D, RB>) : go(pasa_cache_rows<D, RB, false, false, F>, pasa_cache_merge<D, RB>);
+        if (e) return l ? go(pasa_cache_rows<D, RB, true, true, F>, pasa_cache_merge<D, RB, false>, pasa_cache_merge<D, RB, true>) : go(pasa_cache_rows<D, RB, true, false, F>, pasa_cache_merge<D, RB, false>, pasa_cache_merge<D, RB, true>);
+        return l ? go(pasa_cache_rows<D, RB, false, true, F>, pasa_cache_merge<D, RB, false>, pasa_cache_merge<D, RB, true>) : go(pasa_cache_rows<D, RB, false, false, F>, pasa_cache_merge<D, RB, false>, pasa_cache_merge<D, RB, true>);
     };
     // Keys and values that are read once and may be more than the last cache's 256 MB are read past the caches.  us, past / through them: 277 MB
     // (262144 keys, 4 heads) 54.3 / 58.9, 305 MB 63.2 / 65.5; 68 MB, which a program that does little else finds there again, 28.0 / 24.4
