@@ -119,7 +119,7 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
         if (st.left > per) st.left = per;
         return st;
     };
-    if (a.c.S > NT) {
+    if (__builtin_expect(a.c.S > NT, 0)) {
         unsigned per = 0;
         const Place at = find_place<NT>(a.c.length, a.row_start, a.c.S, a.R, most, [&](const Sequence& s) {
             const Extent x = extent_of<ROWS>(a, s);
@@ -147,7 +147,7 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
             sum[i] = (unsigned)__builtin_amdgcn_readlane((int)upto[i], 63);
             all[i] = sum[i];
         }
-        if (one_wave) return;
+        if (__builtin_expect(one_wave, 1)) return;
         if (lane == 0) lds_sum[2 * n][wave] = sum[0], lds_sum[2 * n + 1][wave] = sum[1];
         __syncthreads();
 #pragma unroll
@@ -169,7 +169,7 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
     unsigned per = 0;
     if (ranges) {
         unsigned longest = largest64(pairs > 0 ? units : 0);
-        if (!one_wave) {
+        if (__builtin_expect(!one_wave, 0)) {
             __syncthreads();
             if (lane == 0) lds_sum[0][wave] = longest;
             __syncthreads();
@@ -181,7 +181,7 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
             if (blocks < grid) sure = min(sure, whole_units((total + grid - blocks - 1) / (grid - blocks)));
             const unsigned least = min(whole_units((total + grid - 1) / grid), sure);
             auto size = [&](unsigned i) { return whole_units(least + (sure - least) * i / (SIZES - 1)); };
-            if (one_wave) {                      // the least by halving: more ranges, smaller ones
+            if (__builtin_expect(one_wave, 1)) { // the least by halving: more ranges, smaller ones
                 unsigned low = 0, high = SIZES - 1;
                 for (int i = 0; i < 3; ++i) {
                     const unsigned middle = (low + high) / 2;
@@ -209,11 +209,11 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
     per = (unsigned)__builtin_amdgcn_readfirstlane((int)per);
     const bool is_short = units <= longest_short;
     const unsigned mine = is_short || pairs == 0 ? 0u : ranges ? pairs * ranges_of(units, per) : (units + beside) * pairs;
-    if (!one_wave) __syncthreads();              // the sums are read
+    if (__builtin_expect(!one_wave, 0)) __syncthreads();         // the sums are read
     sums(1, {mine, is_short ? pairs : 0u}, upto, all);
     const unsigned line = all[0];
     if (!ranges) per = whole_units((line + grid - 1) / grid);
-    if (all[1] > 0) {
+    if (__builtin_expect(all[1] > 0, 0)) {
         if (one_wave ? wave == 0 : true) {
             known.s[b] = s;
             known.shorts[b] = upto[1];
@@ -223,7 +223,7 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
     const unsigned want = ranges ? w : w * per, before = upto[0] - mine;
     const bool here = want >= before && want < upto[0];
     Start st = {-1, 0, 0, 0, 0, per, {0, 0, 0}, 0, 0, 0, 1};
-    if (one_wave) {
+    if (__builtin_expect(one_wave, 1)) {
         const unsigned long long who = __builtin_amdgcn_ballot_w64(here);
         if (who != 0ull) {
             const int l = __builtin_ctzll(who);
@@ -336,7 +336,7 @@ void pasa_cache_rows(RowsArgs a)
         return true;
     };
     bool whole_blocks = b < 0;                   // shorts, not ranges
-    if (whole_blocks) {
+    if (__builtin_expect(whole_blocks, 0)) {
         if (tid == 0) a.records[w].pieces = 0;
         if (!take_short()) return;
     }
@@ -637,7 +637,7 @@ void pasa_cache_rows(RowsArgs a)
                 for (int cb = 0; cb < CB; cb += 4)
                     *reinterpret_cast<f4*>(dst + CB * i + cb) = f4{O[rb][cb][i], O[rb][cb + 1][i], O[rb][cb + 2][i], O[rb][cb + 3][i]};
         }
-        if (group == 1) {
+        if (__builtin_expect(group == 1, 0)) {
             __builtin_amdgcn_wave_barrier();     // a wavefront's LDS accesses are done in order
             asm volatile("" ::: "memory");
             constexpr int STEP = 64 / (D / 8);   // rows at a time, eight channels a lane
@@ -687,10 +687,10 @@ void pasa_cache_rows(RowsArgs a)
                 }
             }
         };
-        if (group == NW) bring_together(std::integral_constant<int, NW>{});
+        if (__builtin_expect(group == NW, 1)) bring_together(std::integral_constant<int, NW>{});
         else if (group == 4) bring_together(std::integral_constant<int, 4>{});
         else bring_together(std::integral_constant<int, 2>{});
-        if (whole_blocks) {
+        if (__builtin_expect(whole_blocks, 0)) {
             __syncthreads();                     // the LDS is free again
             if (!take_short()) return;
             continue;

@@ -105,7 +105,7 @@ __device__ inline Place find_place(const int* __restrict__ length, const int* __
     __shared__ int found[5];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     Place p;
-    if (S <= 64) {                     // a sequence a lane: no wavefront needs another
+    if (__builtin_expect(S <= 64, 1)) {          // a sequence a lane: no wavefront needs another
         Sequence s = {0, 0, 0};
         unsigned mine = 0;
         if (lane < S) {
