@@ -210,7 +210,8 @@ int pasa_shift_keys_direct(const void* k, void* kprime, void* k0, int B, int Hkv
  * For servers whose sequences grow token by token and differ in length: S sequences share a pool of `pages` pages of `page`
  * tokens each; table[b][i] is the page in the pool that holds the tokens i * page .. i * page + page - 1 of sequence b (sequences
  * may share pages that neither writes).  A token takes d bytes and a scale for its key and for its value, per KV head; what is
- * held stands for code * scale.  Scales belong to a token and head, so a token that enters changes nothing that is there.
+ * held stands for code * scale.  Scales belong to a token and head, so a token that enters changes nothing that is there.  (What is
+ * brought into the buffers by other means than pasa_cache_write keeps its rules: scales above zero, no NaN among the codes.)
  *
  * Eq. (9) of the paper: a vector taken from every key leaves softmax unchanged.  kshift is such a vector per KV head (the bias
  * of the key projection, or a mean over a prompt): it is taken off before keys are rounded to 8 bits, which then need not cover

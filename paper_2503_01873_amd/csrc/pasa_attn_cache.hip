@@ -73,8 +73,7 @@ struct Start {
     int longest_short, group;
 };
 
-// What a workgroup keeps of the sequences for its shorts, where there are as many threads: each one, and how many blocks of rows of short sequences there
-// are up to and with it.
+// What a workgroup keeps of the sequences for its shorts: each one, and how many blocks of rows of short sequences there are up to and with it.
 template <int NT>
 struct Known {
     Sequence s[NT];
@@ -97,10 +96,12 @@ __device__ inline unsigned ranges_of(unsigned units, unsigned size)
 //   left when every block has one range that is not full.
 // - More, or where that gives larger ranges than an even share: the units of all, with what a block costs beside them, are one line that is cut evenly, and a
 //   workgroup's range may end inside one block and begin inside the next, as often as it has to.  (Trees behind 8 sequences, 204 blocks of 128
-//   units at most: ranges of 120 units 61 us; the line, an even share 80, 47 us, but 72 us where it does not count what blocks cost beside their units.)  Short sequences, which would leave wavefronts idle, stay out of the line: groups of 1, 2, 4 or 8 wavefronts, as many as there are for
-//   each, take their blocks whole, in 5 us and 1 us a unit and wavefront, while a workgroup would take its blocks one after the other.
+//   units at most: ranges of 120 units 59.1 us; the line, an even share of 80, 49.8; 65.4 where it does not count what blocks cost beside their units.)
+//   Short sequences, which would leave wavefronts idle, stay out of the line: groups of 1, 2, 4 or 8 wavefronts, as many as there are for each, take
+//   their blocks whole, in 5 us and 1 us a unit and wavefront, while a workgroup would take its blocks one after the other (64 sequences of up to 500
+//   keys, 8 KV heads, 14.7 us; single wavefronts 20.4).
 // Never cut (where the host knows that no sequence is long): ranges are whole sequences, and there is no line.
-// Up to 64 sequences a wavefront has one a lane and needs no other; up to as many as threads the wavefronts exchange their sums; beyond, the line alone.
+// Up to 64 sequences a wavefront has one a lane and needs no other; up to as many as threads the wavefronts exchange their sums.  More go in launches of their own.
 template <int ROWS, int NT>
 __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid, int most, Known<NT>& known)
 {
@@ -119,15 +120,6 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
         if (st.left > per) st.left = per;
         return st;
     };
-    if (__builtin_expect(a.c.S > NT, 0)) {
-        unsigned per = 0;
-        const Place at = find_place<NT>(a.c.length, a.row_start, a.c.S, a.R, most, [&](const Sequence& s) {
-            const Extent x = extent_of<ROWS>(a, s);
-            return (unsigned)x.row_blocks * (unsigned)a.c.Hkv * ((unsigned)x.units + beside);
-        }, [&](unsigned total) { return w * (per = whole_units((total + grid - 1) / grid)); });
-        if (at.b >= 0) return start_at(at.b, at.s, at.rest, at.total, (unsigned)__builtin_amdgcn_readfirstlane((int)per), false);
-        return Start{-1, 0, 0, 0, 0, 0, {0, 0, 0}, 0, 0, 0, 1};
-    }
     const bool one_wave = a.c.S <= 64;
     const int b = one_wave ? lane : tid;
     unsigned units = 1, pairs = 0;
@@ -270,6 +262,12 @@ __device__ inline void store_row(const RowsArgs& a, int row0, int hk, int p, int
 // One workgroup = 8 wavefronts sweeps a contiguous range of units; a range may end inside one (sequence, head, row block) and begin
 // inside another, whose parts go to slots and are merged by a second kernel.  So the work is even whatever the lengths, and the host need not
 // know them.  The rows are those of all query heads of a KV head: a decoding step reads its keys once.
+//
+// What bounds it: long sequences, memory (262144 keys on 4 heads, 277 MB, 47.8 us, 5.8 TB/s; 16 ragged sequences, 305 MB, 56.5 us); few keys, what hangs on one
+// another, about 10 us whatever is done in between (lengths 1.1, the table's entries 0.9, keys and queries 2, a unit 1.5, the wavefronts' states 2, the start of
+// eight XCDs 2); 32 rows, the vector unit (a unit's 495 vector instructions and 64 MFMAs of 16 clocks, two wavefronts to a SIMD: 90 % of its time).
+// Widening takes 1 instruction a key's number and 1.25 a value's (which is turned too), e4m3 0.5 and 0.75, of every lane; shared by the 16 or 32 rows it is
+// two thirds of the vector work with 16.
 //
 // GEMMs on v_mfma_f32_16x16x32_f16, transposed: S^T = K Q^T, O^T += V^T P^T.  Lane l holds query row l % 16 and, with g = l / 16, keys
 // 4g .. 4g+3 of a block of 16.  Which channels a k-step of the first GEMM consists of is free, so a lane takes 16 consecutive bytes of a
@@ -817,6 +815,7 @@ hipError_t pasa_launch_attn_cache(const pasa_cache& c, const void* q, void* o, i
                                   float scale, const unsigned long long* tree, const int* blocks, int count, int io_bf16,
                                   const CachePlan& plan, void* workspace, hipStream_t stream)
 {
+    constexpr int kSequences = 64 * kUnitsAtOnce;                    // of a launch: one a thread
     RowsArgs a;
     a.c = c;
     a.q = static_cast<const unsigned short*>(q);
@@ -835,16 +834,28 @@ hipError_t pasa_launch_attn_cache(const pasa_cache& c, const void* q, void* o, i
     a.never_cut = plan.never_cut;
     a.page_log2 = log2_of(c.page);
     a.G = fast_div((unsigned)(Hq / c.Hkv));
-    auto go = [&](auto rows, auto merge, auto merge_each) {
+    auto one = [&](auto rows, auto merge, auto merge_each) {
         rows<<<plan.grid, 64 * kUnitsAtOnce, 0, stream>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || plan.grid == 1 || plan.never_cut) return e;
         const long long most = (long long)R * (Hq / c.Hkv);          // rows of a block
         const unsigned each = (unsigned)(most < 16 * plan.row_blocks ? most : 16 * plan.row_blocks);
         // up to 16 pieces a block on average: a wavefront takes them in one step
-        if ((long long)c.S * c.Hkv * 16 >= plan.grid) merge_each<<<(unsigned)plan.grid * ((each + 3) / 4), kCacheThreads, 0, stream>>>(a, fast_div((each + 3) / 4));
+        if ((long long)a.c.S * c.Hkv * 16 >= plan.grid) merge_each<<<(unsigned)plan.grid * ((each + 3) / 4), kCacheThreads, 0, stream>>>(a, fast_div((each + 3) / 4));
         else merge<<<(unsigned)plan.grid * each, kCacheThreads, 0, stream>>>(a, fast_div(each));
         return hipGetLastError();
+    };
+    auto go = [&](auto rows, auto merge, auto merge_each) {
+        for (int b = 0; b < c.S; b += kSequences) {
+            a.c.S = c.S - b < kSequences ? c.S - b : kSequences;
+            a.c.table = c.table + (size_t)b * c.table_width;
+            a.c.length = c.length + b;
+            a.row_start = row_start + b;
+            if (blocks != nullptr) a.blocks = blocks + (size_t)b * c.Hkv * count;
+            const hipError_t e = one(rows, merge, merge_each);
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
     };
     const bool e = c.format == PASA_CACHE_E4M3, l = blocks != nullptr;
     auto of_kind = [&](auto d, auto rb, auto far) {

@@ -89,93 +89,6 @@ __device__ inline unsigned largest64(unsigned x)
     return (unsigned)__builtin_amdgcn_readlane((int)x, 63);
 }
 
-// A workgroup's place in work that is shared out over the sequences: sequence b has count(sequence) pieces, and piece `at(total)` of all
-// lies in sequence `b`, the `rest`-th there.  b < 0 where there is no such piece.  All NT threads call it (at with the same result in all); every
-// thread counts its own share of the sequences, one scan over the threads finds who has the piece, and that one walks its share (which is a single one up to NT sequences)
-// and leaves what it has read: nothing is waited for twice.
-struct Place {
-    int b;
-    unsigned rest, total;
-    Sequence s;
-};
-template <int NT, class Count, class At>
-__device__ inline Place find_place(const int* __restrict__ length, const int* __restrict__ row_start, int S, int R, int most, Count count, At at)
-{
-    __shared__ unsigned sums[NT / 64];
-    __shared__ int found[5];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    Place p;
-    if (__builtin_expect(S <= 64, 1)) {          // a sequence a lane: no wavefront needs another
-        Sequence s = {0, 0, 0};
-        unsigned mine = 0;
-        if (lane < S) {
-            s = sequence_at(length, row_start, lane, R, most);
-            mine = count(s);
-        }
-        const unsigned upto = scan64(mine);
-        p.total = (unsigned)__builtin_amdgcn_readlane((int)upto, 63);
-        const unsigned want = at(p.total), before = upto - mine;
-        const unsigned long long who = __builtin_amdgcn_ballot_w64(want >= before && want < upto);
-        p.b = -1;
-        if (who != 0ull) {
-            p.b = __builtin_ctzll(who);
-            p.rest = want - (unsigned)__builtin_amdgcn_readlane((int)before, p.b);
-            p.s.length = __builtin_amdgcn_readlane(s.length, p.b);
-            p.s.row0 = __builtin_amdgcn_readlane(s.row0, p.b);
-            p.s.rows = __builtin_amdgcn_readlane(s.rows, p.b);
-        }
-        return p;
-    }
-    const int each = (S + NT - 1) / NT, b0 = tid * each;
-    Sequence s = {0, 0, 0};
-    unsigned mine = 0;
-    for (int i = 0; i < each; ++i)
-        if (b0 + i < S) {
-            s = sequence_at(length, row_start, b0 + i, R, most);
-            mine += count(s);
-        }
-    const unsigned upto = scan64(mine);
-    if (tid == 0) found[0] = -1;
-    if (lane == 63) sums[wave] = upto;
-    __syncthreads();
-    p.total = 0;
-    unsigned before = upto - mine;
-#pragma unroll
-    for (int w = 0; w < NT / 64; ++w) {
-        if (w < wave) before += sums[w];
-        p.total += sums[w];
-    }
-    const unsigned want = at(p.total);
-    if (want >= before && want < before + mine) {
-        int b = b0;
-        unsigned left = want - before;
-        if (each > 1)
-            for (;; ++b) {
-                if (b >= S || b >= b0 + each) {      // not as it was counted: somebody writes to length or row_start meanwhile
-                    b = -1;
-                    break;
-                }
-                s = sequence_at(length, row_start, b, R, most);
-                const unsigned c = count(s);
-                if (left < c) break;
-                left -= c;
-            }
-        found[0] = b;
-        found[1] = (int)left;
-        found[2] = s.length;
-        found[3] = s.row0;
-        found[4] = s.rows;
-    }
-    __syncthreads();
-    p.b = __builtin_amdgcn_readfirstlane(found[0]);
-    p.rest = (unsigned)__builtin_amdgcn_readfirstlane(found[1]);
-    p.total = (unsigned)__builtin_amdgcn_readfirstlane((int)p.total);
-    p.s.length = __builtin_amdgcn_readfirstlane(found[2]);
-    p.s.row0 = __builtin_amdgcn_readfirstlane(found[3]);
-    p.s.rows = __builtin_amdgcn_readfirstlane(found[4]);
-    return p;
-}
-
 // Four e4m3 or excess-128 bytes -> fp32, exactly
 template <bool E4M3>
 __device__ inline void widen4(unsigned w, float (&x)[4])

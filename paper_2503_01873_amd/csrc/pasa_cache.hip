@@ -116,10 +116,92 @@ __device__ inline float largest(float x)
     return x;
 }
 
+// Where piece `want` of work lies that is shared out over the sequences, of which one has count(sequence) pieces: in sequence `b`, the `rest`-th
+// there; b < 0 where there is no such piece.  All NT threads call it.  Up to 64 sequences a wavefront has one a lane and needs no other; otherwise every thread
+// counts its own share of them, one scan over the threads finds who has the piece, and that one walks its share (a single one up to NT
+// sequences) and leaves what it has read: nothing is waited for twice.
+struct Place {
+    int b;
+    unsigned rest;
+    Sequence s;
+};
+template <int NT, class Count>
+__device__ inline Place find_place(const int* __restrict__ length, const int* __restrict__ row_start, int S, int R, int most, unsigned want, Count count)
+{
+    __shared__ unsigned sums[NT / 64];
+    __shared__ int found[5];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    Place p;
+    if (__builtin_expect(S <= 64, 1)) {
+        Sequence s = {0, 0, 0};
+        unsigned mine = 0;
+        if (lane < S) {
+            s = sequence_at(length, row_start, lane, R, most);
+            mine = count(s);
+        }
+        const unsigned upto = scan64(mine);
+        const unsigned before = upto - mine;
+        const unsigned long long who = __builtin_amdgcn_ballot_w64(want >= before && want < upto);
+        p.b = -1;
+        if (who != 0ull) {
+            p.b = __builtin_ctzll(who);
+            p.rest = want - (unsigned)__builtin_amdgcn_readlane((int)before, p.b);
+            p.s.length = __builtin_amdgcn_readlane(s.length, p.b);
+            p.s.row0 = __builtin_amdgcn_readlane(s.row0, p.b);
+            p.s.rows = __builtin_amdgcn_readlane(s.rows, p.b);
+        }
+        return p;
+    }
+    const int each = (S + NT - 1) / NT, b0 = tid * each;
+    Sequence s = {0, 0, 0};
+    unsigned mine = 0;
+    for (int i = 0; i < each; ++i)
+        if (b0 + i < S) {
+            s = sequence_at(length, row_start, b0 + i, R, most);
+            mine += count(s);
+        }
+    const unsigned upto = scan64(mine);
+    if (tid == 0) found[0] = -1;
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    unsigned before = upto - mine;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w)
+        if (w < wave) before += sums[w];
+    if (want >= before && want < before + mine) {
+        int b = b0;
+        unsigned left = want - before;
+        if (each > 1)
+            for (;; ++b) {
+                if (b >= S || b >= b0 + each) {      // not as it was counted: somebody writes to length or row_start meanwhile
+                    b = -1;
+                    break;
+                }
+                s = sequence_at(length, row_start, b, R, most);
+                const unsigned c = count(s);
+                if (left < c) break;
+                left -= c;
+            }
+        found[0] = b;
+        found[1] = (int)left;
+        found[2] = s.length;
+        found[3] = s.row0;
+        found[4] = s.rows;
+    }
+    __syncthreads();
+    p.b = __builtin_amdgcn_readfirstlane(found[0]);
+    p.rest = (unsigned)__builtin_amdgcn_readfirstlane(found[1]);
+    p.s.length = __builtin_amdgcn_readfirstlane(found[2]);
+    p.s.row0 = __builtin_amdgcn_readfirstlane(found[3]);
+    p.s.rows = __builtin_amdgcn_readfirstlane(found[4]);
+    return p;
+}
+
 // One workgroup per page that is written to and KV head: D / 8 neighbouring lanes take a token.  Where means are kept, the page's
 // older tokens are read too: a mean made from all tokens is the same whatever the steps that brought them, and writing a
 // token again corrects it.  Partial sums of the lanes that share channels are added in a fixed order.
-// What bounds it: a step, what hangs on one another (lengths, table, tokens; 5 us); prompts, memory.
+// What bounds it: a step, what hangs on one another (lengths, table, tokens: 16 tokens 4.4 us); prompts, the vector unit (10 to 16 instructions a
+// value) and memory: 32768 tokens on 8 heads, integers, 201 MB, 45 us, 4.5 TB/s.
 template <int D, bool E4M3, int NT>
 __global__ __launch_bounds__(NT)
 void pasa_cache_write_k(pasa_cache c, const unsigned short* __restrict__ k, const unsigned short* __restrict__ v, int R, long long row_stride,
@@ -138,9 +220,9 @@ void pasa_cache_write_k(pasa_cache c, const unsigned short* __restrict__ k, cons
         shift[1] = *reinterpret_cast<const f4*>(c.kshift + hk * D + 8 * lt + 4);
     }
     auto first_page = [&](const Sequence& s) { return (s.length > s.rows ? s.length - s.rows : 0) >> page_log2; };
-    const Place at = find_place<NT>(c.length, row_start, c.S, R, most, [&](const Sequence& s) {
+    const Place at = find_place<NT>(c.length, row_start, c.S, R, most, piece, [&](const Sequence& s) {
         return s.rows == 0 || s.length == 0 ? 0u : (unsigned)(((s.length - 1) >> page_log2) - first_page(s) + 1);
-    }, [&](unsigned) { return piece; });
+    });
     if (at.b < 0) return;
     const Sequence s = at.s;
     const int place = first_page(s) + (int)at.rest, pos0 = place << page_log2;
@@ -306,8 +388,8 @@ __device__ inline unsigned long long order_of(double x)
 // One wavefront takes 16 pages of a sequence and head, on v_mfma_f64_16x16x4f64: rows of queries times means, lane l with g = l / 16 holding
 // a quarter of the channels (D / 4 from D / 4 * g on; which channels a k-step consists of is free) of query row and of page l % 16.
 // The products of fp16 queries and fp32 means are exact in 64 bits, and so, nearly, are their sums: which pages are chosen does
-// not depend on an order of additions unless two scores agree to 15 digits.  The matrix unit's rate in 64 bits is far from bounding it (16 steps of
-// 16 sequences of 512 pages on 4 heads: 1 us of it); what hangs on one another does: lengths, table, means.
+// not depend on an order of additions unless two scores agree to 15 digits.  A wavefront's 32 steps (d = 128) take the matrix unit 0.9 us; what
+// bounds it is what hangs on one another, lengths, table, means: 16 sequences of up to 512 pages on 4 heads, 8.6 MB, 7.5 us.
 typedef double d4 __attribute__((ext_vector_type(4)));
 template <int D>
 __global__ __launch_bounds__(kCacheThreads)
@@ -366,7 +448,7 @@ void pasa_cache_score_k(pasa_cache c, const unsigned short* __restrict__ q, int 
 // One workgroup per sequence and head.  The pages that are always taken leave first; of the others the want-th largest word is found
 // digit by digit, 8 bits at a time, from the first bit on that they differ in (sign and exponents of scores are much alike), until
 // the words that share the digits so far are all taken.  Words above it are taken, and of its equals the first.  They leave in order.
-// NT threads of EACH words: 256 of 4 for tables up to 1024 pages.
+// NT threads of EACH words: 256 of 4 for tables up to 1024 pages (16 x 4 of up to 512 pages 4.0 us, with 1024 threads and all 64 bits 6.7), which a barrier costs less.
 template <int NT, int EACH>
 __global__ __launch_bounds__(NT)
 void pasa_cache_pick_k(pasa_cache c, const int* __restrict__ row_start, int R, int count, int page_log2, FastDiv heads,

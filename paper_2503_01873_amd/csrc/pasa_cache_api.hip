@@ -41,9 +41,11 @@ int check_rows(const pasa_cache* c, const void* p, int R, long long row_stride, 
 
 int check_workspace(const void* ws, size_t bytes, size_t need) { return buffer(ws, 256) && bytes >= need ? PASA_OK : PASA_EWORKSPACE; }
 
-// Rows per workgroup: 16 where the rows of a KV head fill no more on average, 32 otherwise.  Workgroups: one to a compute unit (their eight wavefronts take
-// its registers), and no more than there are blocks of rows or leave each wavefront a unit.  Never cut: up to 1024 keys, where a merge costs what it saves,
-// and as many sequences as the kernel has threads.  False where the units do not fit 31 bits.
+// Rows per workgroup: 16 where the rows of a KV head fill no more on average, 32 otherwise (16 sequences of 8192 keys, 28 heads on 4, four rows each, that is 28 rows: 39.5 us, in
+// blocks of 16, which read the keys twice, 45.2; 8 of 30000 keys, 8 KV heads, 20 rows: 103 / 153).  Workgroups: one to a compute unit (their eight
+// wavefronts take its registers), and no more than there are blocks of rows or leave each wavefront a unit.  Never cut: up to 1024 keys, where a merge costs
+// what it saves (us, never / cut: one sequence of 500 keys 10.6 / 12.4, of 1024 13.8 / 13.8, 64 of 1024 15.5 / 17.4; one of 2048 19.1 / 13.8).  False where
+// the units, with what blocks cost beside them, do not fit 31 bits.
 bool plan_of(const pasa_cache& c, int R, int Hq, int count, CachePlan* plan)
 {
     const long long G = Hq / c.Hkv;
@@ -53,7 +55,7 @@ bool plan_of(const pasa_cache& c, int R, int Hq, int count, CachePlan* plan)
     if (R * G > kMaxGrid || blocks > kMaxGrid / c.Hkv || blocks * c.Hkv > kMaxGrid / (units + 40)) return false;
     const long long pairs = blocks * c.Hkv, filled = (pairs * units + kUnitsAtOnce - 1) / kUnitsAtOnce, all = pairs > filled ? pairs : filled;
     plan->grid = (int)(all < kComputeUnits ? all : kComputeUnits);
-    plan->never_cut = units <= 16 && c.S <= 64 * kUnitsAtOnce;
+    plan->never_cut = units <= 16;
     return true;
 }
 

@@ -395,3 +395,36 @@ def test_tables_of_which_little_is_used(Hq, Hkv, d, format, listed):
     scale = float(np.float32(d ** -0.5))
     got = ch.run_attend(_gpu(c), q, ch.starts([1] * 5), scale, "f16", blocks=blocks)
     ch.check_attend(c, got, co.attend(c, q, ch.starts([1] * 5), scale, blocks=blocks), "f16", 1500)
+
+
+@pytest.mark.parametrize("S", [64, 65, 256, 300, 700])
+def test_many_sequences_write_and_attend(S):
+    """As many sequences as a wavefront has lanes, as a workgroup has threads, and more; some without rows."""
+    import torch
+    g = np.random.default_rng(S)
+    Hkv, Hq, d, page = 2, 4, 64, 16
+    lengths = g.integers(0, 40, S)
+    c = ch.filled(g, [int(n) for n in lengths], Hkv, d, page, "i8", width=5, shift=True)
+    rows = g.integers(0, 4, S)
+    c["length"] = (c["length"] + rows).astype(np.int32)
+    R = int(rows.sum()) + 2
+    k, v = (ch.rounded(g.standard_normal((R, Hkv, d)), "f16") for _ in range(2))
+    q = _queries(g, R, Hq, d, "f16")
+    gpu = _gpu(c)
+    co.write(c, k, v, ch.starts(rows))
+    _write(gpu, k, v, ch.starts(rows), "f16")
+    _same_cache(gpu, c)
+    blocks = np.full((S, Hkv, 3), -1, np.int32)
+    for b in range(S):
+        pages = min(3, -(-int(c["length"][b]) // page))
+        blocks[b, :, :pages] = np.arange(pages)
+    for chosen in (None, blocks):
+        got = ch.run_attend(gpu, q, ch.starts(rows), 0.125, "f16", blocks=chosen)
+        ch.check_attend(c, got, co.attend(c, q, ch.starts(rows), 0.125, blocks=chosen), "f16", 80)
+    out = torch.empty((S, Hkv, 2), dtype=torch.int32, device="cuda:0")
+    ws = torch.empty(P.pasa_cache_choose_workspace(gpu.cache), dtype=torch.uint8, device="cuda:0")
+    tq, st = ch.tensor(q, "f16")
+    c["kmean"] = gpu.back("kmean")
+    P.pasa_cache_choose(gpu.cache, tq, R, st, ch.ints(ch.starts(rows)), Hq, out, 2, 0, 1, ws, ws.numel(), torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    assert np.array_equal(out.cpu().numpy(), co.choose(c, q, ch.starts(rows), 2, 0, 1))
