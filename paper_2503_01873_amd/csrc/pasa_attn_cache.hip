@@ -7,8 +7,9 @@
 
 namespace {
 
-// A row's output moves to a new level when a score exceeds the stored one by 2^8: P stays below 2^8 until then, far inside fp16.
-constexpr float kRise = 8.f;
+// A row's level is set 2^7 below its largest product of score and scale, and set again when one exceeds it by 2^15: P is 2^7 to 2^15 there, inside fp16, and
+// what is 2^-21 of it or more keeps all of fp16's bits (2^-14 with levels at the largest itself; many keys of little weight each are a long row's rule).
+constexpr float kBelow = 7.f, kRise = 15.f;
 constexpr float kNoLevel = -1e30f;               // finite: a score of -inf against it gives 0 and no NaN
 
 // The bytes of two keys' values, two channels a word, as fp16 pairs (key, next key) of one channel; and of a key, as pairs of channels.
@@ -275,8 +276,8 @@ __device__ inline void store_row(const RowsArgs& a, int row0, int hk, int p, int
 // consecutive bytes of a key's value, and the 8 keys x D / 16 channels that it holds are turned while they are widened.
 //
 // The value's scale is not applied to values (there are 128 of them per key, and one P per row): it goes into the exponent.  With
-// t = score + log2(vscale), M the running maximum of t and P = 2^(t - M): O = sum P y, and the sum of the softmax is sum P / vscale.
-// P is at most 1 (2^8 between moves of the level), so fp16 holds what matters of it whatever the scales.
+// t = score + log2(vscale), M a level near the running maximum of t and P = 2^(t - M): O = sum P y, and the sum of the softmax is sum P / vscale.
+// P is at most 2^15, whatever the scales, and fp16 holds what matters of it.
 template <int D, int RB, bool E4M3, bool LISTED, bool FAR>
 __global__ __launch_bounds__(64 * kUnitsAtOnce, 2)
 void pasa_cache_rows(RowsArgs a)
@@ -480,6 +481,7 @@ void pasa_cache_rows(RowsArgs a)
             int n = 0;
             do {
                 const bool whole = __builtin_amdgcn_ballot_w64(page_now >= 0 && pos_now + 16 <= new0) == ~0ull;      // all rows see all keys of the unit
+                const bool vs_one = vs_raw == 1.f;
                 // per key: what its score is multiplied by, and the value's scale; in the lanes' order of keys
                 key_f[lane] = ks_raw * a.scale2;
                 key_f[kUnit + lane] = __builtin_amdgcn_logf(vs_raw);
@@ -533,6 +535,27 @@ void pasa_cache_rows(RowsArgs a)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) S[rb][blk][i] = __builtin_fmaf(S[rb][blk][i], factor[i], lv[i]);
                 }
+                // A token whose value is all zeros has the scale 1, which may be far above the others', and adds nothing to O: it is not to raise the
+                // level that P is rounded at (a first token with most of the weight would take the others below what fp16 holds).  Any scale
+                // stands for its value; 2^-60 is below those of fp16 values, and far above where its share of the sum would be lost.
+                if (__builtin_expect(__builtin_amdgcn_ballot_w64(vs_one) != 0ull, 0)) {
+#pragma unroll
+                    for (int blk = 0; blk < 4; ++blk)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            unsigned any = 0;
+#pragma unroll
+                            for (int d = 0; d < VW; ++d) {
+                                const unsigned y = V[blk >> 1][4 * (blk & 1) + i][d];
+                                any |= E4M3 ? y & 0x7f7f7f7fu : y ^ 0x80808080u;
+                            }
+                            const unsigned long long who = __builtin_amdgcn_ballot_w64(any != 0u);       // lanes 16 g .. 16 g + 15 have a key
+                            const bool zeros = ((unsigned)(who >> (16 * g)) & 0xffffu) == 0u && inv[blk][i] == 1.f;
+                            inv[blk][i] = zeros ? 0x1p60f : inv[blk][i];
+#pragma unroll
+                            for (int rb = 0; rb < RB; ++rb) S[rb][blk][i] = zeros ? S[rb][blk][i] - 60.f : S[rb][blk][i];
+                        }
+                }
                 if (__builtin_expect(!whole, 0)) {
 #pragma unroll
                     for (int blk = 0; blk < 4; ++blk) {
@@ -564,7 +587,7 @@ void pasa_cache_rows(RowsArgs a)
                         for (int i = 0; i < 4; ++i) top = __builtin_fmaxf(top, S[rb][blk][i]);
                     if (__builtin_amdgcn_ballot_w64(top > M[rb] + kRise) != 0ull) {
                         const float row_top = max_row(top);
-                        const float level = row_top > M[rb] + kRise ? row_top : M[rb];
+                        const float level = row_top > M[rb] + kRise ? row_top - kBelow : M[rb];
                         const float r = __builtin_amdgcn_exp2f(M[rb] - level);
                         M[rb] = level;
                         l[rb] *= r;

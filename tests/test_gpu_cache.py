@@ -428,3 +428,51 @@ def test_many_sequences_write_and_attend(S):
     P.pasa_cache_choose(gpu.cache, tq, R, st, ch.ints(ch.starts(rows)), Hq, out, 2, 0, 1, ws, ws.numel(), torch.cuda.current_stream())
     torch.cuda.synchronize()
     assert np.array_equal(out.cpu().numpy(), co.choose(c, q, ch.starts(rows), 2, 0, 1))
+
+
+@pytest.mark.parametrize("format", FORMATS)
+@pytest.mark.parametrize("Hq,Hkv,d,rows", [(8, 2, 128, 1), (4, 4, 64, 1), (8, 2, 128, 7), (16, 4, 64, 5)])
+def test_tokens_without_a_value_do_not_blur_the_others(Hq, Hkv, d, rows, format):
+    """The first token, and a few others, have values of zeros (and so the scale 1) and half of the weight; the others' values are small."""
+    g = np.random.default_rng([13, d, rows])
+    L, S, page = 5000, 2, 64
+    c = ch.filled(g, [0, 0], Hkv, d, page, format, width=-(-L // page))
+    c["length"][:] = [L, 700]
+    q = _queries(g, 1, Hq, d, "f16", 0.3).repeat(S * rows, 0)
+    k, v = 0.3 * g.standard_normal((L + 700, Hkv, d)), 0.01 * (1 + 0.25 * g.standard_normal((L + 700, Hkv, d)))
+    for n in (0, 77, 78, L, L + 699):
+        v[n] = 0.0
+    scale = float(np.float32(d ** -0.5))
+    for n in (0, L):                                                    # a key whose scores are about log(L)
+        for h in range(Hkv):
+            t = q[0, h * Hq // Hkv:(h + 1) * Hq // Hkv].T
+            k[n, h] = np.linalg.lstsq(t.T, np.full(t.shape[1], np.log(L) / scale), rcond=None)[0]
+    co.write(c, ch.rounded(k, "f16"), ch.rounded(v, "f16"), np.array([0, L, L + 700], np.int32))
+    zeros = c["vscale"] == 1.0
+    assert zeros.any()
+    ref = co.attend(c, q, ch.starts([rows] * S), scale)
+    got = ch.run_attend(_gpu(c), q, ch.starts([rows] * S), scale, "f16")
+    c["vscale"] = np.where(zeros, 0.0, c["vscale"]).astype(np.float32)       # no part of what a row's largest product may be
+    ch.check_attend(c, got, ref, "f16", L)
+    # nothing but such tokens: zeros
+    c["vscale"] = np.ones_like(c["vscale"])
+    c["v"][:] = 128 if format == "i8" else 0x80
+    assert not ch.run_attend(_gpu(c), q, ch.starts([rows] * S), scale, "f16").any()
+
+
+@pytest.mark.parametrize("share", [0.3, 0.5, 0.83])
+@pytest.mark.parametrize("rows", [1, 9])
+def test_many_keys_of_little_weight(rows, share):
+    """One key has a share of the weight, 100000 others the rest, all alike, and values of one sign: what P's rounding takes from each adds up.  P keeps 2^-25 of
+    a level that is at least 2^7 below the row's largest product."""
+    g = np.random.default_rng([14, rows])
+    L, Hq, Hkv, d, page = 100000, 2, 1, 64, 128
+    c = ch.filled(g, [0], Hkv, d, page, "i8", width=-(-L // page))
+    c["length"][:] = L
+    q = ch.rounded(g.standard_normal((1, 1, d)), "f16").astype(np.float64).repeat(Hq, 1).repeat(rows, 0)
+    k, v = np.zeros((L, Hkv, d)), 1 + 0.1 * g.standard_normal((L, Hkv, d))
+    k[0] = q[0, 0] / (q[0, 0] @ q[0, 0]) * np.log(L * share / (1 - share)) / 0.125
+    co.write(c, ch.rounded(k, "f16"), ch.rounded(v, "f16"), np.array([0, L], np.int32))
+    ref = co.attend(c, q, ch.starts([rows]), 0.125)
+    got = ch.run_attend(_gpu(c), q, ch.starts([rows]), 0.125, "f16")
+    ch.check_attend(c, got, ref, "f16", L / 128)
