@@ -515,15 +515,15 @@ void pasa_cache_pick_k(pasa_cache c, const int* __restrict__ row_start, int R, i
         for (int i = 0; i < EACH; ++i)
             if (word[i] != kAlways) word[i] = word[i] >= base ? word[i] - base + one : 0ull;
         const int top = 63 - __builtin_clzll(((unsigned long long)(largest - least) << 32 | 0xffffffffull) + one);
-        shift = top < 7 ? 0 : top - 7;
+        shift = top - 7;                         // top is 31 at least
         limit = 0ull;
-        for (;;) {
+        for (int from = top + 1;;) {             // the digit in hand: bits shift .. from - 1
             for (int i = tid; i < 256; i += NT) bins[i] = 0;
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < EACH; ++i)
-                if (tid * EACH + i < pages && word[i] != kAlways && (shift + 8 >= 64 || (word[i] >> (shift + 8)) == (limit >> (shift + 8))))
-                    atomicAdd(&bins[(word[i] >> shift) & 255u], 1u);
+                if (tid * EACH + i < pages && word[i] != kAlways && (from >= 64 || (word[i] >> from) == (limit >> from)))
+                    atomicAdd(&bins[(word[i] >> shift) & ((1u << (from - shift)) - 1u)], 1u);
             __syncthreads();
             if (tid < 64) {                      // four bins a lane, from the top: lane 0 has 255 .. 252
                 unsigned mine[4], total = 0;
@@ -546,8 +546,9 @@ void pasa_cache_pick_k(pasa_cache c, const int* __restrict__ row_start, int R, i
             limit |= (unsigned long long)digit_found << shift;
             want -= above_found;
             if (done || shift == 0) break;
+            // the last digit has the bits that are left: with 8, words above the limit, which `want` no longer counts, would be counted again
+            from = shift;
             shift = shift < 8 ? 0 : shift - 8;
-            limit &= ~((1ull << (shift + 8)) - 1ull);            // digits overlap where fewer than 8 bits are left
         }
     }
     // pages that are always taken count as above, or, where there are more of them than wanted, as the equals
