@@ -10,7 +10,7 @@ namespace {
 // A row's level is set 2^7 below its largest product of score and scale, and set again when one exceeds it by 2^15: P is 2^7 to 2^15 there, inside fp16, and
 // what is 2^-21 of it or more keeps all of fp16's bits (2^-14 with levels at the largest itself; many keys of little weight each are a long row's rule).
 constexpr float kBelow = 7.f, kRise = 15.f;
-constexpr float kNoLevel = -1e30f;               // finite: a score of -inf against it gives 0 and no NaN
+constexpr float kNoLevel = -3.402823466e38f;     // the lowest finite number: a score of -inf against it gives 0 and no NaN, and no finite one lies below it
 
 // The bytes of two keys' values, two channels a word, as fp16 pairs (key, next key) of one channel; and of a key, as pairs of channels.
 // Excess-128 bytes become 1024 + byte by putting 0x64 above them, exactly, and 1152 is taken off, exactly.
