@@ -12,6 +12,11 @@ namespace {
 constexpr float kBelow = 7.f, kRise = 15.f;
 constexpr float kNoLevel = -3.402823466e38f;     // the lowest finite number: a score of -inf against it gives 0 and no NaN, and no finite one lies below it
 
+// The sum of a row's softmax is held times 2^-14.  A weight over a value's scale is up to 2^15 / (2^-100 / 448), and 262144 of them come to 2^142, which fp32
+// holds no more; at the other end, P = 2^7 and values of 2^128, it is 2^-128 then, which fp32 still holds.
+constexpr int kSumBits = 14;
+constexpr float kSum = 1.f / (1 << kSumBits);
+
 // The bytes of two keys' values, two channels a word, as fp16 pairs (key, next key) of one channel; and of a key, as pairs of channels.
 // Excess-128 bytes become 1024 + byte by putting 0x64 above them, exactly, and 1152 is taken off, exactly.
 template <bool E4M3, bool HIGH>
@@ -246,15 +251,17 @@ __device__ inline unsigned logical_workgroup(unsigned idx, unsigned grid)
     return x * whole + (x < rest ? x : rest) + (idx >> 3);
 }
 
-// Eight channels of a row's output, divided by the sum of its softmax
+// Eight channels of a row's output, divided by the sum of its softmax: by its mantissa, then by the power of two, as fp32 may not hold what is
+// between (one over a sum below 2^-126)
 __device__ inline void store_row(const RowsArgs& a, int row0, int hk, int p, int D, int c8, const f4 (&acc)[2], float sum)
 {
-    const float f = sum == 0.f ? 0.f : 1.f / sum;
+    const float f = sum == 0.f ? 0.f : 1.f / __builtin_amdgcn_frexp_mantf(sum);
+    const int bits = -kSumBits - __builtin_amdgcn_frexp_expf(sum);
     const int t = (int)a.G.quotient((unsigned)p), h = (int)a.G.rest((unsigned)p, (unsigned)t);
     unsigned out[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float y0 = acc[i >> 1][2 * (i & 1)] * f, y1 = acc[i >> 1][2 * (i & 1) + 1] * f;
+        const float y0 = __builtin_ldexpf(acc[i >> 1][2 * (i & 1)] * f, bits), y1 = __builtin_ldexpf(acc[i >> 1][2 * (i & 1) + 1] * f, bits);
         out[i] = a.io_bf16 ? pack_bf16(y0, y1) : pack_f16(y0, y1);
     }
     *reinterpret_cast<uint4*>(a.o + ((size_t)(row0 + t) * a.Hq + hk * (int)a.G.d + h) * D + c8) = make_uint4(out[0], out[1], out[2], out[3]);
@@ -276,7 +283,7 @@ __device__ inline void store_row(const RowsArgs& a, int row0, int hk, int p, int
 // consecutive bytes of a key's value, and the 8 keys x D / 16 channels that it holds are turned while they are widened.
 //
 // The value's scale is not applied to values (there are 128 of them per key, and one P per row): it goes into the exponent.  With
-// t = score + log2(vscale), M a level near the running maximum of t and P = 2^(t - M): O = sum P y, and the sum of the softmax is sum P / vscale.
+// t = score + log2(vscale), M a level near the running maximum of t and P = 2^(t - M): O = sum P y, and the sum of the softmax is sum P / vscale (held times kSum).
 // P is at most 2^15, whatever the scales, and fp16 holds what matters of it.
 template <int D, int RB, bool E4M3, bool LISTED, bool FAR>
 __global__ __launch_bounds__(64 * kUnitsAtOnce, 2)
@@ -287,7 +294,7 @@ void pasa_cache_rows(RowsArgs a)
     constexpr int VW = CB / 4;                   // words of a key's value that a lane takes
     constexpr int ONCE = FAR ? 2 : 0;            // non-temporal
     constexpr bool QLDS = RB > 1;                // the query fragments wait in LDS: the registers are needed for RB blocks
-    // A wavefront's own part: while it sweeps, per key of the unit the score's factor, log2 of the value's scale and 1 / it, and the query fragments;
+    // A wavefront's own part: while it sweeps, per key of the unit the score's factor, log2 of the value's scale and kSum over it, and the query fragments;
     // afterwards its stored output.
     __shared__ __attribute__((aligned(16))) float lds_o[NW * ROWS * LD];
     static_assert(3 * kUnit * 4 + (QLDS ? RB * KS * 1024 : 0) <= ROWS * LD * 4, "what a wavefront keeps while it sweeps fits its part");
@@ -482,11 +489,11 @@ void pasa_cache_rows(RowsArgs a)
             do {
                 const bool whole = __builtin_amdgcn_ballot_w64(page_now >= 0 && pos_now + 16 <= new0) == ~0ull;      // all rows see all keys of the unit
                 const bool vs_one = vs_raw == 1.f;
-                // per key: what its score is multiplied by, and the value's scale; in the lanes' order of keys
+                // per key: what its score is multiplied by, log2 of the value's scale and kSum over it; in the lanes' order of keys
                 key_f[lane] = ks_raw * a.scale2;
                 key_f[kUnit + lane] = __builtin_amdgcn_logf(vs_raw);
                 // finite, so that 0 times it is 0: a key that is not there may have any scale, and a NaN shows in the score of the rows that see it
-                key_f[2 * kUnit + lane] = __builtin_fminf(__builtin_fmaxf(__builtin_amdgcn_rcpf(vs_raw), 0.f), 3e38f);
+                key_f[2 * kUnit + lane] = kSum * __builtin_fminf(__builtin_fmaxf(__builtin_amdgcn_rcpf(vs_raw), 0.f), 3e38f);
                 __builtin_amdgcn_wave_barrier();                 // a wavefront's LDS accesses are done in order
                 asm volatile("" ::: "memory");
 
@@ -550,8 +557,8 @@ void pasa_cache_rows(RowsArgs a)
                                 any |= E4M3 ? y & 0x7f7f7f7fu : y ^ 0x80808080u;
                             }
                             const unsigned long long who = __builtin_amdgcn_ballot_w64(any != 0u);       // lanes 16 g .. 16 g + 15 have a key
-                            const bool zeros = ((unsigned)(who >> (16 * g)) & 0xffffu) == 0u && inv[blk][i] == 1.f;
-                            inv[blk][i] = zeros ? 0x1p60f : inv[blk][i];
+                            const bool zeros = ((unsigned)(who >> (16 * g)) & 0xffffu) == 0u && inv[blk][i] == kSum;
+                            inv[blk][i] = zeros ? kSum * 0x1p60f : inv[blk][i];
 #pragma unroll
                             for (int rb = 0; rb < RB; ++rb) S[rb][blk][i] = zeros ? S[rb][blk][i] - 60.f : S[rb][blk][i];
                         }
