@@ -70,12 +70,13 @@ __device__ inline Extent extent_of(const RowsArgs& a, const Sequence& s)
 
 // What a workgroup sweeps first: from `at` on, block of rows `pair` (of all heads) of sequence b, and how far from there on; b < 0: nothing.  Counted in
 // units, with `beside` for each block before its first one.
-// Then, in groups of `group` wavefronts, whole blocks of rows of short sequences: `shorts` of them in all, of which the first ones go to workgroup `used`.
+// Then, in groups of `group` wavefronts, whole blocks of rows of short sequences: `shorts` of them in all, dealt to the workgroups in turn (none where
+// there are no more blocks than workgroups).
 struct Start {
     int b, at, beside;
     unsigned pair, left, per;
     Sequence s;
-    unsigned shorts, used;
+    unsigned shorts;
     int longest_short, group;
 };
 
@@ -120,7 +121,7 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
     auto start_at = [&](int b, const Sequence& s, unsigned rest, unsigned line, unsigned per, bool ranges) {
         const Extent x = extent_of<ROWS>(a, s);
         const unsigned of_pair = ranges ? ranges_of((unsigned)x.units, per) : (unsigned)x.units + beside;
-        Start st = {b, 0, ranges ? 0 : (int)beside, rest / of_pair, 0, per, s, 0, 0, 0, 1};
+        Start st = {b, 0, ranges ? 0 : (int)beside, rest / of_pair, 0, per, s, 0, 0, 1};
         st.at = (int)((rest - st.pair * of_pair) * (ranges ? per : 1u));
         st.left = ranges ? (unsigned)(x.units - st.at) : line - w * per;
         if (st.left > per) st.left = per;
@@ -220,7 +221,7 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
     }
     const unsigned want = ranges ? w : w * per, before = upto[0] - mine;
     const bool here = want >= before && want < upto[0];
-    Start st = {-1, 0, 0, 0, 0, per, {0, 0, 0}, 0, 0, 0, 1};
+    Start st = {-1, 0, 0, 0, 0, per, {0, 0, 0}, 0, 0, 1};
     if (__builtin_expect(one_wave, 1)) {
         const unsigned long long who = __builtin_amdgcn_ballot_w64(here);
         if (who != 0ull) {
@@ -236,7 +237,6 @@ __device__ inline Start find_start(const RowsArgs& a, unsigned w, unsigned grid,
         st = found;
     }
     st.shorts = all[1];
-    st.used = ranges ? line : 0;
     st.longest_short = (int)longest_short;
     st.group = (int)group;
     while (st.group < NW && (int)st.shorts * 2 * st.group <= (int)(NW * grid)) st.group *= 2;        // fewer shorts than blocks
@@ -312,16 +312,16 @@ void pasa_cache_rows(RowsArgs a)
     Start at = find_start<ROWS, NT>(a, w, grid, most, known);
     // the same in all lanes, which the compiler does not see on all ways to here: the buffers' descriptions would be taken lane by lane
     auto uniform = [](auto& v) { v = (std::remove_reference_t<decltype(v)>)__builtin_amdgcn_readfirstlane((int)v); };
-    uniform(at.b), uniform(at.per), uniform(at.beside), uniform(at.at), uniform(at.shorts), uniform(at.used), uniform(at.longest_short), uniform(at.group);
+    uniform(at.b), uniform(at.per), uniform(at.beside), uniform(at.at), uniform(at.shorts), uniform(at.longest_short), uniform(at.group);
     unsigned left = at.left, pair = at.pair;     // units of this workgroup still to be swept
     int b = at.b, pos = at.at, beside = at.beside;
     Sequence s = at.s;
     Extent x = extent_of<ROWS>(a, s);
     bool first_piece = true;
-    // Shorts: neighbours go to different workgroups, the first ones to those without a range.  False where the workgroup has no more; a group
+    // Shorts: neighbours go to different workgroups.  False where the workgroup has no more; a group
     // for which there is none while the first one still has one goes along with no rows and no keys.
     int group = NW, lead = wave;                 // wavefronts that share a range or a short, and one's place among them
-    unsigned next_short = w >= at.used ? w - at.used : w + grid - at.used;
+    unsigned next_short = w;
     auto take_short = [&] {
         const unsigned groups = NW / (unsigned)at.group, first = next_short, mine = first + grid * ((unsigned)wave / (unsigned)at.group);
         group = at.group;
