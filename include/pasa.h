@@ -227,9 +227,9 @@ int pasa_shift_keys_direct(const void* k, void* kprime, void* k0, int B, int Hkv
  * (drafted tokens that were not accepted) is a smaller length at the next call; what was written behind it is overwritten.
  *
  * table, length and row_start are read on the device, so that a captured graph follows them; they are not checked by the host.
- * The kernels keep to the buffers whatever they hold: lengths are taken as at most table_width * page and at least 0, row_start as
- * between 0 and R; positions before 0 and pages outside the pool are not there (nothing is written to them, they read as zeros
- * and no row sees them).  row_start has to ascend. */
+ * row_start has to ascend.  The kernels keep to the buffers whatever else they hold: lengths are taken as at most table_width * page
+ * and at least 0, row_start as between 0 and R; positions before 0 and pages outside the pool are not there (nothing is written to
+ * them, they read as zeros and no row sees them). */
 typedef enum {
     PASA_CACHE_I8 = 0,    /* bytes hold value + 128, value = -127 .. 127; scale = largest magnitude / 127 */
     PASA_CACHE_E4M3 = 1   /* OCP 8-bit floats, 4 exponent bits; scale = largest magnitude / 448 */
@@ -255,13 +255,14 @@ typedef struct {
  * scale = fp32(largest magnitude / 127 or 448), 1 where that magnitude is below 2^-100, and codes the nearest of
  * value / scale (ties to even), exactly.  A token with a value that is not finite gets the scale NaN, and so does whoever sees it.
  * kmean != NULL: the means of the pages that are written to are made again, over all their tokens below length[b].
- * PASA_EINVAL also for R <= 0. */
+ * PASA_EINVAL also for R <= 0; PASA_EUNSUPPORTED also for 2^23 or more pages (of all heads) that may be written to. */
 int pasa_cache_write(const pasa_cache* cache, const void* k, const void* v, int R, long long row_stride, const int* row_start,
                      int io_dtype, void* stream);
 
 /* Positions first[b] .. first[b] + N - 1 of every sequence (first: DEVICE [S], NULL: zeros) as fp16 or bf16 in k, v:
  * [S, Hkv, N, d], 16-byte aligned, what pasa_prepare_kv takes with B = S: a long chunk of a prompt is attended to that way.  code * scale
- * + kshift, rounded to fp32 and then to the type.  Zeros where a sequence has no such position. */
+ * + kshift, rounded to fp32 and then to the type.  Zeros where a sequence has no such position.  PASA_EUNSUPPORTED also where the
+ * stretches of 64 tokens (of all sequences and heads) come to 2^24. */
 int pasa_cache_read(const pasa_cache* cache, void* k, void* v, const int* first, int N, int io_dtype, void* stream);
 
 /* For every sequence and KV head the pages that its rows' queries point at: the first `head` and the last `tail` pages always (the
@@ -270,7 +271,8 @@ int pasa_cache_read(const pasa_cache* cache, void* k, void* v, const int* first,
  * [S][Hkv][count], the places in the sequence's row of the table, ascending, -1 behind the last.  All pages where there are
  * no more than count; none for a sequence without rows.  One row per sequence (Nq = 1 of a decoding step) makes it a choice per
  * query; rows that are to have choices of their own go in as sequences of one row each.  `tail` should cover the pages that the rows themselves lie in.
- * workspace: DEVICE, 256-byte aligned, pasa_cache_choose_workspace() bytes.  PASA_EINVAL also for count < 1, head or tail < 0. */
+ * workspace: DEVICE, 256-byte aligned, pasa_cache_choose_workspace() bytes.  PASA_EINVAL also for count < 1, head or tail < 0;
+ * PASA_EUNSUPPORTED also where S * Hkv reaches 2^22, or, with count < table_width, S * Hkv * ceil(table_width / 64) 2^24. */
 size_t pasa_cache_choose_workspace(const pasa_cache* cache);
 int pasa_cache_choose(const pasa_cache* cache, const void* q, int R, long long row_stride, const int* row_start, int Hq, int* blocks,
                       int count, int head, int tail, int io_dtype, void* workspace, size_t workspace_bytes, void* stream);
@@ -287,7 +289,8 @@ int pasa_cache_choose(const pasa_cache* cache, const void* q, int R, long long r
  * as they are loaded.  A row that sees no key, or whose scores (times log2(e), in fp32) are all -inf, is zeros.
  * Meant for rows up to some hundred per sequence; more are correct, but long chunks are faster through pasa_cache_read.
  * workspace: DEVICE, 256-byte aligned, pasa_attn_cache_workspace() bytes; calls that share one must not overlap in time.
- * PASA_EUNSUPPORTED also where the keys of all row blocks come to 2^37 or more. */
+ * PASA_EUNSUPPORTED also where the rows' blocks of all heads, up to (R * Hq / Hkv / n + S) * Hkv with n = 16, or 32 where a sequence
+ * and KV head have more than 16 rows on average, times 40 more than a table's units of 64 keys come to 2^31. */
 size_t pasa_attn_cache_workspace(const pasa_cache* cache, int R, int Hq);
 int pasa_attn_cache(const pasa_cache* cache, const void* q, void* o, int R, long long row_stride, const int* row_start, int Hq,
                     float scale, const unsigned long long* tree, const int* blocks, int count, int io_dtype, void* workspace,

@@ -9,10 +9,12 @@
 namespace {
 
 constexpr long long kMaxTokens = 262144;         // of a sequence, as in the other entry points
-constexpr long long kMaxGrid = 0x7fffffff;       // workgroups of a launch
+constexpr long long kMaxGrid = 0x7fffffff;       // of what the kernels count in 31 bits
+constexpr long long kMaxThreads = 0xffffffff;    // of a launch: the hardware counts them in 32 bits
 constexpr int kComputeUnits = 256;               // MI355X
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+bool fits(long long workgroups, int threads) { return workgroups <= kMaxThreads / threads; }
 bool buffer(const void* p, uintptr_t a) { return p != nullptr && aligned(p, a); }
 
 int check_cache(const pasa_cache* c)
@@ -80,7 +82,8 @@ int pasa_cache_write(const pasa_cache* cache, const void* k, const void* v, int 
     st = check_rows(cache, k, R, row_stride, row_start, cache->Hkv, io_dtype);
     if (st != PASA_OK) return st;
     if (!buffer(v, 16)) return PASA_EINVAL;
-    if (((long long)R / cache->page + 2LL * cache->S) * cache->Hkv > kMaxGrid) return PASA_EUNSUPPORTED;
+    const long long most = (long long)R / cache->page + 2LL * cache->S;  // pages that are written to
+    if (!fits((most < R ? most : R) * cache->Hkv, 512)) return PASA_EUNSUPPORTED;
     return status(pasa_launch_cache_write(*cache, k, v, R, row_stride, row_start, io_dtype == PASA_IO_BF16, static_cast<hipStream_t>(stream)));
 }
 
@@ -90,7 +93,7 @@ int pasa_cache_read(const pasa_cache* cache, void* k, void* v, const int* first,
     if (st != PASA_OK) return st;
     if (!buffer(k, 16) || !buffer(v, 16) || k == v || !aligned(first, 4) || N <= 0) return PASA_EINVAL;
     if (io_dtype != PASA_IO_F16 && io_dtype != PASA_IO_BF16) return PASA_EINVAL;
-    if (N > kMaxTokens || (((long long)N + 63) / 64) * cache->S > kMaxGrid / cache->Hkv) return PASA_EUNSUPPORTED;
+    if (N > kMaxTokens || !fits((((long long)N + 63) / 64) * cache->S * cache->Hkv, kCacheThreads)) return PASA_EUNSUPPORTED;
     return status(pasa_launch_cache_read(*cache, k, v, first, N, io_dtype == PASA_IO_BF16, static_cast<hipStream_t>(stream)));
 }
 
@@ -104,7 +107,9 @@ int pasa_cache_choose(const pasa_cache* cache, const void* q, int R, long long r
     st = check_rows(cache, q, R, row_stride, row_start, Hq, io_dtype);
     if (st != PASA_OK) return st;
     if (Hq % cache->Hkv != 0 || cache->kmean == nullptr || !buffer(blocks, 4) || count < 1 || head < 0 || tail < 0) return PASA_EINVAL;
-    if (count > kMaxTokens || ((long long)cache->table_width + 63) / 64 * cache->S > kMaxGrid / cache->Hkv || (long long)R * (Hq / cache->Hkv) > kMaxGrid)
+    const long long lists = (long long)cache->S * cache->Hkv;
+    if (count > kMaxTokens || (long long)R * (Hq / cache->Hkv) > kMaxGrid || !fits(lists, 1024) ||
+        (cache->table_width > count && !fits(((long long)cache->table_width + 63) / 64 * lists, kCacheThreads)))
         return PASA_EUNSUPPORTED;
     st = check_workspace(workspace, workspace_bytes, choose_workspace_bytes(*cache));
     if (st != PASA_OK) return st;
