@@ -288,7 +288,8 @@ int pasa_cache_choose(const pasa_cache* cache, const void* q, int R, long long r
  * largest on; the scales of the values that a row sees are meant to lie within 2^80 of each other), bf16 queries are converted to fp16
  * as they are loaded.  A row that sees no key, or whose scores (times log2(e), in fp32) are all -inf, is zeros.
  * Meant for rows up to some hundred per sequence; more are correct, but long chunks are faster through pasa_cache_read.
- * workspace: DEVICE, 256-byte aligned, pasa_attn_cache_workspace() bytes; calls that share one must not overlap in time.
+ * workspace: DEVICE, 256-byte aligned, pasa_attn_cache_workspace() bytes (which are enough for fewer rows too); calls that share one
+ * must not overlap in time.
  * PASA_EUNSUPPORTED also where the rows' blocks of all heads, up to (R * Hq / Hkv / n + S) * Hkv with n = 16, or 32 where a sequence
  * and KV head have more than 16 rows on average, times 40 more than a table's units of 64 keys come to 2^31. */
 size_t pasa_attn_cache_workspace(const pasa_cache* cache, int R, int Hq);

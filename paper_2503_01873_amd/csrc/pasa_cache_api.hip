@@ -121,7 +121,15 @@ size_t pasa_attn_cache_workspace(const pasa_cache* cache, int R, int Hq)
 {
     CachePlan plan;
     if (check_cache(cache) != PASA_OK || R <= 0 || Hq <= 0 || Hq % cache->Hkv != 0 || !plan_of(*cache, R, Hq, 0, &plan)) return 0;
-    return attn_workspace_bytes(*cache, plan);
+    size_t bytes = attn_workspace_bytes(*cache, plan);
+    if (plan.row_blocks == 2) {                  // as many rows as go in blocks of 16: half the slot, but more workgroups where there are few
+        const int rows = (int)(16LL * cache->S / (Hq / cache->Hkv));
+        if (rows > 0 && plan_of(*cache, rows, Hq, 0, &plan)) {
+            const size_t fewer = attn_workspace_bytes(*cache, plan);
+            if (fewer > bytes) bytes = fewer;
+        }
+    }
+    return bytes;
 }
 
 int pasa_attn_cache(const pasa_cache* cache, const void* q, void* o, int R, long long row_stride, const int* row_start, int Hq, float scale,
