@@ -80,3 +80,53 @@ def test_scores_that_rise_and_scales_that_differ(rows, format):
         i, at = c["table"][1, n // page], n % page
         c["k"][i, :, at], c["kscale"][i, :, at] = code, (0.002 if format == "i8" else 0.0006) * (1 + n) / 8
     _check(c, q, [rows, rows], "bf16", scale=0.125)
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,rows", [(128, 1, 128, 1), (71, 1, 64, 3), (40, 2, 128, 2), (64, 64, 64, 1)])
+def test_many_heads(Hq, Hkv, d, rows):
+    """All query heads on one KV head, odd numbers of them, and none that share."""
+    g = np.random.default_rng([46, Hq])
+    lengths = [1100, 3, 200]
+    c = ch.filled(g, lengths, Hkv, d, 64, "e4m3", wild=True)
+    _check(c, _queries(g, 3 * rows, Hq, d, "f16", 1.5), [rows] * 3)
+
+
+def test_two_calls_at_once():
+    """Two streams that read one cache with workspaces of their own."""
+    import torch
+
+    import paper_2503_01873_amd as P
+    g = np.random.default_rng(47)
+    Hq, Hkv, d, S = 8, 2, 128, 3
+    c = ch.filled(g, [5000, 900, 2000], Hkv, d, 64, "i8")
+    gpu, calls = ch.OnGpu(c), []
+    for rows in (1, 6):
+        q = _queries(g, S * rows, Hq, d, "f16", 1.5)
+        tq, stride = ch.tensor(q, "f16")
+        need = P.pasa_attn_cache_workspace(gpu.cache, S * rows, Hq)
+        calls.append((q, rows, tq, stride, torch.full((S * rows, Hq, d), float("nan"), dtype=torch.float16, device="cuda:0"),
+                      torch.empty(need, dtype=torch.uint8, device="cuda:0"), ch.ints(ch.starts([rows] * S)), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for q, rows, tq, stride, o, ws, row_start, stream in calls:
+            P.pasa_attn_cache(gpu.cache, tq, o, S * rows, stride, row_start, Hq, 0.088, ws, ws.numel(), stream)
+    torch.cuda.synchronize()
+    for q, rows, _, _, o, *_ in calls:
+        cb.check(o.double().cpu().numpy(), cb.attend(c, q, ch.starts([rows] * S), float(np.float32(0.088)), "f16"))
+
+
+@pytest.mark.parametrize("format", ["i8", "e4m3"])
+@pytest.mark.parametrize("rows", [1, 9])
+@pytest.mark.parametrize("some", [0.02, 0.5, 0.98])
+def test_tokens_without_a_value(some, rows, format):
+    """Their weight counts, wherever they lie: alone in a unit of work, in the first, beside others."""
+    g = np.random.default_rng([48, rows, int(100 * some)])
+    Hq, Hkv, d, L, page = 4, 2, 64, 3000, 64
+    c = ch.empty(g, 2, Hkv, d, page, -(-L // page), format)
+    n = [L, 150]
+    c["length"][:] = n
+    k, v = g.standard_normal((sum(n), Hkv, d)), g.standard_normal((sum(n), Hkv, d)) * 2.0 ** g.integers(-8, 9, (sum(n), Hkv, 1))
+    v[g.random(sum(n)) < some] = 0.0
+    v[:130] = v[1024:1600] = 0.0
+    co.write(c, ch.rounded(k, "f16"), ch.rounded(v, "f16"), ch.starts(n))
+    _check(c, _queries(g, 2 * rows, Hq, d, "f16", 2.0), [rows, rows])
