@@ -211,7 +211,7 @@ int pasa_shift_keys_direct(const void* k, void* kprime, void* k0, int B, int Hkv
  * tokens each; table[b][i] is the page in the pool that holds the tokens i * page .. i * page + page - 1 of sequence b (sequences
  * may share pages that neither writes).  A token takes d bytes and a scale for its key and for its value, per KV head; what is
  * held stands for code * scale.  Scales belong to a token and head, so a token that enters changes nothing that is there.  (What is
- * brought into the buffers by other means than pasa_cache_write keeps its rules: scales above zero, no NaN among the codes.)
+ * brought into the buffers by other means than pasa_cache_write keeps its rules: scales 2^-109 at least, no NaN among the codes.)
  *
  * Eq. (9) of the paper: a vector taken from every key leaves softmax unchanged.  kshift is such a vector per KV head (the bias
  * of the key projection, or a mean over a prompt): it is taken off before keys are rounded to 8 bits, which then need not cover
@@ -285,7 +285,8 @@ int pasa_cache_choose(const pasa_cache* cache, const void* q, int R, long long r
  * blocks == NULL: all pages.  blocks: DEVICE [S][Hkv][count] as pasa_cache_choose leaves it: only keys of these pages, of those that
  * the row sees; ascending without repeats, -1 behind the last.
  * Scores, statistics and output are held in fp32, P times the value's scale is rounded to fp16 (all its bits from 2^-21 of the row's
- * largest on; the scales of the values that a row sees are meant to lie within 2^80 of each other), bf16 queries are converted to fp16
+ * largest on; the scales of the values that a row sees are meant to lie within 2^80 of each other, where a token whose value is all
+ * zeros and has the scale 1 counts as 2^-60), bf16 queries are converted to fp16
  * as they are loaded.  A row that sees no key, or whose scores (times log2(e), in fp32) are all -inf, is zeros.
  * Meant for rows up to some hundred per sequence; more are correct, but long chunks are faster through pasa_cache_read.
  * workspace: DEVICE, 256-byte aligned, pasa_attn_cache_workspace() bytes (which are enough for fewer rows too); calls that share one

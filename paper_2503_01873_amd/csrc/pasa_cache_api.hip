@@ -46,7 +46,8 @@ int check_workspace(const void* ws, size_t bytes, size_t need) { return buffer(w
 // Rows per workgroup: 16 where the rows of a KV head fill no more on average, 32 otherwise (16 sequences of 8192 keys, 28 heads on 4, four rows each, that is 28 rows: 39.5 us, in
 // blocks of 16, which read the keys twice, 45.2; 8 of 30000 keys, 8 KV heads, 20 rows: 103 / 153).  Workgroups: one to a compute unit (their eight
 // wavefronts take its registers), and no more than there are blocks of rows or leave each wavefront a unit.  Never cut: up to 1024 keys, where a merge costs
-// what it saves (us, never / cut: one sequence of 500 keys 10.6 / 12.4, of 1024 13.8 / 13.8, 64 of 1024 15.5 / 17.4; one of 2048 19.1 / 13.8).  False where
+// what it saves (us, never / cut: one sequence of 500 keys 10.6 / 12.4, of 1024 13.8 / 13.8, 64 of 1024 15.5 / 17.4; one of 2048 19.1 / 13.8).  All of it goes by what tables
+// hold, as lengths are on the device: 16 ragged sequences of up to 500 keys in tables of 262144 tokens 13.9 us, in tables that fit 10.5; of up to 4096, 19.9 and 19.1.  False where
 // the units, with what blocks cost beside them, do not fit 31 bits.
 bool plan_of(const pasa_cache& c, int R, int Hq, int count, CachePlan* plan)
 {
