@@ -1,0 +1,855 @@
+"""What a server does around attention over a paged cache: positions turned into keys and queries, a cache in 4 bits, and its pages shared,
+copied and packed.  Calls as a program makes them, with their plain forms.
+
+Kinds of work:
+
+  rotate   rotary positions of whole sequences, out of a joint projection into the layout of pasa_attn_fwd, or as gradients back (pasa_rotate)
+  place    rotary positions of a step's rows, where their sequences in the cache have come to (pasa_cache_rotate)
+  append   tokens of several sequences enter a cache in 4 bits (pasa_cache_write) and come back as attention will see them (pasa_cache_read)
+  attend   a few rows of every sequence against a cache in 4 bits: decoding steps, trees of drafted tokens (pasa_attn_cache)
+  beams    a step of a beam search: sequences go on as copies of others or end (pasa_cache_fork), and each gets a page of its own for its next
+           token (pasa_cache_room)
+  pack     the pages of a pool that others have left move together at its beginning (pasa_cache_compact)
+  move     pages of one pool to places in another (pasa_cache_copy)
+  turn     a decoding step of one layer: pages, positions, the token written, attention (pasa_cache_room, _rotate, _write, pasa_attn_cache)
+
+The head layouts are those of `workloads/` (28 query heads on 4 with d = 128, 8 heads with d = 128, 5 heads with d = 64) and generic ones.
+
+A cache in 4 bits: per token and KV head a scale; per 32 channels a factor of 1 .. 224; per channel a code of -7 .. 7.  A value is
+scale * factor * code.  With `top` the largest magnitude of the token: scale is the least number of 8 significant bits that is not below top / 1568
+(1 where top < 2^-100), a factor the nearest to the 32 channels' largest magnitude over 7 scale, 1 at least, a code the nearest to the value over scale * factor.
+Ties go to the even number.  A page of a head is its codes, two to a byte, the lower four bits first, held as code + 8, and behind them its factors.
+"""
+import math
+
+import torch
+
+own = False
+
+_SERVE = {"S": 1, "Hq": 28, "Hkv": 4, "d": 128, "L": 64, "rows": 1, "page": 64, "dtype": "f16", "ragged": True, "tree": False, "shift": False}
+_TURN = {"layout": "halves", "rot": 128, "base": 10000.0, "scaling": "plain", "factor": 1.0, "original": 0, "magnitude": 1.0}
+
+
+def _case(name, work, **kw):
+    return {"name": name, "work": work, **kw}
+
+
+def listed():
+    return [
+        # queries and keys of a decoding step of sixteen sequences: the smallest call, all latency
+        _case("place_step_b16", "place", **{**_SERVE, **_TURN, "S": 16, "L": 8192, "dtype": "bf16"}),
+        # drafted tokens of trees, rotary in neighbouring pairs of a part of the channels: positions are depths in the tree
+        _case("place_trees_b8", "place", **{**_SERVE, **_TURN, "S": 8, "L": 8192, "rows": 48, "tree": True, "layout": "pairs", "rot": 64}),
+        # two long prompts out of the joint projection, frequencies stretched for a context eight times as long as trained
+        _case("rotate_prompts_b2", "rotate", **{**_TURN, "B": 2, "N": 16384, "Hq": 28, "Hkv": 4, "d": 128, "dtype": "bf16", "joint": True, "row0": 0,
+                                                "packed": False, "back": False, "scaling": "ramp", "factor": 8.0, "original": 4096,
+                                                "magnitude": 1.2079441541679836}),
+        # gradients of the queries of a video's frames, an odd number of rows, a part of the channels
+        _case("rotate_back_d64", "rotate", **{**_TURN, "B": 14, "N": 2305, "Hq": 5, "Hkv": 0, "d": 64, "dtype": "f16", "joint": False, "row0": 0,
+                                              "packed": True, "back": True, "layout": "pairs", "rot": 32}),
+        # four prompts of ragged length, in the type models are stored in
+        _case("append4_prompts_bf16", "append", **{**_SERVE, "S": 4, "L": 8192, "rows": 8192, "page": 128, "dtype": "bf16", "shift": True}),
+        # a decoding step of one sequence of no round length
+        _case("step4_one_4999", "attend", **{**_SERVE, "L": 4999}),
+        # a decoding step of sixteen sequences of ragged length
+        _case("step4_b16_ragged", "attend", **{**_SERVE, "S": 16, "L": 32768, "shift": True}),
+        # a decoding step of the longest sequence that the library takes
+        _case("step4_long", "attend", **{**_SERVE, "L": 262144, "page": 128, "dtype": "bf16"}),
+        # trees of drafted tokens behind eight sequences
+        _case("tree4_b8", "attend", **{**_SERVE, "S": 8, "L": 8192, "rows": 48, "dtype": "bf16", "tree": True}),
+        # sixteen requests of four beams each: half of the beams go on twice, some requests are done
+        _case("beams_16x4", "beams", **{**_SERVE, "S": 64, "beam": 4, "L": 4097}),
+        # half of a pool's sequences are gone
+        _case("pack_half", "pack", **{**_SERVE, "S": 32, "L": 16384}),
+        # what a layer does in a decoding step
+        _case("turn4_b16", "turn", **{**_SERVE, **_TURN, "S": 16, "L": 16384, "dtype": "bf16"}),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _draw_turn(rng, d):
+    scaling = rng.choice(["plain", "plain", "linear", "base", "ramp", "waves"])
+    return {"layout": rng.choice(["halves", "pairs"]), "rot": rng.choice([d, d, d // 2, d // 4, 2 * rng.randint(1, d // 2)]),
+            "base": rng.choice([10000.0, 500000.0, 1e6]), "scaling": scaling, "factor": 1.0 if scaling == "plain" else rng.uniform(1.5, 32.0),
+            "original": rng.choice([2048, 4096, 8192]), "magnitude": rng.choice([1.0, 1.0, rng.uniform(0.5, 1.5)])}
+
+
+def draw(rng):
+    while True:
+        work = rng.choice(["rotate", "rotate", "place", "append", "attend", "attend", "attend", "beams", "pack", "move", "turn"])
+        Hq, Hkv, d = rng.choice([(28, 4, 128), (28, 4, 128), (32, 8, 128), (8, 8, 128), (12, 2, 128), (5, 5, 64), (16, 16, 64), (16, 2, 64)])
+        dtype = rng.choice(["f16", "bf16"])
+        if work == "rotate":
+            joint, back = rng.random() < 0.6, rng.random() < 0.4
+            B, N = rng.choice([1, 1, 2, 4, 14]), _log(rng, 1, 32768)
+            row0 = 0 if rng.random() < 0.5 else rng.randint(1, 262144 - N)
+            c = _case("", work, **_draw_turn(rng, d), B=B, N=N, Hq=Hq, Hkv=Hkv if joint else 0, d=d, dtype=dtype, joint=joint, row0=row0,
+                      packed=row0 == 0 and rng.random() < 0.4, back=back)
+            if B * N * (Hq + Hkv) * d > 2 * 16384 * 32 * 128:
+                continue
+        else:
+            S, L, rows = _log(rng, 1, 64), _log(rng, 16, 262144), 1
+            if work == "append":
+                rows = rng.choice([1, _log(rng, 2, L)])
+            elif work in ("place", "attend"):
+                rows = rng.choice([1, 1, min(L, _log(rng, 2, 64))])
+            c = _case("", work, S=S, Hq=Hq, Hkv=Hkv, d=d, L=L, rows=rows, page=rng.choice([16, 32, 64, 64, 128]), dtype=dtype,
+                      ragged=rng.random() < 0.6, tree=rows > 1 and work != "append" and rng.random() < 0.7, shift=rng.random() < 0.5)
+            if work in ("place", "turn"):
+                c.update(_draw_turn(rng, d))
+            if work == "beams":
+                c["beam"] = rng.choice([1, 2, 4, 5, 8])
+            # within what the largest listed ones hold and compute
+            held = S * L * Hkv * d * (2 if work in ("pack", "move") else 1)
+            if held > 16 * 32768 * 4 * 128 or _flops(c) > 5e10 or S * L * Hq * rows > (1 << 30 if work == "attend" else 1 << 62):
+                continue
+        del c["name"]
+        return c
+
+
+# ---- sizes ----
+
+def _lengths(c):
+    """Tokens of every sequence with the new ones, and new ones among them."""
+    if not c["ragged"]:
+        return [c["L"]] * c["S"], [c["rows"]] * c["S"]
+    part = [(0.618033988749895 * b) % 1.0 for b in range(c["S"])]
+    lengths = [c["L"] - int(p * c["L"]) for p in part]
+    if c["work"] == "beams":                                    # those of a request are as long as its first one
+        lengths = [lengths[b - b % c["beam"]] for b in range(c["S"])]
+    spread = [(0.414213562373095 * b) % 1.0 for b in range(c["S"])]
+    return lengths, [min(n, c["rows"] - int(p * c["rows"])) for n, p in zip(lengths, spread)]
+
+
+def _width(c):
+    return (c["L"] + c["page"]) // c["page"]                    # room for one token more
+
+
+def _token(c):
+    """Bytes of a token's key, or value, of one head without its scale."""
+    return c["d"] // 2 + c["d"] // 32
+
+
+def _sources(c):
+    """What every sequence goes on from: of a request's beams every other one, twice; every fifth request is done."""
+    out = []
+    for b in range(c["S"]):
+        request, i = divmod(b, c["beam"])
+        out.append(-1 if request % 5 == 4 else request * c["beam"] + min(i // 2 * 2, c["S"] - 1 - request * c["beam"]))
+    return out
+
+
+def _type(c):
+    return torch.float16 if c["dtype"] == "f16" else torch.bfloat16
+
+
+# ---- plain forms ----
+
+def _frequencies(c, dev):
+    """Radians a position of every pair of channels, in 64 bits."""
+    pairs = c["rot"] // 2
+    i = torch.arange(pairs, dtype=torch.float64, device=dev)
+    base = c["base"] * (c["factor"] ** (c["rot"] / (c["rot"] - 2.0)) if c["scaling"] == "base" and c["rot"] > 2 else 1.0)
+    f = base ** (-2.0 * i / c["rot"])
+    if c["scaling"] == "linear":
+        f = f / c["factor"]
+    elif c["scaling"] in ("ramp", "waves"):
+        turns = c["original"] * f / (2.0 * math.pi)             # over the length that was trained on
+        if c["scaling"] == "waves":                             # from 1 to 4 turns, by the turns
+            keep = ((turns - 1.0) / 3.0).clamp(0.0, 1.0)
+        else:                                                   # from the pair that turns 32 times to the one that turns once, by the pair's number
+            def pair(t):
+                return c["rot"] * math.log(c["original"] / (2.0 * math.pi * t)) / (2.0 * math.log(c["base"]))
+            first, last = max(math.floor(pair(32.0)), 0), min(math.ceil(pair(1.0)), c["rot"] - 1)
+            keep = 1.0 - ((i - first) / max(last - first, 0.001)).clamp(0.0, 1.0)
+        f = f / c["factor"] * (1.0 - keep) + f * keep
+    return f
+
+
+def _rotate(x, position, c, back=False):
+    """x [..., heads, d] turned by position [...]: angles in 64 bits, the rest in 32."""
+    angle = position.double()[..., None] * _frequencies(c, x.device)
+    cos, sin = (c["magnitude"] * angle.cos()).float()[..., None, :], (c["magnitude"] * angle.sin()).float()[..., None, :]
+    if back:
+        sin = -sin
+    x, rot = x.float(), c["rot"]
+    out = x.clone()
+    even, odd = (slice(0, rot // 2), slice(rot // 2, rot)) if c["layout"] == "halves" else (slice(0, rot, 2), slice(1, rot, 2))
+    a, b = x[..., even], x[..., odd]
+    out[..., even] = a * cos - b * sin
+    out[..., odd] = a * sin + b * cos
+    return out
+
+
+def _codes(x):
+    """x [..., d] in 32 bits as codes + 8 [..., d], factors [..., d / 32] and scales.  In 64 bits: ties."""
+    x = x.double()
+    top = x.abs().amax(-1)
+    want = top / torch.full_like(top, 1568.0)                   # a true quotient: with a number torch multiplies by its reciprocal
+    rest = 1 << 45                                              # 45 of the 52 bits are rounded up
+    scale = ((want.view(torch.int64) + (rest - 1)) & ~(rest - 1)).view(torch.float64)
+    scale = torch.where(top < 2.0 ** -100, torch.ones_like(scale), scale)
+    parts = x.unflatten(-1, (-1, 32))
+    factor = (parts.abs().amax(-1) / (7.0 * scale)[..., None]).round().clamp(min=1.0)
+    code = (parts / (scale[..., None] * factor)[..., None]).round().clamp(-7.0, 7.0)
+    return (code + 8.0).flatten(-2).to(torch.uint8), factor.to(torch.uint8), scale.float()
+
+
+def _split(pool, c):
+    """Codes [..., page, d] and factors [..., page, d / 32] of pages."""
+    page, d = c["page"], c["d"]
+    b = pool[..., :page * d // 2]
+    code = torch.stack([b & 15, b >> 4], -1).flatten(-2).unflatten(-1, (page, d))
+    return code, pool[..., page * d // 2:].unflatten(-1, (page, d // 32))
+
+
+def _join(code, factor):
+    """The other way: pages as they are held."""
+    b = code[..., 0::2] | (code[..., 1::2] << 4)
+    return torch.cat([b.flatten(-2), factor.flatten(-2)], -1)
+
+
+def _values(pool, scale, c):
+    """Values [..., page, d] of pages in 32 bits: factor * code is a whole number, so one rounding."""
+    code, factor = _split(pool, c)
+    return (code.float() - 8.0) * factor.float().repeat_interleave(32, -1) * scale[..., None]
+
+
+def _rows(s):
+    """Of every row: its sequence, its number among that sequence's new tokens, its position."""
+    start, length = s["row_start"].long(), s["length"].long()
+    row = torch.arange(s["R"], device=start.device)
+    b = torch.searchsorted(start, row, right=True) - 1
+    t = row - start[b]
+    return b, t, length[b] - (start[b + 1] - start[b]) + t
+
+
+def _depths(s):
+    """Positions of the rows of trees: behind the older tokens, as many as they see of the others."""
+    b, t, position = _rows(s)
+    sees = (s["tree"][:, None] >> torch.arange(64, device=b.device)) & 1
+    return position - t + sees.sum(1) - 1
+
+
+def _put(pool, at, code, factor, c):
+    """Tokens into pages, at (page, head, token) [n, Hkv] each."""
+    page, d = c["page"], c["d"]
+    i, h, t = at
+    flat = pool.view(-1)
+    begin = (i * c["Hkv"] + h) * (page * _token(c))
+    b = code[..., 0::2] | (code[..., 1::2] << 4)
+    flat[(begin + t * (d // 2))[..., None] + torch.arange(d // 2, device=flat.device)] = b
+    flat[(begin + page * d // 2 + t * (d // 32))[..., None] + torch.arange(d // 32, device=flat.device)] = factor
+
+
+def _plain_write(s, k_new, v_new):
+    c = s["c"]
+    b, t, pos = _rows(s)
+    heads = torch.arange(c["Hkv"], device=b.device)
+    page = s["table"].long()[b, pos // c["page"]]
+    at = (page[:, None].expand(-1, c["Hkv"]), heads.expand(b.numel(), -1), (pos % c["page"])[:, None].expand(-1, c["Hkv"]))
+    k = k_new.float()
+    if c["shift"]:
+        k = k - s["kshift"]
+    for pool, scales, x in (("k", "kscale", k), ("v", "vscale", v_new.float())):
+        code, factor, scale = _codes(x)
+        _put(s[pool], at, code, factor, c)
+        s[scales][at] = scale
+    if "kmean" in s:
+        # the mean keys of the pages that were written to; a sequence's places beyond its last such page stand for the last one again
+        start, length = s["row_start"].long(), s["length"].long()
+        first = (length - (start[1:] - start[:-1])) // c["page"]
+        place = first[:, None] + torch.arange(1 + (c["rows"] + c["page"] - 2) // c["page"], device=first.device)
+        place = torch.minimum(place, ((length - 1) // c["page"])[:, None])
+        page = s["table"].long().gather(1, place)
+        left = (length[:, None] - place * c["page"]).clamp(max=c["page"])
+        there = (torch.arange(c["page"], device=first.device) < left[..., None]).double()
+        x = _values(s["k"][page], s["kscale"][page], c).double()                    # [S, pages, Hkv, page, d]
+        s["kmean"][page] = ((x * there[:, :, None, :, None]).sum(3) / left[..., None, None]).float()
+
+
+def _plain_read(s):
+    c = s["c"]
+    pos = s["first"].long()[:, None] + torch.arange(c["rows"], device=s["k"].device)
+    there = pos < s["length"].long()[:, None]
+    place = torch.where(there, pos, torch.zeros_like(pos)) // c["page"]
+    # whole pages, and of them the tokens
+    low = s["first"].long() // c["page"]
+    wide = (low[:, None] + torch.arange(1 + (c["rows"] + c["page"] - 2) // c["page"], device=low.device)).clamp(max=s["table"].shape[1] - 1)
+    page = s["table"].long().gather(1, wide)
+    at = torch.where(there, (place - low[:, None]) * c["page"] + pos % c["page"], torch.zeros_like(pos))
+    out = []
+    for pool, scales in (("k", "kscale"), ("v", "vscale")):
+        x = _values(s[pool][page], s[scales][page], c).permute(0, 2, 1, 3, 4).flatten(2, 3)         # [S, Hkv, pages * page, d]
+        if pool == "k" and c["shift"]:
+            x = x + s["kshift"][:, None]
+        x = x.gather(2, at[:, None, :, None].expand(-1, c["Hkv"], -1, c["d"]))
+        out.append(torch.where(there[:, None, :, None], x, torch.zeros_like(x)).to(_type(c)))
+    return out
+
+
+def _plain_attend(s, q_rows):
+    c = s["c"]
+    dev, G, T = q_rows.device, c["Hq"] // c["Hkv"], c["rows"]
+    start, length = s["row_start"].long(), s["length"].long()
+    t = torch.arange(T, device=dev)
+    row = (start[:-1, None] + t).clamp(max=s["R"] - 1)
+    q = q_rows.float()[row].view(c["S"], T, c["Hkv"], G, c["d"]).permute(0, 2, 1, 3, 4).reshape(c["S"], c["Hkv"], T * G, c["d"])
+    places = (c["L"] + c["page"] - 1) // c["page"]
+    page = s["table"].long()[:, :places].clamp(min=0)
+    pos = torch.arange(places * c["page"], device=dev)
+    n = start[1:] - start[:-1]
+    new = (pos - (length - n)[:, None])[..., None]                                  # number among the new tokens, [S, keys, 1]
+    if c["tree"]:
+        sees = (new < 0) | ((s["tree"][row][:, None] >> new.clamp(0, 63)) & 1).bool()
+    else:
+        sees = new <= t
+    sees = (sees & (pos < length[:, None])[..., None]).repeat_interleave(G, 2)[:, None]             # [S, 1, keys, T * G]
+    k = _values(s["k"][page], s["kscale"][page], c).permute(0, 2, 1, 3, 4).flatten(2, 3)
+    score = (k @ q.transpose(2, 3).contiguous()) * s["scale"]
+    del k
+    score = torch.where(sees, score, torch.full_like(score, -math.inf))
+    top = score.amax(2, keepdim=True)
+    p = torch.exp(score - torch.where(top == -math.inf, torch.zeros_like(top), top))
+    v = _values(s["v"][page], s["vscale"][page], c).permute(0, 2, 1, 3, 4).flatten(2, 3)
+    out = (p.transpose(2, 3) @ v) / p.sum(2)[..., None].clamp(min=1e-30)            # [S, Hkv, T * G, d]
+    out = out.view(c["S"], c["Hkv"], T, G, c["d"]).permute(0, 2, 1, 3, 4).reshape(c["S"], T, c["Hq"], c["d"])
+    b, t, _ = _rows(s)
+    return out[b, t].to(_type(c))
+
+
+def _plain_fork(s):
+    c = s["c"]
+    table, length, refs, source = s["table"], s["length"], s["refs"], s["source"].long()
+    b = torch.arange(c["S"], device=source.device)
+    stays, ends = source == b, (source < 0) | (source >= c["S"])
+    rows, lengths = table[source.clamp(0, c["S"] - 1)], length[source.clamp(0, c["S"] - 1)]
+    there = torch.arange(table.shape[1], device=b.device) < ((lengths + c["page"] - 1) // c["page"])[:, None]
+    none = torch.full_like(rows, -1)
+    rows = torch.where(stays[:, None], table, torch.where(there & ~ends[:, None], rows, none))
+    ones = torch.ones(rows.numel(), dtype=torch.int32, device=b.device)
+    for entries, sign in ((table, -1), (rows, 1)):
+        held = (entries >= 0) & (entries < s["pages"])
+        refs.index_add_(0, entries.long().clamp(0, s["pages"] - 1).flatten(), sign * (ones * held.flatten()))
+    table.copy_(rows)
+    length.copy_(torch.where(ends, torch.zeros_like(lengths), lengths))
+
+
+def _plain_room(s):
+    c = s["c"]
+    table, refs, pages = s["table"], s["refs"], s["pages"]
+    n, length = (s["row_start"][1:] - s["row_start"][:-1]).long(), s["length"].long()
+    S, W = table.shape
+    place = torch.arange(W, device=n.device)
+    first = (length - n).clamp(min=0)
+    written = (n > 0)[:, None] & (place >= (first // c["page"])[:, None]) & (place * c["page"] < length[:, None])
+    entry = table.long()
+    held = written & (entry >= 0) & (entry < pages)
+    entry = torch.where(held, entry, torch.full_like(entry, pages))
+    b = torch.arange(S, device=n.device)[:, None].expand(S, W)
+    writers = torch.zeros(pages + 1, dtype=torch.int32, device=n.device).index_add_(0, entry.flatten(), held.flatten().int())
+    last = torch.full((pages + 1,), -1, dtype=torch.int64, device=n.device).scatter_reduce_(0, entry.flatten(), b.flatten(), "amax")
+    holds = torch.cat([refs, refs.new_zeros(1)])
+    keeps = held & (writers[entry] == holds[entry]) & (last[entry] == b)
+    need = written & ~keeps
+    free = torch.nonzero(refs == 0)[:, 0]
+    which = need.flatten().cumsum(0).view(S, W) - 1
+    lacks = need & (which >= free.numel())
+    fresh = torch.full_like(entry, -1)
+    at = need & ~lacks
+    fresh[at] = free[which[at]]
+    table.copy_(torch.where(need, fresh, table.long()).int())
+    gone = need & held
+    refs.index_add_(0, entry[gone], refs.new_full((int(gone.sum()),), -1))
+    refs[fresh[at]] = 1
+    s["lacking"].copy_(lacks.sum())
+    copied = at & held & (place * c["page"] < first[:, None])
+    _plain_copy(s, s, fresh[copied], entry[copied])
+
+
+def _plain_copy(to, of, to_pages, from_pages):
+    for name in ("k", "v", "kscale", "vscale") + (("kmean",) if "kmean" in of else ()):
+        to[name][to_pages] = of[name][from_pages]
+
+
+def _plain_pack(s):
+    table, refs = s["table"], s["refs"]
+    live = refs != 0
+    used = live.sum()
+    ids = torch.arange(s["pages"], device=refs.device)
+    to, of = torch.nonzero(~live & (ids < used))[:, 0], torch.nonzero(live & (ids >= used))[:, 0]
+    now = ids.clone()
+    now[of] = to
+    held = (table >= 0) & (table < s["pages"])
+    table.copy_(torch.where(held, now[table.long().clamp(0, s["pages"] - 1)].int(), table))
+    refs[to] = refs[of]
+    refs[of] = 0
+    s["used"].copy_(used)
+    _plain_copy(s, s, to, of)
+
+
+# ---- inputs ----
+
+def _inputs(c, seed):
+    dev = torch.device("cuda:0")
+    g = torch.Generator(device=dev)
+    g.manual_seed(1000003 * int(seed) + 31)
+    d = c["d"]
+
+    def normal(*shape):
+        return torch.randn(shape, generator=g, device=dev, dtype=torch.float32)
+
+    def whole(x, dtype=torch.int32):
+        return torch.tensor(x, device=dev, dtype=dtype)
+
+    if c["work"] == "rotate":
+        B, N, heads = c["B"], c["N"], c["Hq"] + 2 * c["Hkv"]
+        s = {"c": c}
+        if c["joint"]:
+            s["x"] = (2.0 * normal(B, N, heads, d)).to(_type(c))
+        else:
+            s["x"] = (2.0 * normal(B, heads, N, d)).to(_type(c))
+        s["position"] = c["row0"] + torch.arange(N, device=dev).expand(B, N)
+        if c["packed"]:                                         # texts one behind the other, each from 0 on
+            begin = torch.rand((B, N), generator=g, device=dev) < 4.0 / N
+            begin[:, 0] = True
+            at = torch.where(begin, torch.arange(N, device=dev), torch.zeros_like(s["position"])).cummax(1)[0]
+            s["position"] = torch.arange(N, device=dev) - at
+            s["positions"] = s["position"].int()
+        return s
+
+    S, Hq, Hkv, page, W = c["S"], c["Hq"], c["Hkv"], c["page"], _width(c)
+    lengths, new = _lengths(c)
+    R = sum(new)
+    places = [(n + page - 1) // page for n in lengths]
+    s = {"c": c, "R": R, "row_start": whole([0] + new).cumsum(0).to(torch.int32), "first": whole([n - m for n, m in zip(lengths, new)]),
+         "scale": float(torch.tensor(d ** -0.5, dtype=torch.float32))}
+
+    # which pages sequences hold, and how many hold each
+    pages = S * W + 3 if c["work"] != "pack" else 2 * sum(places) + 5
+    s["pages"] = pages
+    order = torch.randperm(pages, generator=g, device=dev).to(torch.int32)
+    own_place = torch.arange(W, device=dev)[None, :] < whole(places)[:, None]
+    begin = whole([0] + places).cumsum(0)[:-1]
+    if c["work"] == "pack":
+        table = order[(begin[:, None] + torch.arange(W, device=dev)).clamp(max=pages - 1)]
+    else:
+        table = order[:S * W].view(S, W).clone()
+        if c["work"] == "beams":                                # a request's beams have three quarters of their pages in common
+            shared = torch.arange(W, device=dev)[None, :] < whole([3 * n // page // 4 for n in lengths])[:, None]
+            b = torch.arange(S, device=dev)
+            table = torch.where(shared, table[b - b % c["beam"]], table)
+    if c["work"] in ("beams", "pack", "turn"):
+        table = torch.where(own_place, table, torch.full_like(table, -1))
+        refs = torch.zeros(pages, dtype=torch.int32, device=dev)
+        refs.index_add_(0, table[own_place].long(), torch.ones(sum(places), dtype=torch.int32, device=dev))
+        # what is known of the pages, in one piece: holders, tables, lengths
+        padded = (pages + 3) // 4 * 4
+        s["book"] = torch.zeros(padded + S * W + S, dtype=torch.int32, device=dev)
+        s["refs"], s["table"], s["length"] = s["book"][:pages], s["book"][padded:padded + S * W].view(S, W), s["book"][padded + S * W:]
+        s["refs"].copy_(refs)
+        s["table"].copy_(table)
+        s["length"].copy_(whole(lengths))
+        s["book0"] = s["book"].clone()
+        s["lacking"], s["used"] = torch.zeros(1, dtype=torch.int32, device=dev), torch.zeros(1, dtype=torch.int32, device=dev)
+    else:
+        s["table"], s["length"] = table, whole(lengths)
+    if c["work"] == "beams":
+        s["source"] = whole(_sources(c))
+        s["goes_on"] = (s["source"] >= 0).int()
+        s["row_start"] = torch.cat([s["goes_on"].new_zeros(1), s["goes_on"].cumsum(0).int()])
+        s["R"] = max(1, sum(x >= 0 for x in _sources(c)))
+    if c["work"] == "move":
+        n = S * W // 2 + 1
+        s["from_pages"] = order[:n].clone()
+        s["to_pages"] = torch.randperm(pages + 8, generator=g, device=dev)[:n].to(torch.int32)
+        s["n"] = n
+
+    # keys have a bias of their own in every channel, four channels a large one; the cache may take it off
+    bias = normal(Hkv, d)
+    bias[:, torch.randperm(d, generator=g, device=dev)[:4]] += 60.0
+    s["kshift"] = bias
+    if c["work"] != "place":
+        mean = torch.empty((pages, Hkv, d), device=dev)
+        for name in ("k", "v"):
+            pool = torch.empty((pages, Hkv, page * _token(c)), dtype=torch.uint8, device=dev)
+            scales = torch.empty((pages, Hkv, page), device=dev)
+            for p in range(0, pages, 2048):
+                x = normal(min(2048, pages - p), Hkv, page, d)
+                if name == "k" and not c["shift"]:
+                    x += 0.1 * bias[:, None]
+                code, factor, scales[p:p + 2048] = _codes(x)
+                pool[p:p + 2048] = _join(code, factor)
+                if name == "k":
+                    mean[p:p + 2048] = x.mean(2)
+            s[name], s[name + "scale"] = pool, scales
+        if c["work"] in ("append", "pack", "move"):
+            s["kmean"] = mean
+    if c["work"] in ("place", "append", "turn", "attend"):
+        # a joint projection's rows: queries, keys and values side by side
+        q, k, v = 2.0 * normal(R, Hq, d), normal(R, Hkv, d) + (bias if c["work"] == "append" else 0.1 * bias), normal(R, Hkv, d)
+        s["qkv"] = torch.cat([q, k, v], 1).to(_type(c))
+    if c["tree"]:
+        # every drafted token has a parent among those before it, and sees its ancestors
+        b, t, _ = _rows(s)
+        parent = (torch.rand(R, generator=g, device=dev) * t).long()
+        base = s["row_start"].long()[b]
+        see = torch.ones(R, dtype=torch.int64, device=dev) << t
+        for depth in range(6):                                  # ancestors up to 64 steps away, doubling
+            see = torch.where(t > 0, see | see[base + parent], see)
+            parent = parent[base + parent]
+        s["tree"] = see
+    return s
+
+
+def prepare(c, seed):
+    s = _inputs(c, seed)
+    dev = torch.device("cuda:0")
+    work = c["work"]
+    # what a program keeps from step to step: where results go, the frequencies, the cache's description, workspaces
+    if work == "rotate":
+        s["y"] = [torch.empty((c["B"], h, c["N"], c["d"]), dtype=_type(c), device=dev) for h in (c["Hq"], c["Hkv"]) if h]
+    elif work in ("place", "turn"):
+        s["turned"] = torch.zeros_like(s["qkv"])
+    if work == "append":
+        s["k_out"] = torch.empty((c["S"], c["Hkv"], c["rows"], c["d"]), dtype=_type(c), device=dev)
+        s["v_out"] = torch.empty_like(s["k_out"])
+    if work in ("attend", "turn"):
+        s["o"] = torch.empty((s["R"], c["Hq"], c["d"]), dtype=_type(c), device=dev)
+    if work == "move":
+        s["there"] = {n: torch.zeros((s["pages"] + 8,) + s[n].shape[1:], dtype=s[n].dtype, device=dev) for n in ("k", "v", "kscale", "vscale", "kmean")}
+    if own:
+        import paper_2503_01873_amd as P
+        s["io"] = P.IO_F16 if c["dtype"] == "f16" else P.IO_BF16
+        if "rot" in c:
+            s["rotary"] = P.pasa_rotary()
+            P.pasa_rotary_set(s["rotary"], P.ROTARY_HALVES if c["layout"] == "halves" else P.ROTARY_PAIRS, c["rot"], c["base"],
+                              scaling={"plain": P.ROTARY_PLAIN, "linear": P.ROTARY_LINEAR, "base": P.ROTARY_BASE, "ramp": P.ROTARY_RAMP,
+                                       "waves": P.ROTARY_WAVES}[c["scaling"]],
+                              factor=c["factor"], original=c["original"], slow=1.0, fast=4.0 if c["scaling"] == "waves" else 32.0, magnitude=c["magnitude"])
+        if work != "rotate":
+            def described(t, pages):
+                return P.pasa_cache(t["k"], t["v"], t["kscale"], t["vscale"], s["table"], s["length"], S=c["S"], Hkv=c["Hkv"], d=c["d"],
+                                    page=c["page"], pages=pages, table_width=s["table"].shape[1], format=P.CACHE_I4, kmean=t.get("kmean"),
+                                    kshift=s["kshift"] if c["shift"] else None)
+            if work == "place":                                 # positions come from lengths alone: any buffers
+                s.update({n: torch.empty(64, dtype=torch.uint8, device=dev) for n in ("k", "v", "kscale", "vscale")})
+            s["cache"] = described(s, s["pages"])
+            if work == "move":
+                s["other"] = described(s["there"], s["pages"] + 8)
+            need = {"attn": P.pasa_attn_cache_workspace(s["cache"], s["R"], c["Hq"]), "fork": P.pasa_cache_fork_workspace(s["cache"]),
+                    "room": P.pasa_cache_room_workspace(s["cache"], s["R"]), "compact": P.pasa_cache_compact_workspace(s["cache"])}
+            for name, size in need.items():
+                s[name + "_bytes"], s[name + "_ws"] = size, torch.empty(max(size, 1), dtype=torch.uint8, device=dev)
+    return s
+
+
+def _run_plain(s):
+    c = s["c"]
+    work, Hq, Hkv = c["work"], c["Hq"], c["Hkv"]
+    if work == "rotate":
+        if not c["joint"]:
+            return [_rotate(s["x"].transpose(1, 2), s["position"], c, c["back"]).transpose(1, 2).to(_type(c)).contiguous()]
+        return [_rotate(x, s["position"], c, c["back"]).transpose(1, 2).to(_type(c)).contiguous()
+                for x in (s["x"][:, :, :Hq], s["x"][:, :, Hq:Hq + Hkv])]
+    if work in ("place", "turn"):
+        if work == "turn":
+            _plain_room(s)
+        position = _depths(s) if c["tree"] else _rows(s)[2]
+        s["turned"][:, :Hq + Hkv] = _rotate(s["qkv"][:, :Hq + Hkv], position, c).to(_type(c))
+        if work == "place":
+            return s["turned"]
+        _plain_write(s, s["turned"][:, Hq:Hq + Hkv], s["qkv"][:, Hq + Hkv:])
+        return [_plain_attend(s, s["turned"][:, :Hq]), s["book"]]
+    if work == "append":
+        _plain_write(s, s["qkv"][:, Hq:Hq + Hkv], s["qkv"][:, Hq + Hkv:])
+        return _plain_read(s) + [s["kmean"]]
+    if work == "attend":
+        return _plain_attend(s, s["qkv"][:, :Hq])
+    if work == "move":
+        _plain_copy(s["there"], s, s["to_pages"].long(), s["from_pages"].long())
+        return [s["there"][n] for n in ("k", "v", "kscale", "vscale", "kmean")]
+    s["book"].copy_(s["book0"])                                 # the same step again
+    if work == "beams":
+        _plain_fork(s)
+        s["length"].add_(s["goes_on"])
+        _plain_room(s)
+        return [s["book"], s["lacking"], s["k"], s["v"], s["kscale"], s["vscale"]]
+    _plain_pack(s)
+    return [s["book"], s["used"], s["k"], s["v"], s["kscale"], s["vscale"], s["kmean"]]
+
+
+def run(s):
+    if not own:
+        return _run_plain(s)
+    import paper_2503_01873_amd as P
+    c, stream = s["c"], torch.cuda.current_stream()
+    work, Hq, Hkv, d = c["work"], c["Hq"], c["Hkv"], c["d"]
+    if work == "rotate":
+        first = 0
+        for y in s["y"]:
+            heads = y.shape[1]
+            x = s["x"][:, :, first:first + heads] if c["joint"] else s["x"]
+            strides = (x.stride(0), x.stride(2), x.stride(1)) if c["joint"] else None
+            P.pasa_rotate(s["rotary"], x, y, c["B"], heads, c["N"], d, stream, x_strides=strides, positions=s.get("positions"), row0=c["row0"],
+                          transposed=c["back"], io_dtype=s["io"])
+            first += heads
+        return s["y"]
+    qkv, stride = s.get("qkv"), (Hq + 2 * Hkv) * d
+    if work == "turn":
+        P.pasa_cache_room(s["cache"], s["refs"], s["R"], s["row_start"], s["lacking"], s["room_ws"], s["room_bytes"], stream)
+    if work in ("place", "turn"):
+        P.pasa_cache_rotate(s["cache"], s["rotary"], qkv, s["turned"], Hq + Hkv, s["R"], stride, stride, s["row_start"], stream, tree=s.get("tree"),
+                            io_dtype=s["io"])
+        if work == "place":
+            return s["turned"]
+    if work in ("append", "turn"):
+        P.pasa_cache_write(s["cache"], (qkv if work == "append" else s["turned"])[:, Hq:], qkv[:, Hq + Hkv:], s["R"], stride, s["row_start"], stream,
+                           io_dtype=s["io"])
+        if work == "append":
+            P.pasa_cache_read(s["cache"], s["k_out"], s["v_out"], s["first"], c["rows"], stream, io_dtype=s["io"])
+            return [s["k_out"], s["v_out"], s["kmean"]]
+    if work in ("attend", "turn"):
+        P.pasa_attn_cache(s["cache"], qkv if work == "attend" else s["turned"], s["o"], s["R"], stride, s["row_start"], Hq, s["scale"], s["attn_ws"],
+                          s["attn_bytes"], stream, tree=s.get("tree"), io_dtype=s["io"])
+        return s["o"] if work == "attend" else [s["o"], s["book"]]
+    if work == "move":
+        P.pasa_cache_copy(s["other"], s["cache"], s["to_pages"], s["from_pages"], s["n"], stream)
+        return [s["there"][n] for n in ("k", "v", "kscale", "vscale", "kmean")]
+    s["book"].copy_(s["book0"])
+    if work == "beams":
+        P.pasa_cache_fork(s["cache"], s["refs"], s["source"], s["fork_ws"], s["fork_bytes"], stream)
+        s["length"].add_(s["goes_on"])
+        P.pasa_cache_room(s["cache"], s["refs"], s["R"], s["row_start"], s["lacking"], s["room_ws"], s["room_bytes"], stream)
+        return [s["book"], s["lacking"], s["k"], s["v"], s["kscale"], s["vscale"]]
+    P.pasa_cache_compact(s["cache"], s["refs"], s["used"], s["compact_ws"], s["compact_bytes"], stream)
+    return [s["book"], s["used"], s["k"], s["v"], s["kscale"], s["vscale"], s["kmean"]]
+
+
+# ---- what a pass cannot do without ----
+
+def _flops(c):
+    if c["work"] not in ("attend", "turn"):
+        return 0.0
+    lengths, new = _lengths(c)
+    return sum(4.0 * c["d"] * c["Hq"] * m * n for m, n in zip(new, lengths))
+
+
+def work(c):
+    if c["work"] == "rotate":
+        return {"bytes": 4 * c["B"] * c["N"] * (c["Hq"] + c["Hkv"]) * c["d"], "flops": 3.0 * c["B"] * c["N"] * (c["Hq"] + c["Hkv"]) * c["rot"]}
+    lengths, new = _lengths(c)
+    S, Hq, Hkv, d, page, R = c["S"], c["Hq"], c["Hkv"], c["d"], c["page"], sum(new)
+    token = Hkv * 2 * (_token(c) + 4)                           # codes, factors and scales of a token's key and value
+    whole, entries = page * token, 4 * S * _width(c)
+    moved = 0
+    if c["work"] in ("place", "turn"):
+        moved += 4 * R * (Hq + Hkv) * d
+    if c["work"] in ("append", "turn"):
+        moved += R * (4 * Hkv * d + token)
+    if c["work"] == "append":
+        older = sum((n - m) % page for n, m in zip(lengths, new))
+        touched = sum((n - 1) // page - (n - m) // page + 1 for n, m in zip(lengths, new))
+        moved += older * Hkv * (_token(c) + 4) + touched * Hkv * 4 * d + 4 * S * c["rows"] * Hkv * d
+    if c["work"] in ("attend", "turn"):
+        moved += 4 * R * Hq * d + sum(lengths) * token
+    if c["work"] == "beams":
+        source = _sources(c)
+        last = {}                                               # sequences that go on within a page which others hold too
+        for b, x in enumerate(source):
+            if x >= 0 and lengths[x] % page != 0:
+                last[x] = last.get(x, 0) + 1
+        moved += 4 * entries + 2 * whole * sum(n - 1 for n in last.values())
+    if c["work"] in ("pack", "move"):
+        whole += Hkv * 4 * d                                    # its mean
+        if c["work"] == "move":
+            moved += 2 * whole * (S * _width(c) // 2 + 1)
+        else:                                                   # of the pages in use those that lie behind as many
+            used = sum((n + page - 1) // page for n in lengths)
+            moved += 2 * entries + int(2 * whole * used * (1.0 - used / (2.0 * used + 5)))
+    return {"bytes": moved, "flops": _flops(c)}
+
+
+# ---- the same in 64 bits, from the definitions ----
+
+def _exact_rotate(x, position, c, back=False):
+    """x [..., heads, d] by complex numbers."""
+    rot, base, factor = c["rot"], c["base"], c["factor"]
+    freq = []
+    for i in range(rot // 2):
+        f = math.exp(-2 * i / rot * math.log(base))
+        if c["scaling"] == "base" and rot > 2:
+            f = math.exp(-2 * i / rot * (math.log(base) + rot / (rot - 2) * math.log(factor)))
+        elif c["scaling"] == "linear":
+            f = f / factor
+        elif c["scaling"] == "waves":
+            turns = c["original"] * f / (2 * math.pi)
+            slower = min(1.0, max(0.0, (4 - turns) / 3))
+            f = slower * f / factor + (1 - slower) * f
+        elif c["scaling"] == "ramp":
+            first, last = (rot / 2 * math.log(c["original"] / (2 * math.pi * t)) / math.log(base) for t in (32, 1))
+            first, last = max(0, math.floor(first)), min(rot - 1, math.ceil(last))
+            slower = min(1.0, max(0.0, (i - first) / max(0.001, last - first)))
+            f = slower * f / factor + (1 - slower) * f
+        freq.append(f)
+    angle = position.double()[..., None, None] * torch.tensor(freq, dtype=torch.float64, device=x.device)
+    turn = c["magnitude"] * torch.exp(torch.complex(torch.zeros_like(angle), -angle if back else angle))
+    x = x.double()
+    if c["layout"] == "halves":
+        z = turn * torch.complex(x[..., :rot // 2].contiguous(), x[..., rot // 2:rot].contiguous())
+        return torch.cat([z.real, z.imag, x[..., rot:]], -1)
+    z = turn * torch.view_as_complex(x[..., :rot].reshape(*x.shape[:-1], rot // 2, 2))
+    return torch.cat([torch.view_as_real(z).flatten(-2), x[..., rot:]], -1)
+
+
+def _exact_codes(x):
+    """The values that x [n, d] is held as."""
+    top = x.abs().max(1, keepdim=True)[0]
+    want = top / torch.full_like(top, 1568)
+    powers = torch.tensor([2.0 ** e for e in range(-160, 160)], dtype=torch.float64, device=x.device)
+    step = powers[torch.searchsorted(powers, want, right=True).clamp(min=1) - 1] / 128                      # of numbers of 8 bits next to it
+    scale = torch.where(top < 2.0 ** -100, torch.ones_like(want), torch.ceil(want / step) * step)
+    held = torch.empty_like(x)
+    for j in range(0, x.shape[1], 32):
+        part = x[:, j:j + 32]
+        unit = scale * torch.round(part.abs().max(1, keepdim=True)[0] / (7 * scale)).clamp(min=1)
+        held[:, j:j + 32] = torch.round(part / unit).clamp(-7, 7) * unit
+    return held
+
+
+def _exact_old(s, which, b, h):
+    """What sequence b, head h of the cache holds, [tokens, d]."""
+    c = s["c"]
+    ids = s["table"][b].long()
+    ids = ids[ids >= 0]
+    raw = s[which][ids, h].long()
+    codes, factor = raw[:, :c["page"] * c["d"] // 2].reshape(-1, c["d"] // 2), raw[:, c["page"] * c["d"] // 2:].reshape(-1, c["d"] // 32)
+    x = torch.empty((codes.shape[0], c["d"]), dtype=torch.float64, device=raw.device)
+    x[:, 0::2], x[:, 1::2] = (codes % 16 - 8).double(), (codes // 16 - 8).double()
+    return x * factor.double().repeat_interleave(32, 1) * s[which + "scale"][ids, h].reshape(-1, 1).double()
+
+
+def _exact_pages(s):
+    """beams and pack: page by page, as their definitions read."""
+    c, dev = s["c"], s["book"].device
+    table, length, refs = s["table"].tolist(), s["length"].tolist(), s["refs"].tolist()
+    names = ("k", "v", "kscale", "vscale") + (("kmean",) if "kmean" in s else ())
+    pairs, lacking = [], 0
+    if c["work"] == "beams":
+        source, page, W = s["source"].tolist(), c["page"], len(table[0])
+        was, were = [list(row) for row in table], list(length)
+        for b, x in enumerate(source):
+            if x == b:
+                continue
+            for p in table[b]:
+                if p >= 0:
+                    refs[p] -= 1
+            n = were[x] if x >= 0 else 0
+            kept = (n + page - 1) // page
+            table[b] = (was[x][:kept] if x >= 0 else []) + [-1] * (W - kept)
+            length[b] = n
+            for p in table[b]:
+                if p >= 0:
+                    refs[p] += 1
+        free = [p for p, n in enumerate(refs) if n == 0]
+        for b, x in enumerate(source):
+            if x < 0:
+                continue
+            at = length[b] // page
+            old = table[b][at]
+            length[b] += 1
+            if old >= 0 and refs[old] == 1:
+                continue
+            if old >= 0:
+                refs[old] -= 1
+            if not free:
+                table[b][at], lacking = -1, lacking + 1
+                continue
+            table[b][at] = free.pop(0)
+            refs[table[b][at]] = 1
+            if old >= 0 and at * page < length[b] - 1:
+                pairs.append((table[b][at], old))
+        extra = lacking
+    else:
+        extra = used = sum(n != 0 for n in refs)
+        holes = [p for p in range(used) if refs[p] == 0]
+        pairs = list(zip(holes, [p for p in range(used, len(refs)) if refs[p] != 0]))
+        now = {old: to for to, old in pairs}
+        table = [[now.get(p, p) for p in row] for row in table]
+        for to, old in pairs:
+            refs[to], refs[old] = refs[old], 0
+    refs += [0] * ((len(refs) + 3) // 4 * 4 - len(refs))
+    book = torch.tensor(refs + [p for row in table for p in row] + length, device=dev)
+    after = []
+    for name in names:
+        x = s[name].clone()
+        for to, old in pairs:
+            x[to] = s[name][old]
+        after.append(x)
+    return [book, torch.tensor([extra], device=dev)] + after
+
+
+def exact(c, seed):
+    s = _inputs(c, seed)
+    work, Hq, Hkv, d = c["work"], c["Hq"], c["Hkv"], c["d"]
+    if work == "rotate":
+        if not c["joint"]:
+            return [_exact_rotate(s["x"].transpose(1, 2), s["position"], c, c["back"]).transpose(1, 2)]
+        return [_exact_rotate(x, s["position"], c, c["back"]).transpose(1, 2) for x in (s["x"][:, :, :Hq], s["x"][:, :, Hq:Hq + Hkv])]
+    if work in ("beams", "pack"):
+        return _exact_pages(s)
+    if work == "move":
+        out = []
+        for name in ("k", "v", "kscale", "vscale", "kmean"):
+            x = torch.zeros((s["pages"] + 8,) + s[name].shape[1:], dtype=s[name].dtype, device=s[name].device)
+            for to, old in zip(s["to_pages"].tolist(), s["from_pages"].tolist()):
+                x[to] = s[name][old]
+            out.append(x)
+        return out
+    dev = s["qkv"].device
+    lengths, new = _lengths(c)
+    S, page, G = c["S"], c["page"], Hq // Hkv
+    rows = s["qkv"].double()
+    if work in ("place", "turn"):
+        turned = torch.zeros_like(rows)
+        r0 = 0
+        for n, m in zip(lengths, new):
+            position = torch.arange(n - m, n, device=dev)
+            if c["tree"]:
+                position = torch.tensor([n - m + bin(x).count("1") - 1 for x in (y & (1 << 64) - 1 for y in s["tree"][r0:r0 + m].tolist())], device=dev)
+            turned[r0:r0 + m, :Hq + Hkv] = _exact_rotate(rows[r0:r0 + m, :Hq + Hkv], position, c)
+            r0 += m
+        if work == "place":
+            return turned
+        rows[:, :Hq + Hkv] = turned[:, :Hq + Hkv].to(_type(c)).double()             # in 16 bits from one call to the next
+    o = torch.zeros((s["R"], Hq, d), dtype=torch.float64, device=dev)
+    back = torch.zeros((2, S, Hkv, c["rows"], d), dtype=torch.float64, device=dev)
+    kmean = s["kmean"].double() if "kmean" in s else None
+    r0 = 0
+    for b in range(S):
+        n, m = lengths[b], new[b]
+        ids = s["table"][b].long()
+        for h in range(Hkv):
+            k, v = _exact_old(s, "k", b, h), _exact_old(s, "v", b, h)
+            if work in ("append", "turn"):
+                x = rows[r0:r0 + m, Hq + h] - (s["kshift"][h].double() if c["shift"] else 0.0)
+                k[n - m:n], v[n - m:n] = _exact_codes(x.float().double()), _exact_codes(rows[r0:r0 + m, Hq + Hkv + h])
+            if work == "append":
+                for p in range((n - m) // page, (n + page - 1) // page):
+                    kmean[ids[p], h] = k[p * page:min(n, (p + 1) * page)].mean(0)
+                back[0, b, h, :m] = k[n - m:n] + (s["kshift"][h].double() if c["shift"] else 0.0)
+                back[1, b, h, :m] = v[n - m:n]
+                continue
+            see = torch.arange(n, device=dev)[None, :] <= torch.arange(n - m, n, device=dev)[:, None]
+            if c["tree"]:
+                see[:, n - m:] = ((s["tree"][r0:r0 + m, None] >> torch.arange(m, device=dev)[None, :]) & 1).bool()
+            score = (rows[r0:r0 + m, h * G:(h + 1) * G].reshape(-1, d) @ k[:n].t().contiguous()).view(m, G, n) * s["scale"]
+            score = torch.softmax(score.masked_fill_(~see[:, None], -math.inf), 2)
+            o[r0:r0 + m, h * G:(h + 1) * G] = (score.view(-1, n) @ v[:n]).view(m, G, d)
+        r0 += m
+    if work == "append":
+        return [back[0], back[1], kmean]
+    return o if work == "attend" else [o, s["book"]]
