@@ -17,7 +17,7 @@ The head layouts are those of `workloads/` (28 query heads on 4 with d = 128, 8 
 
 A cache in 4 bits: per token and KV head a scale; per 32 channels a factor of 1 .. 224; per channel a code of -7 .. 7.  A value is
 scale * factor * code.  With `top` the largest magnitude of the token: scale is the least number of 8 significant bits that is not below top / 1568
-(1 where top < 2^-100), a factor the nearest to the 32 channels' largest magnitude over 7 scale, 1 at least, a code the nearest to the value over scale * factor.
+(1 where top < 2^-98), a factor the nearest to the 32 channels' largest magnitude over 7 scale, 1 at least, a code the nearest to the value over scale * factor.
 Ties go to the even number.  A page of a head is its codes, two to a byte, the lower four bits first, held as code + 8, and behind them its factors.
 """
 import math
@@ -191,7 +191,7 @@ def _codes(x):
     want = top / torch.full_like(top, 1568.0)                   # a true quotient: with a number torch multiplies by its reciprocal
     rest = 1 << 45                                              # 45 of the 52 bits are rounded up
     scale = ((want.view(torch.int64) + (rest - 1)) & ~(rest - 1)).view(torch.float64)
-    scale = torch.where(top < 2.0 ** -100, torch.ones_like(scale), scale)
+    scale = torch.where(top < 2.0 ** -98, torch.ones_like(scale), scale)
     parts = x.unflatten(-1, (-1, 32))
     factor = (parts.abs().amax(-1) / (7.0 * scale)[..., None]).round().clamp(min=1.0)
     code = (parts / (scale[..., None] * factor)[..., None]).round().clamp(-7.0, 7.0)
@@ -711,7 +711,7 @@ def _exact_codes(x):
     want = top / torch.full_like(top, 1568)
     powers = torch.tensor([2.0 ** e for e in range(-160, 160)], dtype=torch.float64, device=x.device)
     step = powers[torch.searchsorted(powers, want, right=True).clamp(min=1) - 1] / 128                      # of numbers of 8 bits next to it
-    scale = torch.where(top < 2.0 ** -100, torch.ones_like(want), torch.ceil(want / step) * step)
+    scale = torch.where(top < 2.0 ** -98, torch.ones_like(want), torch.ceil(want / step) * step)
     held = torch.empty_like(x)
     for j in range(0, x.shape[1], 32):
         part = x[:, j:j + 32]
