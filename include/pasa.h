@@ -232,11 +232,16 @@ int pasa_shift_keys_direct(const void* k, void* kprime, void* k0, int B, int Hkv
  * them, they read as zeros and no row sees them). */
 typedef enum {
     PASA_CACHE_I8 = 0,    /* bytes hold value + 128, value = -127 .. 127; scale = largest magnitude / 127 */
-    PASA_CACHE_E4M3 = 1   /* OCP 8-bit floats, 4 exponent bits; scale = largest magnitude / 448 */
+    PASA_CACHE_E4M3 = 1,  /* OCP 8-bit floats, 4 exponent bits; scale = largest magnitude / 448 */
+    PASA_CACHE_I4 = 4     /* 4 bits, code + 8 for a code of -7 .. 7, and a factor of 1 .. 224 for every 32 channels; a value is scale * factor *
+                             code.  scale is the least number of 8 significant bits that is not below the token's largest magnitude / 1568, a factor the
+                             nearest to the largest magnitude of its channels / (7 scale), at least 1, a code the nearest to the value / (scale * factor), within
+                             -7 .. 7; ties go to the even number.  scale 1 and factors 1 where all is below 2^-98.  A page of a KV head is page * d / 2 bytes of
+                             codes, channels 2 i and 2 i + 1 in the lower and upper half of a token's byte i, and behind them page * d / 32 factors. */
 } pasa_cache_format;
 
 typedef struct {
-    void* k;              /* DEVICE [pages][Hkv][page][d] bytes, 16-byte aligned, as v */
+    void* k;              /* DEVICE [pages][Hkv][page][d] bytes (PASA_CACHE_I4: [pages][Hkv][page * d * 17 / 32]), 16-byte aligned, as v */
     void* v;
     float* kscale;        /* DEVICE [pages][Hkv][page], 16-byte aligned, as vscale */
     float* vscale;

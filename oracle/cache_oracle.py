@@ -39,7 +39,8 @@ def encode(x, format):
 
 
 def values(codes, scale, format):
-    x = codes.astype(np.float64) - 128.0 if format == "i8" else E4M3[codes]
+    """format "i4": the codes times their factors, as cache4_oracle gives them."""
+    x = codes.astype(np.float64) - 128.0 if format == "i8" else codes.astype(np.float64) if format == "i4" else E4M3[codes]
     return x * scale.astype(np.float64)[..., None]
 
 

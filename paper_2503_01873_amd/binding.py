@@ -15,7 +15,7 @@ import os
 MIXED, STRICT16, NAIVE16, S16, DIRECT = 0, 1, 2, 3, 4
 SHIFT_MEAN, SHIFT_MATRIX, SHIFT_MATRIX_MFMA = 0, 1, 2
 IO_F16, IO_BF16 = 0, 1
-CACHE_I8, CACHE_E4M3 = 0, 1
+CACHE_I8, CACHE_E4M3, CACHE_I4 = 0, 1, 4
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.environ.get("PASA_LIB") or os.path.join(_PKG, "libpasa.so")

@@ -30,6 +30,24 @@ __device__ inline h2 widen2(unsigned w)
     }
 }
 
+// Eight codes of 4 bits -> (code - 8) * factor, exactly, as four pairs of fp16: elements i and i + 4.  A code put into bits 4 .. 7 of 64.0 adds itself; the products are whole
+// numbers of 11 bits, and so is 72 * factor over 8, so the multiply-add that takes the 8 off is exact.  1.4 instructions a value.
+__device__ inline h2 times72(h2 factor) { return factor * h2{(_Float16)-72, (_Float16)-72}; }
+template <int I>
+__device__ inline h2 widen4bit(unsigned w, h2 factor, h2 off)
+{
+    const unsigned x = I == 0 ? w << 4 : I == 1 ? w : I == 2 ? w >> 4 : w >> 8;
+    return __builtin_elementwise_fma(__builtin_bit_cast(h2, (x & 0x00f000f0u) | 0x54005400u), factor, off);
+}
+// Two bytes -> fp16: 1024 + byte, less 1024
+template <int I>
+__device__ inline h2 factors2(unsigned w)
+{
+    return __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w, I == 0 ? 0x04010400u : 0x04030402u)) - h2{(_Float16)1024, (_Float16)1024};
+}
+
+typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+
 struct RowsArgs {
     pasa_cache c;
     const unsigned short* q;
@@ -285,19 +303,26 @@ __device__ inline void store_row(const RowsArgs& a, int row0, int hk, int p, int
 // The value's scale is not applied to values (there are 128 of them per key, and one P per row): it goes into the exponent.  With
 // t = score + log2(vscale), M a level near the running maximum of t and P = 2^(t - M): O = sum P y, and the sum of the softmax is sum P / vscale (held times kSum).
 // P is at most 2^15, whatever the scales, and fp16 holds what matters of it.
-template <int D, int RB, bool E4M3, bool LISTED, bool FAR>
+//
+// In 4 bits a lane takes D / 4 consecutive channels of a key, a word to a k-step, and D / 16 of a value; the factors of a unit's keys go through LDS, as fp16, where
+// the lanes that widen find them.
+template <int D, int RB, int FORMAT, bool LISTED, bool FAR>
 __global__ __launch_bounds__(64 * kUnitsAtOnce, 2)
 void pasa_cache_rows(RowsArgs a)
 {
     constexpr int ROWS = 16 * RB, KS = D / 32, CB = D / 16, NW = kUnitsAtOnce, NT = 64 * NW;
+    constexpr bool E4M3 = FORMAT == PASA_CACHE_E4M3, I4 = FORMAT == PASA_CACHE_I4;
     constexpr int LD = D + 4;                    // LDS row of the merge, in floats
-    constexpr int VW = CB / 4;                   // words of a key's value that a lane takes
+    constexpr int VW = I4 ? 1 : CB / 4;          // words of a key's value that a lane takes; in 4 bits and d = 64 half a word
+    constexpr int RAW = I4 ? D / 2 : D;          // bytes of a key's codes
+    constexpr int GROUPS = D / kFactorChannels, KLD = kUnit + 16;    // factors of a key; LDS row of the keys' factors, so that the lanes' banks differ
     constexpr int ONCE = FAR ? 2 : 0;            // non-temporal
     constexpr bool QLDS = RB > 1;                // the query fragments wait in LDS: the registers are needed for RB blocks
     // A wavefront's own part: while it sweeps, per key of the unit the score's factor, log2 of the value's scale and kSum over it, and the query fragments;
     // afterwards its stored output.
     __shared__ __attribute__((aligned(16))) float lds_o[NW * ROWS * LD];
-    static_assert(3 * kUnit * 4 + (QLDS ? RB * KS * 1024 : 0) <= ROWS * LD * 4, "what a wavefront keeps while it sweeps fits its part");
+    constexpr int FACTORS = I4 ? GROUPS * (4 * KLD + 2 * kUnit) : 0;
+    static_assert(3 * kUnit * 4 + (QLDS ? RB * KS * 1024 : 0) + FACTORS <= ROWS * LD * 4, "what a wavefront keeps while it sweeps fits its part");
     __shared__ float lds_l[NW][ROWS], lds_m[NW][ROWS];
     __shared__ Known<NT> known;
 
@@ -308,6 +333,9 @@ void pasa_cache_rows(RowsArgs a)
     const unsigned grid = gridDim.x, w = logical_workgroup(blockIdx.x, grid);
     float* const key_f = lds_o + wave * ROWS * LD;
     h8* const lds_q = reinterpret_cast<h8*>(key_f + 3 * kUnit);
+    // in 4 bits: by group of channels and key, the key's factor twice, and the value's
+    h2* const lds_fk = reinterpret_cast<h2*>(lds_q + (QLDS ? RB * KS * 64 : 0));
+    _Float16* const lds_fv = reinterpret_cast<_Float16*>(lds_fk + GROUPS * KLD);
 
     Start at = find_start<ROWS, NT>(a, w, grid, most, known);
     // the same in all lanes, which the compiler does not see on all ways to here: the buffers' descriptions would be taken lane by lane
@@ -373,8 +401,8 @@ void pasa_cache_rows(RowsArgs a)
         auto row_of = [&](int rb) { return p0 + 16 * rb + lq < list ? p0 + 16 * rb + lq : list - 1; };
         auto query = [&](int p, int ks) {
             const int t = (int)a.G.quotient((unsigned)p), h = (int)a.G.rest((unsigned)p, (unsigned)t);
-            return *reinterpret_cast<const u16x8*>(a.q + (size_t)(s.row0 + t) * (size_t)a.row_stride + (size_t)(hk * G + h) * D + 16 * g +
-                                                   64 * (ks / 2) + 8 * (ks & 1));
+            return *reinterpret_cast<const u16x8*>(a.q + (size_t)(s.row0 + t) * (size_t)a.row_stride + (size_t)(hk * G + h) * D +
+                                                   (I4 ? D / 4 * g + 8 * ks : 16 * g + 64 * (ks / 2) + 8 * (ks & 1)));
         };
         if (units > 0) {
             // Places of the blocks of 16 keys, lane group g that of block g, by way of the list where there is one.  Three steps, each an
@@ -402,30 +430,53 @@ void pasa_cache_rows(RowsArgs a)
                 page_next = in ? entry_b : -1;
             };
 
-            uint4 K[4][D / 64];
+            uint4 K[4][I4 ? 1 : D / 64];
             unsigned V[2][8][VW];                // k-step of 32 keys, key, word
             float ks_raw, vs_raw;
-            const int koff = lq * D + 16 * g, voff = 4 * g * D + lq * CB;
+            unsigned kf_raw = 0, vf_raw = 0;     // factors
+            const int koff = lq * RAW + (I4 ? D / 8 : 16) * g, voff = 4 * g * RAW + lq * (I4 ? CB / 2 : CB);
             // A block that is not there reads nothing and comes as zeros: its buffer has no bytes.
             unsigned long long at_next = 0, at_now = 0;          // bytes from the first key (value) of the pool to the block's
             auto buffer_of = [&](void* base, int blk, unsigned long long offsets, int pages) {
                 const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)offsets, 16 * blk), hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(offsets >> 32), 16 * blk);
                 return __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(base) + ((unsigned long long)hi << 32 | lo), 0,
-                                                         __builtin_amdgcn_readlane(pages, 16 * blk) < 0 ? 0 : 16 * D, 0x00020000);
+                                                         __builtin_amdgcn_readlane(pages, 16 * blk) < 0 ? 0 : 16 * RAW, 0x00020000);
             };
             auto load_k = [&] {
                 const size_t slot = ((size_t)(unsigned)(page_next < 0 ? 0 : page_next) * (unsigned)a.c.Hkv + (unsigned)hk) * (unsigned)a.c.page +
                                     (unsigned)(pos_next & (a.c.page - 1));
-                at_next = slot * D;
+                size_t factors = 0;
+                if constexpr (I4) {
+                    const size_t first = ((size_t)(unsigned)(page_next < 0 ? 0 : page_next) * (unsigned)a.c.Hkv + (unsigned)hk) * (unsigned)(a.c.page * token_bytes4(D));
+                    const unsigned at_page = (unsigned)(pos_next & (a.c.page - 1));
+                    at_next = first + at_page * RAW;
+                    factors = first + (unsigned)(a.c.page * RAW) + (at_page + lq) * GROUPS;
+                } else {
+                    at_next = slot * D;
+                }
 #pragma unroll
                 for (int blk = 0; blk < 4; ++blk) {
                     const __amdgpu_buffer_rsrc_t from = buffer_of(a.c.k, blk, at_next, page_next);
+                    if constexpr (I4) {
+                        if constexpr (D == 128) {
+                            K[blk][0] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(from, koff, 0, ONCE));
+                        } else {
+                            const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(from, koff, 0, ONCE));
+                            K[blk][0].x = y.x, K[blk][0].y = y.y;
+                        }
+                        continue;
+                    }
 #pragma unroll
-                    for (int j = 0; j < D / 64; ++j) K[blk][j] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(from, koff + 64 * j, 0, ONCE));
+                    for (int j = 0; j < (I4 ? 1 : D / 64); ++j) K[blk][j] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(from, koff + 64 * j, 0, ONCE));
                 }
                 // a lane a key
                 ks_raw = a.c.kscale[slot + lq];
                 vs_raw = a.c.vscale[slot + lq];
+                if constexpr (I4) {
+                    using Factors = std::conditional_t<GROUPS == 4, unsigned, unsigned short>;
+                    kf_raw = *reinterpret_cast<const Factors*>(static_cast<const char*>(a.c.k) + factors);
+                    vf_raw = *reinterpret_cast<const Factors*>(static_cast<const char*>(a.c.v) + factors);
+                }
             };
             auto load_v = [&] {
 #pragma unroll
@@ -433,7 +484,11 @@ void pasa_cache_rows(RowsArgs a)
                     const __amdgpu_buffer_rsrc_t from = buffer_of(a.c.v, blk, at_now, page_now);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        if constexpr (VW == 2) {
+                        if constexpr (I4 && D == 64) {
+                            V[blk >> 1][4 * (blk & 1) + i][0] = __builtin_amdgcn_raw_buffer_load_b16(from, voff + i * RAW, 0, ONCE);
+                        } else if constexpr (I4) {
+                            V[blk >> 1][4 * (blk & 1) + i][0] = __builtin_amdgcn_raw_buffer_load_b32(from, voff + i * RAW, 0, ONCE);
+                        } else if constexpr (VW == 2) {
                             const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(from, voff + i * D, 0, ONCE));
                             V[blk >> 1][4 * (blk & 1) + i][0] = y.x;
                             V[blk >> 1][4 * (blk & 1) + i][VW - 1] = y.y;
@@ -477,6 +532,12 @@ void pasa_cache_rows(RowsArgs a)
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks) Qr[rb][ks] = bf16x8_to_h8(raw[rb][ks]);
             }
+            if constexpr (I4) {                  // in the order that a word of codes is widened in
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) Qr[rb][ks] = __builtin_shufflevector(Qr[rb][ks], Qr[rb][ks], 0, 4, 1, 5, 2, 6, 3, 7);
+            }
             if (QLDS) {
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb)
@@ -494,6 +555,16 @@ void pasa_cache_rows(RowsArgs a)
                 key_f[kUnit + lane] = __builtin_amdgcn_logf(vs_raw);
                 // finite, so that 0 times it is 0: a key that is not there may have any scale, and a NaN shows in the score of the rows that see it
                 key_f[2 * kUnit + lane] = kSum * __builtin_fminf(__builtin_fmaxf(__builtin_amdgcn_rcpf(vs_raw), 0.f), 3e38f);
+                if constexpr (I4) {
+#pragma unroll
+                    for (int i = 0; i < GROUPS; i += 2) {
+                        const h2 fk = i == 0 ? factors2<0>(kf_raw) : factors2<2>(kf_raw), fv = i == 0 ? factors2<0>(vf_raw) : factors2<2>(vf_raw);
+                        lds_fk[i * KLD + lane] = h2{fk[0], fk[0]};
+                        lds_fk[(i + 1) * KLD + lane] = h2{fk[1], fk[1]};
+                        lds_fv[i * kUnit + lane] = fv[0];
+                        lds_fv[(i + 1) * kUnit + lane] = fv[1];
+                    }
+                }
                 __builtin_amdgcn_wave_barrier();                 // a wavefront's LDS accesses are done in order
                 asm volatile("" ::: "memory");
 
@@ -508,6 +579,22 @@ void pasa_cache_rows(RowsArgs a)
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks) q[rb][ks] = Q(rb, ks);
                 if (QLDS) PASA_FENCE();          // all asked for before the first is used
+                if constexpr (I4) {
+#pragma unroll
+                    for (int blk = 0; blk < 4; ++blk) {
+                        const h2 factor = lds_fk[(GROUPS == 4 ? g : g >> 1) * KLD + 16 * blk + lq], off = times72(factor);
+#pragma unroll
+                        for (int ks = 0; ks < KS; ++ks) {
+                            const unsigned w = ks == 0 ? K[blk][0].x : ks == 1 ? K[blk][0].y : ks == 2 ? K[blk][0].z : K[blk][0].w;
+                            const h2 y[4] = {widen4bit<0>(w, factor, off), widen4bit<1>(w, factor, off), widen4bit<2>(w, factor, off), widen4bit<3>(w, factor, off)};
+                            h8 f;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) f[2 * e] = y[e][0], f[2 * e + 1] = y[e][1];
+#pragma unroll
+                            for (int rb = 0; rb < RB; ++rb) S[rb][blk] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, q[rb][ks], S[rb][blk], 0, 0, 0);
+                        }
+                    }
+                } else
 #pragma unroll
                 for (int j = 0; j < D / 64; ++j)
 #pragma unroll
@@ -554,7 +641,7 @@ void pasa_cache_rows(RowsArgs a)
 #pragma unroll
                             for (int d = 0; d < VW; ++d) {
                                 const unsigned y = V[blk >> 1][4 * (blk & 1) + i][d];
-                                any |= E4M3 ? y & 0x7f7f7f7fu : y ^ 0x80808080u;
+                                any |= E4M3 ? y & 0x7f7f7f7fu : y ^ (!I4 ? 0x80808080u : D == 128 ? 0x88888888u : 0x8888u);
                             }
                             const unsigned long long who = __builtin_amdgcn_ballot_w64(any != 0u);       // lanes 16 g .. 16 g + 15 have a key
                             const bool zeros = ((unsigned)(who >> (16 * g)) & 0xffffu) == 0u && inv[blk][i] == kSum;
@@ -616,6 +703,41 @@ void pasa_cache_rows(RowsArgs a)
                     }
                 }
                 PASA_FENCE();
+                if constexpr (I4) {
+#pragma unroll
+                    for (int st = 0; st < 2; ++st) {
+                        h2 factor[4], off[4];    // of pairs of keys
+#pragma unroll
+                        for (int e = 0; e < 4; e += 2) {
+                            const h4 four = *reinterpret_cast<const h4*>(lds_fv + lq / (16 / GROUPS) * kUnit + 32 * st + 8 * e + 4 * g);
+                            factor[e] = h2{four[0], four[1]}, factor[e + 1] = h2{four[2], four[3]};
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) off[e] = times72(factor[e]);
+#pragma unroll
+                        for (int half = 0; half < D / 64; ++half) {
+                            unsigned two[4];     // four channels of a pair of keys
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) two[e] = __builtin_amdgcn_perm(V[st][2 * e + 1][0], V[st][2 * e][0], half == 0 ? 0x05040100u : 0x07060302u);
+                            auto channel = [&](auto ch) {
+                                constexpr int I = decltype(ch)::value;
+                                h8 f;
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const h2 y = widen4bit<I>(two[e], factor[e], off[e]);
+                                    f[2 * e] = y[0];
+                                    f[2 * e + 1] = y[1];
+                                }
+#pragma unroll
+                                for (int rb = 0; rb < RB; ++rb) O[rb][4 * half + I] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, P[rb][st], O[rb][4 * half + I], 0, 0, 0);
+                            };
+                            channel(std::integral_constant<int, 0>{});
+                            channel(std::integral_constant<int, 1>{});
+                            channel(std::integral_constant<int, 2>{});
+                            channel(std::integral_constant<int, 3>{});
+                        }
+                    }
+                } else
 #pragma unroll
                 for (int st = 0; st < 2; ++st)
 #pragma unroll
@@ -887,17 +1009,22 @@ hipError_t pasa_launch_attn_cache(const pasa_cache& c, const void* q, void* o, i
         }
         return hipSuccess;
     };
-    const bool e = c.format == PASA_CACHE_E4M3, l = blocks != nullptr;
     auto of_kind = [&](auto d, auto rb, auto far) {
         constexpr int D = decltype(d)::value, RB = decltype(rb)::value;
         constexpr bool F = decltype(far)::value;
-        if (e) return l ? go(pasa_cache_rows<D, RB, true, true, F>, pasa_cache_merge<D, RB, false>, pasa_cache_merge<D, RB, true>) : go(pasa_cache_rows<D, RB, true, false, F>, pasa_cache_merge<D, RB, false>, pasa_cache_merge<D, RB, true>);
-        return l ? go(pasa_cache_rows<D, RB, false, true, F>, pasa_cache_merge<D, RB, false>, pasa_cache_merge<D, RB, true>) : go(pasa_cache_rows<D, RB, false, false, F>, pasa_cache_merge<D, RB, false>, pasa_cache_merge<D, RB, true>);
+        auto held_as = [&](auto format) {
+            constexpr int FORMAT = decltype(format)::value;
+            return blocks != nullptr ? go(pasa_cache_rows<D, RB, FORMAT, true, F>, pasa_cache_merge<D, RB, false>, pasa_cache_merge<D, RB, true>)
+                                     : go(pasa_cache_rows<D, RB, FORMAT, false, F>, pasa_cache_merge<D, RB, false>, pasa_cache_merge<D, RB, true>);
+        };
+        if (c.format == PASA_CACHE_I4) return held_as(std::integral_constant<int, PASA_CACHE_I4>{});
+        if (c.format == PASA_CACHE_E4M3) return held_as(std::integral_constant<int, PASA_CACHE_E4M3>{});
+        return held_as(std::integral_constant<int, PASA_CACHE_I8>{});
     };
     // Keys and values that are read once and may be more than the last cache's 256 MB are read past the caches.  us, past / through them: 277 MB
     // (262144 keys, 4 heads) 54.3 / 58.9, 305 MB 63.2 / 65.5; 68 MB, which a program that does little else finds there again, 28.0 / 24.4
     const long long held = (blocks != nullptr && count < c.table_width ? count : c.table_width);
-    const bool far = (double)held * c.page * c.S * c.Hkv * 2 * c.d > 256e6;
+    const bool far = (double)held * c.page * c.S * c.Hkv * 2 * cache_token_bytes(c) > 256e6;
     auto of_format = [&](auto d, auto rb) {
         if constexpr (decltype(rb)::value == 1) {
             if (far) return of_kind(d, rb, std::true_type{});

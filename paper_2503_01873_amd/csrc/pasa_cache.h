@@ -17,6 +17,11 @@ inline int log2_of(int page)
     return n;
 }
 
+// In 4 bits a page of a head is its codes, two to a byte, and behind them a factor per token and kFactorChannels channels.
+constexpr int kFactorChannels = 32;
+__host__ __device__ constexpr int token_bytes4(int d) { return d / 2 + d / kFactorChannels; }
+inline int cache_token_bytes(const pasa_cache& c) { return c.format == PASA_CACHE_I4 ? token_bytes4(c.d) : c.d; }      // of a key or value and head, without its scale
+
 // The kernels of attention over the cache: rows per workgroup are 16 * row_blocks, `grid` workgroups share the units of work; no block of rows
 // is shared by two of them (and nothing merged) where never_cut.
 struct CachePlan {

@@ -90,6 +90,56 @@ __device__ inline uint2 encode8(const float (&x)[8], float top, float& scale, fl
     return make_uint2(w[0], w[1]);
 }
 
+// The nearest whole number to x / unit, ties to even, where that is below 2^15 and unit has 16 significant bits: numbers times unit are exact in fp32, and so is what is left
+// of x.  inverse: of unit, off by a step or two.
+__device__ inline float nearest(float x, float unit, float inverse)
+{
+    float n = __builtin_rintf(x * inverse);
+    const float left = __builtin_fabsf(__builtin_fmaf(-n, unit, x)), half = 0.5f * unit;
+    const bool odd = ((int)n & 1) != 0;
+    if (left > half || (left == half && odd)) n += __builtin_copysignf(1.f, __builtin_fmaf(-n, unit, x));
+    return n;
+}
+
+// Eight values of a token -> eight codes of 4 bits, and the numbers factor * code that they hold.  top: the largest magnitude of the token, NaN where one is; of_group: that
+// of the 32 channels that the factor is for.  All of it exact: scale has 8 significant bits, factor 8, code 3 and a half 4, so that limits are products
+// that fp32 holds.
+__device__ inline unsigned encode4(const float (&x)[8], float top, float of_group, float& scale, unsigned& factor, float (&held)[8])
+{
+    const bool finite = top < __builtin_inff();
+    constexpr float part = (float)((1.0 - 0x1p-20) / 1568.0);    // the product is below top / 1568, and by less than 8 bits show
+    unsigned u = (__float_as_uint(top * part) & 0xffff0000u) + 0x10000u;
+    if (__uint_as_float(u) * 1568.f < top) u += 0x10000u;
+    scale = top < 0x1p-98f ? 1.f : __uint_as_float(u);
+    const float group = 7.f * scale;
+    float m = __builtin_fmaxf(nearest(of_group, group, __builtin_amdgcn_rcpf(group)), 1.f);
+    if (!finite) scale = __builtin_nanf(""), m = 1.f;
+    factor = (unsigned)m;
+    const float unit = m * scale, inverse = __builtin_amdgcn_rcpf(unit);
+    unsigned word = 0x88888888u;
+    if (finite) {
+        word = 0u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float n = __builtin_fminf(__builtin_fmaxf(nearest(x[i], unit, inverse), -7.f), 7.f);
+            held[i] = n * m;
+            word |= (unsigned)((int)n + 8) << (4 * i);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) held[i] = 0.f;
+    }
+    return word;
+}
+
+// Eight codes of 4 bits and their factor -> fp32, exactly
+__device__ inline void widen8(unsigned w, unsigned factor, float (&x)[8])
+{
+    const float m = (float)factor;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = ((float)((w >> (4 * i)) & 15u) - 8.f) * m;
+}
+
 __device__ inline void widen_io(u16x8 raw, int io_bf16, float (&x)[8])
 {
     if (io_bf16) {
@@ -101,7 +151,7 @@ __device__ inline void widen_io(u16x8 raw, int io_bf16, float (&x)[8])
     }
 }
 
-// Largest of x over LANES neighbouring lanes (8 or 16), NaN where one is
+// Largest of x over LANES neighbouring lanes (4, 8 or 16), NaN where one is
 template <int LANES>
 __device__ inline float largest(float x)
 {
@@ -111,7 +161,7 @@ __device__ inline float largest(float x)
     };
     with(std::integral_constant<int, 0xb1>{});       // lane ^ 1, ^ 2 (quads), 7 - lane of 8, 15 - lane of 16
     with(std::integral_constant<int, 0x4e>{});
-    with(std::integral_constant<int, 0x141>{});
+    if (LANES >= 8) with(std::integral_constant<int, 0x141>{});
     if (LANES == 16) with(std::integral_constant<int, 0x140>{});
     return x;
 }
@@ -203,11 +253,12 @@ __device__ inline Place find_place(const int* __restrict__ length, const int* __
 // What bounds it: a step, what is waited for in turn (lengths, the table's entry, tokens: 16 tokens 4.3 us); prompts, the vector unit (10 to 16 instructions a
 // value) and memory: 32768 tokens on 8 heads, integers, 201 MB, 45 us, 4.5 TB/s; 13924 on 4, e4m3, 43.5 MB, 16.3 us, 2.7 TB/s, with few workgroups to a
 // compute unit.
-template <int D, bool E4M3, int NT>
+template <int D, int FORMAT, int NT>
 __global__ __launch_bounds__(NT)
 void pasa_cache_write_k(pasa_cache c, const unsigned short* __restrict__ k, const unsigned short* __restrict__ v, int R, long long row_stride,
                         const int* __restrict__ row_start, int io_bf16, int page_log2, FastDiv heads)
 {
+    constexpr bool E4M3 = FORMAT == PASA_CACHE_E4M3, I4 = FORMAT == PASA_CACHE_I4;
     constexpr int LT = D / 8, AT = NT / LT, BATCH = 2;   // lanes of a token, tokens at a time, of which so many are on their way
     __shared__ __attribute__((aligned(16))) float sums[AT][D];
     const int tid = threadIdx.x, lt = tid % LT, t0 = tid / LT;
@@ -232,14 +283,16 @@ void pasa_cache_write_k(pasa_cache c, const unsigned short* __restrict__ k, cons
     const int tokens = s.length - pos0 < c.page ? s.length - pos0 : c.page;      // of the page
     const int fresh = s.length - s.rows - pos0;                                  // the first new one, when not negative
     const size_t slot = ((size_t)id * c.Hkv + hk) * c.page;
-    unsigned char* kc = static_cast<unsigned char*>(c.k) + slot * D;
-    unsigned char* vc = static_cast<unsigned char*>(c.v) + slot * D;
+    const size_t first_byte = slot * (I4 ? token_bytes4(D) : D);
+    unsigned char* kc = static_cast<unsigned char*>(c.k) + first_byte;
+    unsigned char* vc = static_cast<unsigned char*>(c.v) + first_byte;
+    auto factor_at = [&](int t) { return c.page * (D / 2) + t * (D / kFactorChannels) + lt / (kFactorChannels / 8); };
     const bool means = c.kmean != nullptr;
 
     f4 sum[2] = {(f4)0.f, (f4)0.f};
     for (int begin = means || fresh < 0 ? 0 : fresh / AT * AT; begin < tokens; begin += BATCH * AT) {
         u16x8 kraw[BATCH], vraw[BATCH];
-        uint2 older[BATCH];
+        uint2 older[BATCH];                      // in 4 bits codes and a factor
         float older_scale[BATCH];
 #pragma unroll
         for (int j = 0; j < BATCH; ++j) {
@@ -250,7 +303,12 @@ void pasa_cache_write_k(pasa_cache c, const unsigned short* __restrict__ k, cons
                 vraw[j] = *reinterpret_cast<const u16x8*>(v + row);
             }
             if (t < tokens && t < fresh && means) {
-                older[j] = *reinterpret_cast<const uint2*>(kc + (size_t)t * D + 8 * lt);
+                if constexpr (I4) {
+                    older[j].x = *reinterpret_cast<const unsigned*>(kc + t * (D / 2) + 4 * lt);
+                    older[j].y = kc[factor_at(t)];
+                } else {
+                    older[j] = *reinterpret_cast<const uint2*>(kc + (size_t)t * D + 8 * lt);
+                }
                 older_scale[j] = c.kscale[slot + t];
             }
         }
@@ -270,22 +328,38 @@ void pasa_cache_write_k(pasa_cache c, const unsigned short* __restrict__ k, cons
                     top_k = __builtin_elementwise_maximum(top_k, __builtin_fabsf(x[i]));
                     top_v = __builtin_elementwise_maximum(top_v, __builtin_fabsf(y[i]));
                 }
-                const uint2 vcode = encode8<E4M3>(y, largest<LT>(top_v), vscale, unused);
-                const uint2 code = encode8<E4M3>(x, largest<LT>(top_k), scale, held);
-                *reinterpret_cast<uint2*>(kc + (size_t)t * D + 8 * lt) = code;
-                *reinterpret_cast<uint2*>(vc + (size_t)t * D + 8 * lt) = vcode;
+                if constexpr (I4) {
+                    unsigned kfactor, vfactor;
+                    const unsigned vcode = encode4(y, largest<LT>(top_v), largest<4>(top_v), vscale, vfactor, unused);
+                    const unsigned code = encode4(x, largest<LT>(top_k), largest<4>(top_k), scale, kfactor, held);
+                    *reinterpret_cast<unsigned*>(kc + t * (D / 2) + 4 * lt) = code;
+                    *reinterpret_cast<unsigned*>(vc + t * (D / 2) + 4 * lt) = vcode;
+                    if (lt % 4 == 0) {
+                        kc[factor_at(t)] = (unsigned char)kfactor;
+                        vc[factor_at(t)] = (unsigned char)vfactor;
+                    }
+                } else {
+                    const uint2 vcode = encode8<E4M3>(y, largest<LT>(top_v), vscale, unused);
+                    const uint2 code = encode8<E4M3>(x, largest<LT>(top_k), scale, held);
+                    *reinterpret_cast<uint2*>(kc + (size_t)t * D + 8 * lt) = code;
+                    *reinterpret_cast<uint2*>(vc + (size_t)t * D + 8 * lt) = vcode;
+                }
                 if (lt == 0) {
                     c.kscale[slot + t] = scale;
                     c.vscale[slot + t] = vscale;
                 }
             } else {
                 if (!means) continue;
-                float lo[4], hi[4];
-                widen4<E4M3>(older[j].x, lo);
-                widen4<E4M3>(older[j].y, hi);
                 scale = older_scale[j];
+                if constexpr (I4) {
+                    widen8(older[j].x, older[j].y, held);
+                } else {
+                    float lo[4], hi[4];
+                    widen4<E4M3>(older[j].x, lo);
+                    widen4<E4M3>(older[j].y, hi);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) held[i] = lo[i], held[4 + i] = hi[i];
+                    for (int i = 0; i < 4; ++i) held[i] = lo[i], held[4 + i] = hi[i];
+                }
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i >> 2][i & 3] = __builtin_fmaf(held[i], scale, sum[i >> 2][i & 3]);
@@ -314,11 +388,12 @@ constexpr int kReadBatch = 4;
 constexpr int read_tokens(int d) { return kReadBatch * kCacheThreads / (d / 8); }
 constexpr size_t kStreamBytes = (size_t)32 << 20;
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
-template <int D, bool E4M3, bool STREAM>
+template <int D, int FORMAT, bool STREAM>
 __global__ __launch_bounds__(kCacheThreads)
 void pasa_cache_read_k(pasa_cache c, unsigned short* __restrict__ k, unsigned short* __restrict__ v, const int* __restrict__ first, int N,
                        int io_bf16, int page_log2, FastDiv heads, FastDiv chunks)
 {
+    constexpr bool E4M3 = FORMAT == PASA_CACHE_E4M3, I4 = FORMAT == PASA_CACHE_I4;
     constexpr int LT = D / 8, AT = kCacheThreads / LT, BATCH = kReadBatch;
     const int tid = threadIdx.x, lt = tid % LT, t0 = tid / LT;
     const unsigned up = chunks.quotient(blockIdx.x);
@@ -344,8 +419,18 @@ void pasa_cache_read_k(pasa_cache c, unsigned short* __restrict__ k, unsigned sh
     for (int j = 0; j < BATCH; ++j) {
         if (pos[j] < 0 || id[j] < 0 || id[j] >= c.pages) pos[j] = -1;
         const size_t slot = pos[j] < 0 ? 0 : (((size_t)id[j] * c.Hkv + hk) << page_log2) + (size_t)(pos[j] & (c.page - 1));
-        code[j][0] = *reinterpret_cast<const uint2*>(static_cast<const unsigned char*>(c.k) + slot * D + 8 * lt);
-        code[j][1] = *reinterpret_cast<const uint2*>(static_cast<const unsigned char*>(c.v) + slot * D + 8 * lt);
+        if constexpr (I4) {                      // a word of codes, a factor
+            const size_t at = pos[j] < 0 ? 0 : (size_t)(pos[j] & (c.page - 1)), first_byte = (slot - at) * token_bytes4(D);
+            const size_t codes = first_byte + at * (D / 2) + 4 * lt;
+            const size_t factor = first_byte + (size_t)c.page * (D / 2) + at * (D / kFactorChannels) + lt / (kFactorChannels / 8);
+            code[j][0].x = *reinterpret_cast<const unsigned*>(static_cast<const unsigned char*>(c.k) + codes);
+            code[j][1].x = *reinterpret_cast<const unsigned*>(static_cast<const unsigned char*>(c.v) + codes);
+            code[j][0].y = static_cast<const unsigned char*>(c.k)[factor];
+            code[j][1].y = static_cast<const unsigned char*>(c.v)[factor];
+        } else {
+            code[j][0] = *reinterpret_cast<const uint2*>(static_cast<const unsigned char*>(c.k) + slot * D + 8 * lt);
+            code[j][1] = *reinterpret_cast<const uint2*>(static_cast<const unsigned char*>(c.v) + slot * D + 8 * lt);
+        }
         scale[j][0] = c.kscale[slot];
         scale[j][1] = c.vscale[slot];
     }
@@ -357,10 +442,17 @@ void pasa_cache_read_k(pasa_cache c, unsigned short* __restrict__ k, unsigned sh
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
             unsigned out[4];
+            float wide[8];
+            if constexpr (I4) widen8(code[j][which].x, code[j][which].y, wide);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 float x[4];
-                widen4<E4M3>(h == 0 ? code[j][which].x : code[j][which].y, x);
+                if constexpr (I4) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = wide[4 * h + i];
+                } else {
+                    widen4<E4M3>(h == 0 ? code[j][which].x : code[j][which].y, x);
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[i] = pos[j] >= 0 ? __builtin_fmaf(x[i], scale[j][which], which == 0 ? shift[h][i] : 0.f) : 0.f;
                 out[2 * h] = io_bf16 ? pack_bf16(x[0], x[1]) : pack_f16(x[0], x[1]);
@@ -595,10 +687,11 @@ hipError_t pasa_launch_cache_write(const pasa_cache& c, const void* k, const voi
         kernel<<<grid, threads, 0, stream>>>(c, static_cast<const unsigned short*>(k), static_cast<const unsigned short*>(v), R, row_stride, row_start,
                                              io_bf16, log2_of(c.page), fast_div(c.Hkv));
     };
-    const bool e = c.format == PASA_CACHE_E4M3;
     auto of_threads = [&](auto d, auto nt) {
         constexpr int D = decltype(d)::value, NT = decltype(nt)::value;
-        e ? go(pasa_cache_write_k<D, true, NT>, NT) : go(pasa_cache_write_k<D, false, NT>, NT);
+        if (c.format == PASA_CACHE_I4) go(pasa_cache_write_k<D, PASA_CACHE_I4, NT>, NT);
+        else if (c.format == PASA_CACHE_E4M3) go(pasa_cache_write_k<D, PASA_CACHE_E4M3, NT>, NT);
+        else go(pasa_cache_write_k<D, PASA_CACHE_I8, NT>, NT);
     };
     auto of_size = [&](auto d) {
         if (lanes <= 1024) of_threads(d, std::integral_constant<int, 256>{});
@@ -616,11 +709,16 @@ hipError_t pasa_launch_cache_read(const pasa_cache& c, void* k, void* v, const i
         kernel<<<grid, kCacheThreads, 0, stream>>>(c, static_cast<unsigned short*>(k), static_cast<unsigned short*>(v), first, N, io_bf16, log2_of(c.page),
                                                    fast_div(c.Hkv), fast_div(chunks));
     };
-    const bool e = c.format == PASA_CACHE_E4M3, far = (size_t)4 * c.S * c.Hkv * N * c.d > kStreamBytes;
+    const bool far = (size_t)4 * c.S * c.Hkv * N * c.d > kStreamBytes;
     auto of_size = [&](auto d) {
         constexpr int D = decltype(d)::value;
-        if (e) far ? go(pasa_cache_read_k<D, true, true>) : go(pasa_cache_read_k<D, true, false>);
-        else far ? go(pasa_cache_read_k<D, false, true>) : go(pasa_cache_read_k<D, false, false>);
+        auto held_as = [&](auto format) {
+            constexpr int FORMAT = decltype(format)::value;
+            far ? go(pasa_cache_read_k<D, FORMAT, true>) : go(pasa_cache_read_k<D, FORMAT, false>);
+        };
+        if (c.format == PASA_CACHE_I4) held_as(std::integral_constant<int, PASA_CACHE_I4>{});
+        else if (c.format == PASA_CACHE_E4M3) held_as(std::integral_constant<int, PASA_CACHE_E4M3>{});
+        else held_as(std::integral_constant<int, PASA_CACHE_I8>{});
     };
     c.d == 128 ? of_size(std::integral_constant<int, 128>{}) : of_size(std::integral_constant<int, 64>{});
     return hipGetLastError();

@@ -24,7 +24,7 @@ int check_cache(const pasa_cache* c)
         c->kscale == c->vscale || !aligned(c->kmean, 16) || !aligned(c->kshift, 16) || !buffer(c->table, 4) || !buffer(c->length, 4))
         return PASA_EINVAL;
     if (c->S <= 0 || c->Hkv <= 0 || c->pages <= 0 || c->table_width <= 0 || c->d <= 0 || c->page <= 0) return PASA_EINVAL;
-    if (c->format != PASA_CACHE_I8 && c->format != PASA_CACHE_E4M3) return PASA_EINVAL;
+    if (c->format != PASA_CACHE_I8 && c->format != PASA_CACHE_E4M3 && c->format != PASA_CACHE_I4) return PASA_EINVAL;
     if (c->d != 64 && c->d != 128) return PASA_EUNSUPPORTED;
     if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return PASA_EUNSUPPORTED;
     if ((long long)c->table_width * c->page > kMaxTokens || (long long)c->S * c->Hkv > kMaxGrid) return PASA_EUNSUPPORTED;
