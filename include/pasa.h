@@ -303,6 +303,87 @@ int pasa_attn_cache(const pasa_cache* cache, const void* q, void* o, int R, long
                     float scale, const unsigned long long* tree, const int* blocks, int count, int io_dtype, void* workspace,
                     size_t workspace_bytes, void* stream);
 
+/* ---- Rotary positions ----
+ *
+ * Pair i of a head's channels, (x_a, x_b), is turned by its position times freq[i]:
+ *     y_a = magnitude * (x_a cos - x_b sin),   y_b = magnitude * (x_a sin + x_b cos),
+ * the angle in 64 bits, the rest in fp32, rounded once to the type of the tensors.  Channels from `rot` on are copied. */
+typedef enum {
+    PASA_ROTARY_HALVES = 0,   /* pair i is channels i and rot / 2 + i */
+    PASA_ROTARY_PAIRS = 1     /* pair i is channels 2 i and 2 i + 1 */
+} pasa_rotary_layout;
+
+/* Frequencies for contexts longer than those trained on, by `factor` (>= 1).  f_i = base^(-2 i / rot). */
+typedef enum {
+    PASA_ROTARY_PLAIN = 0,    /* f_i */
+    PASA_ROTARY_LINEAR = 1,   /* f_i / factor: positions are pressed together */
+    PASA_ROTARY_BASE = 2,     /* base * factor^(rot / (rot - 2)) in place of base: the slowest pair is slowed by the factor, the fastest not at all */
+    PASA_ROTARY_RAMP = 3,     /* f_i where a pair turns `fast` times or more over the `original` length, f_i / factor where `slow` times or less, blended in between
+                                 by the pair's number: keep = 1 - (i - first) / (last - first), within 0 .. 1, with first = floor(p(fast)) and
+                                 last = ceil(p(slow)) within 0 .. rot - 1 (0.001 apart at least), p(t) = rot ln(original / (2 pi t)) / (2 ln base) */
+    PASA_ROTARY_WAVES = 4     /* as RAMP, blended by the turns: keep = (original f_i / (2 pi) - slow) / (fast - slow), within 0 .. 1 */
+} pasa_rotary_scaling;
+
+typedef struct {
+    double freq[64];      /* radians a position, of rot / 2 pairs */
+    double magnitude;     /* of cos and sin; 1 where attention is not scaled with the context */
+    int rot;              /* channels that are turned, the first ones of a head: even, 2 .. d */
+    int layout;           /* a pasa_rotary_layout */
+} pasa_rotary;
+
+/* Host-only: fills a pasa_rotary (which the caller may also fill, or change, as it likes).  base > 1; factor is used but for PLAIN; original > 0 and
+ * 0 < slow < fast by RAMP and WAVES only.  PASA_EUNSUPPORTED for rot > 128. */
+int pasa_rotary_set(pasa_rotary* rotary, int layout, int rot, double base, int scaling, double factor, double original, double slow, double fast,
+                    double magnitude);
+
+/* Whole sequences.  x, y: B x H x N heads of d = 64 or 128 channels, 16-byte aligned, fp16 or bf16; x_strides, y_strides: elements from a batch entry, a head and a
+ * row to the next (host arrays of three, multiples of 8, not negative; of y at least d where there is more than one), or NULL: contiguous [B, H, N, d].  So queries
+ * and keys are taken out of a joint projection and laid out for pasa_attn_fwd as they are turned.  y may be x (with its strides; channels from
+ * rot on are left alone then) and must not overlap it otherwise, nor must its heads overlap.  Positions: positions (DEVICE [B][N]), or, where that is NULL, row0 + n.
+ * transposed != 0: turned back, sin by -sin: for a y's gradient as x, the gradient of x.  PASA_EUNSUPPORTED also where B * N or the launch does not fit 31 and 32 bits. */
+int pasa_rotate(const pasa_rotary* rotary, const void* x, void* y, int B, int H, int N, int d, const long long* x_strides, const long long* y_strides,
+                const int* positions, int row0, int transposed, int io_dtype, void* stream);
+
+/* The rows of a step, at their positions in the cache (only whose lengths are read): R rows of `heads` heads of d channels, x_stride and y_stride elements apart (as
+ * row_stride above); the query and key heads of a joint projection lie side by side and go in one call.  y may be x (with its stride).  tree == NULL: row
+ * row_start[b] + t at length[b] - n_b + t.  tree as in pasa_attn_cache: at length[b] - n_b and as many on as the row sees of its sequence's rows beside
+ * itself, its depth.  Rows of no sequence are left alone.  A step is: lengths, pasa_cache_rotate, pasa_cache_write, pasa_attn_cache. */
+int pasa_cache_rotate(const pasa_cache* cache, const pasa_rotary* rotary, const void* x, void* y, int heads, int R, long long x_stride, long long y_stride,
+                      const int* row_start, const unsigned long long* tree, int transposed, int io_dtype, void* stream);
+
+/* ---- Pages of a cache: shared, given out, taken back and packed on the device ----
+ *
+ * refs: DEVICE [pages], 16-byte aligned: how many entries of the tables hold each page, 0 where a page is free.  A sequence holds a page once; entries that hold none are
+ * -1 (or anything outside the pool).  A caller starts with zeros and entries of -1.  The calls change tables, lengths and refs where the description's pointers
+ * say, all of it on the device and in the order of the stream, so that a captured graph follows; they do the same whatever the order of its threads.  Other callers of
+ * these buffers have to wait meanwhile.  Where refs are not the counts, pages may be given out twice or never; nothing outside the buffers is touched.
+ * pasa_cache_write does not look at refs: pasa_cache_room first gives every row a page that its sequence does not share.
+ * PASA_EUNSUPPORTED also for more than 2^30 pages, pages of more than 2^30 codes, and tables of 2^31 entries. */
+
+/* Contents of pages from_pages[i] of one pool to to_pages[i] of another, or of the same (DEVICE [n] each): codes, scales and, where `to` keeps them, means.  The pools
+ * have the same Hkv, d, page and format.  Pairs with a page outside its pool are passed over.  No page may be written twice, or written and read, in a call. */
+int pasa_cache_copy(const pasa_cache* to, const pasa_cache* from, const int* to_pages, const int* from_pages, int n, void* stream);
+
+/* Afterwards sequence b is what sequence source[b] was before (DEVICE [S], source[b] == b: untouched): its length, and the pages of its tokens, which both hold from then
+ * on.  Outside 0 .. S - 1: empty, its pages let go of.  So beams go on from others, requests branch, and sequences end. */
+size_t pasa_cache_fork_workspace(const pasa_cache* cache);
+int pasa_cache_fork(const pasa_cache* cache, int* refs, const int* source, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Entries behind the tokens of a sequence (places ceil(length[b] / page) and on) let go of their pages: after lengths have become less. */
+int pasa_cache_free(const pasa_cache* cache, int* refs, void* stream);
+
+/* Room for a step's rows: places that they are written to get pages of their own.  In order of sequences and places: a place without a page takes the lowest free one; one
+ * whose page others hold as well lets go of it, takes the lowest free one, and, if older tokens are in the page, a copy of its contents (so the last of several
+ * that go on from the same page keeps it).  Free are the pages that were so before the call.  Where none is left the place is without (rows written there are
+ * lost) and counts in *lacking (DEVICE, may be NULL; it is set, also to 0): the caller ends such a sequence, or another, before the next step. */
+size_t pasa_cache_room_workspace(const pasa_cache* cache, int R);
+int pasa_cache_room(const pasa_cache* cache, int* refs, int R, const int* row_start, int* lacking, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The pages in use become the first ones of the pool: with n of them, those that lie at n or behind move, in order, to the free ones before n, in order.  Tables and refs follow.
+ * *used (DEVICE, may be NULL): n. */
+size_t pasa_cache_compact_workspace(const pasa_cache* cache);
+int pasa_cache_compact(const pasa_cache* cache, int* refs, int* used, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Host-only, fp64: solves the optimal accuracy condition beta/(1-beta) = f(beta) (Eq. (16), (20)-(22)) by
  * fixed-point iteration from beta0, for a shifting matrix of size n rounded to format tp
  * (0 = fp16, 1 = bf16).  Returns NaN for invalid arguments. */

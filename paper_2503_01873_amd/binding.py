@@ -16,6 +16,8 @@ MIXED, STRICT16, NAIVE16, S16, DIRECT = 0, 1, 2, 3, 4
 SHIFT_MEAN, SHIFT_MATRIX, SHIFT_MATRIX_MFMA = 0, 1, 2
 IO_F16, IO_BF16 = 0, 1
 CACHE_I8, CACHE_E4M3, CACHE_I4 = 0, 1, 4
+ROTARY_HALVES, ROTARY_PAIRS = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_RAMP, ROTARY_WAVES = 0, 1, 2, 3, 4
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.environ.get("PASA_LIB") or os.path.join(_PKG, "libpasa.so")
@@ -53,6 +55,14 @@ class pasa_cache(ctypes.Structure):
 
     def data_ptr(self):
         return self.address
+
+
+class pasa_rotary(ctypes.Structure):
+    """Frequencies and layout of rotary positions; pasa_rotary_set fills one."""
+    _fields_ = [("freq", ctypes.c_double * 64), ("magnitude", ctypes.c_double), ("rot", ctypes.c_int), ("layout", ctypes.c_int)]
+
+    def data_ptr(self):
+        return ctypes.addressof(self)
 
 
 def lib_path() -> str:
@@ -109,6 +119,28 @@ def lib() -> ctypes.CDLL:
     L.pasa_attn_cache_workspace.restype = sz
     L.pasa_attn_cache.argtypes = [vp, vp, vp, ci, ll, vp, ci, cf, vp, vp, ci, ci, vp, sz, vp]
     L.pasa_attn_cache.restype = ci
+    L.pasa_rotary_set.argtypes = [vp, ci, ci, cd, ci, cd, cd, cd, cd, cd]
+    L.pasa_rotary_set.restype = ci
+    L.pasa_rotate.argtypes = [vp, vp, vp, ci, ci, ci, ci, vp, vp, vp, ci, ci, ci, vp]
+    L.pasa_rotate.restype = ci
+    L.pasa_cache_rotate.argtypes = [vp, vp, vp, vp, ci, ci, ll, ll, vp, vp, ci, ci, vp]
+    L.pasa_cache_rotate.restype = ci
+    L.pasa_cache_copy.argtypes = [vp, vp, vp, vp, ci, vp]
+    L.pasa_cache_copy.restype = ci
+    L.pasa_cache_fork_workspace.argtypes = [vp]
+    L.pasa_cache_fork_workspace.restype = sz
+    L.pasa_cache_fork.argtypes = [vp, vp, vp, vp, sz, vp]
+    L.pasa_cache_fork.restype = ci
+    L.pasa_cache_free.argtypes = [vp, vp, vp]
+    L.pasa_cache_free.restype = ci
+    L.pasa_cache_room_workspace.argtypes = [vp, ci]
+    L.pasa_cache_room_workspace.restype = sz
+    L.pasa_cache_room.argtypes = [vp, vp, ci, vp, vp, vp, sz, vp]
+    L.pasa_cache_room.restype = ci
+    L.pasa_cache_compact_workspace.argtypes = [vp]
+    L.pasa_cache_compact_workspace.restype = sz
+    L.pasa_cache_compact.argtypes = [vp, vp, vp, vp, sz, vp]
+    L.pasa_cache_compact.restype = ci
     L.pasa_optimal_beta.argtypes = [cd, ci, ci]
     L.pasa_optimal_beta.restype = cd
     L.pasa_invariance_rounded.argtypes = [cd, ci, ci]
@@ -125,7 +157,9 @@ def lib() -> ctypes.CDLL:
                                   ("pasa_attn_fwd_adaptive", "whole", _whole), ("pasa_prepare_kv", "prepare", _prepare),
                                   ("pasa_attn_fwd_chunk", "chunk", _chunk), ("pasa_cache_write", "cache_write", _cache_write),
                                   ("pasa_cache_read", "cache_read", _cache_read), ("pasa_cache_choose", "cache_choose", _cache_choose),
-                                  ("pasa_attn_cache", "attn_cache", _attn_cache)):
+                                  ("pasa_attn_cache", "attn_cache", _attn_cache), ("pasa_cache_rotate", "cache_rotate", _cache_rotate),
+                                  ("pasa_rotate", "rotate", _rotate), ("pasa_cache_fork", "cache_fork", _cache_fork),
+                                  ("pasa_cache_room", "cache_room", _cache_room)):
         f = getattr(L, name)
         call = functools.partial(in_ctypes, f)
         if calls is not None:
@@ -194,6 +228,33 @@ def _cache_choose(f, cache, q, R, row_stride, row_start, Hq, blocks, count, head
 def _attn_cache(f, cache, q, o, R, row_stride, row_start, Hq, scale, workspace, workspace_bytes, stream, tree, blocks, count, io_dtype):
     return f(_ptr(cache), _ptr(q), _ptr(o), R, row_stride, _ptr(row_start), Hq, float(scale), _ptr(tree), _ptr(blocks), count, int(io_dtype),
              _ptr(workspace), int(workspace_bytes), _stream(stream))
+
+
+def _strides(x):
+    """Three strides, as a sequence of integers or the address of a host array."""
+    if x is None or isinstance(x, int):
+        return x
+    if len(x) != 3:
+        raise ValueError("three strides: batch, head, row")
+    return (ctypes.c_longlong * 3)(*x)
+
+
+def _rotate(f, rotary, x, y, B, H, N, d, stream, x_strides, y_strides, positions, row0, transposed, io_dtype):
+    return f(_ptr(rotary), _ptr(x), _ptr(y), B, H, N, d, _strides(x_strides), _strides(y_strides), _ptr(positions), row0, int(transposed), int(io_dtype),
+             _stream(stream))
+
+
+def _cache_rotate(f, cache, rotary, x, y, heads, R, x_stride, y_stride, row_start, stream, tree, transposed, io_dtype):
+    return f(_ptr(cache), _ptr(rotary), _ptr(x), _ptr(y), heads, R, x_stride, y_stride, _ptr(row_start), _ptr(tree), int(transposed), int(io_dtype),
+             _stream(stream))
+
+
+def _cache_fork(f, cache, refs, source, workspace, workspace_bytes, stream):
+    return f(_ptr(cache), _ptr(refs), _ptr(source), _ptr(workspace), int(workspace_bytes), _stream(stream))
+
+
+def _cache_room(f, cache, refs, R, row_start, lacking, workspace, workspace_bytes, stream):
+    return f(_ptr(cache), _ptr(refs), R, _ptr(row_start), _ptr(lacking), _ptr(workspace), int(workspace_bytes), _stream(stream))
 
 
 def _check(status: int, what: str, check: bool):
@@ -338,3 +399,56 @@ def pasa_attn_cache(cache, q, o, R, row_stride, row_start, Hq, scale, workspace,
     st = (_lib or lib()).call_pasa_attn_cache(cache, q, o, R, row_stride, row_start, Hq, scale, workspace, workspace_bytes, stream, tree, blocks,
                                               count, io_dtype)
     return _check(st, "pasa_attn_cache", check)
+
+
+def pasa_rotary_set(rotary, layout, rot, base, scaling=ROTARY_PLAIN, factor=1.0, original=0.0, slow=1.0, fast=32.0, magnitude=1.0, check=True) -> int:
+    st = lib().pasa_rotary_set(_ptr(rotary), layout, rot, float(base), scaling, float(factor), float(original), float(slow), float(fast), float(magnitude))
+    return _check(st, "pasa_rotary_set", check)
+
+
+def pasa_rotate(rotary, x, y, B, H, N, d, stream=None, x_strides=None, y_strides=None, positions=None, row0=0, transposed=False, io_dtype=IO_F16,
+                check=True) -> int:
+    st = (_lib or lib()).call_pasa_rotate(rotary, x, y, B, H, N, d, stream, x_strides, y_strides, positions, row0, transposed, io_dtype)
+    return _check(st, "pasa_rotate", check)
+
+
+def pasa_cache_rotate(cache, rotary, x, y, heads, R, x_stride, y_stride, row_start, stream=None, tree=None, transposed=False, io_dtype=IO_F16,
+                      check=True) -> int:
+    st = (_lib or lib()).call_pasa_cache_rotate(cache, rotary, x, y, heads, R, x_stride, y_stride, row_start, stream, tree, transposed, io_dtype)
+    return _check(st, "pasa_cache_rotate", check)
+
+
+def pasa_cache_copy(to, of, to_pages, from_pages, n, stream=None, check=True) -> int:
+    st = lib().pasa_cache_copy(_ptr(to), _ptr(of), _ptr(to_pages), _ptr(from_pages), n, _stream(stream))
+    return _check(st, "pasa_cache_copy", check)
+
+
+def pasa_cache_fork_workspace(cache) -> int:
+    return lib().pasa_cache_fork_workspace(_ptr(cache))
+
+
+def pasa_cache_fork(cache, refs, source, workspace, workspace_bytes, stream=None, check=True) -> int:
+    st = (_lib or lib()).call_pasa_cache_fork(cache, refs, source, workspace, workspace_bytes, stream)
+    return _check(st, "pasa_cache_fork", check)
+
+
+def pasa_cache_free(cache, refs, stream=None, check=True) -> int:
+    return _check(lib().pasa_cache_free(_ptr(cache), _ptr(refs), _stream(stream)), "pasa_cache_free", check)
+
+
+def pasa_cache_room_workspace(cache, R) -> int:
+    return lib().pasa_cache_room_workspace(_ptr(cache), R)
+
+
+def pasa_cache_room(cache, refs, R, row_start, lacking, workspace, workspace_bytes, stream=None, check=True) -> int:
+    st = (_lib or lib()).call_pasa_cache_room(cache, refs, R, row_start, lacking, workspace, workspace_bytes, stream)
+    return _check(st, "pasa_cache_room", check)
+
+
+def pasa_cache_compact_workspace(cache) -> int:
+    return lib().pasa_cache_compact_workspace(_ptr(cache))
+
+
+def pasa_cache_compact(cache, refs, used, workspace, workspace_bytes, stream=None, check=True) -> int:
+    st = lib().pasa_cache_compact(_ptr(cache), _ptr(refs), _ptr(used), _ptr(workspace), int(workspace_bytes), _stream(stream))
+    return _check(st, "pasa_cache_compact", check)

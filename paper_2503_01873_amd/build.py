@@ -13,7 +13,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libpasa.so")
 CALLS = os.path.join(PKG, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))      # for this interpreter: others do not load it
 SOURCES = ["pasa_api.hip", "pasa_kernels.hip", "pasa_fwd4.hip", "pasa_rows.hip", "pasa_shift_gemm.hip",
-           "pasa_cache_api.hip", "pasa_cache.hip", "pasa_attn_cache.hip"]
+           "pasa_cache_api.hip", "pasa_cache.hip", "pasa_attn_cache.hip", "pasa_rotary.hip", "pasa_pages.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950",

@@ -264,6 +264,74 @@ static PyObject* attn_cache(PyObject* self, PyObject* const* a, Py_ssize_t n)
     return PyLong_FromLong(status);
 }
 
+/* None, an address or a tuple of three integers; `out` is where the tuple's go */
+static int get_strides(PyObject* x, long long* out, void** at)
+{
+    if (x == Py_None || PyLong_Check(x)) return get_ptr(x, at);
+    if (!PyTuple_CheckExact(x) || PyTuple_GET_SIZE(x) != 3) return 0;
+    for (int i = 0; i < 3; ++i)
+        if (!get_long(PyTuple_GET_ITEM(x, i), out + i)) return 0;
+    *at = out;
+    return 1;
+}
+
+/* address, ctypes, rotary, x, y, B, H, N, d, stream, strides of x and y, positions, row0, transposed, type */
+static PyObject* rotate(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    void *f, *p[3], *stream, *strides[2], *positions;
+    long long held[2][3];
+    int s[4], row0, status;
+    unsigned long long transposed, type;
+    if (n != 16 || !get_ptr(a[0], &f) || !get_ptrs(a + 2, 3, p) || !get_sizes(a + 5, 4, s) || !get_stream(a[9], &stream) ||
+        !get_strides(a[10], held[0], strides) || !get_strides(a[11], held[1], strides + 1) || !get_ptr(a[12], &positions) || !get_size(a[13], &row0) ||
+        !get_int(a[14], &transposed) || !get_int(a[15], &type))
+        return through_ctypes(a, n);
+    CALL(status, ((int (*)(const void*, const void*, void*, int, int, int, int, const void*, const void*, const void*, int, int, int, void*))f)(
+                     p[0], p[1], p[2], s[0], s[1], s[2], s[3], strides[0], strides[1], positions, row0, (int)(unsigned)transposed, (int)(unsigned)type,
+                     stream));
+    return PyLong_FromLong(status);
+}
+
+/* address, ctypes, cache, rotary, x, y, heads, R, strides of x and y, row_start, stream, tree, transposed, type */
+static PyObject* cache_rotate(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    void *f, *p[4], *rows, *stream, *tree;
+    int s[2], status;
+    long long stride[2];
+    unsigned long long transposed, type;
+    if (n != 15 || !get_ptr(a[0], &f) || !get_ptrs(a + 2, 4, p) || !get_sizes(a + 6, 2, s) || !get_long(a[8], stride) || !get_long(a[9], stride + 1) ||
+        !get_ptr(a[10], &rows) || !get_stream(a[11], &stream) || !get_ptr(a[12], &tree) || !get_int(a[13], &transposed) || !get_int(a[14], &type))
+        return through_ctypes(a, n);
+    CALL(status, ((int (*)(const void*, const void*, const void*, void*, int, int, long long, long long, const void*, const void*, int, int, void*))f)(
+                     p[0], p[1], p[2], p[3], s[0], s[1], stride[0], stride[1], rows, tree, (int)(unsigned)transposed, (int)(unsigned)type, stream));
+    return PyLong_FromLong(status);
+}
+
+/* address, ctypes, cache, refs, source, workspace, bytes, stream */
+static PyObject* cache_fork(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    void *f, *p[4], *stream;
+    int status;
+    unsigned long long bytes;
+    if (n != 8 || !get_ptr(a[0], &f) || !get_ptrs(a + 2, 4, p) || !get_int(a[6], &bytes) || !get_stream(a[7], &stream)) return through_ctypes(a, n);
+    CALL(status, ((int (*)(const void*, void*, const void*, void*, size_t, void*))f)(p[0], p[1], p[2], p[3], (size_t)bytes, stream));
+    return PyLong_FromLong(status);
+}
+
+/* address, ctypes, cache, refs, R, row_start, lacking, workspace, bytes, stream */
+static PyObject* cache_room(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    void *f, *p[2], *more[3], *stream;
+    int R, status;
+    unsigned long long bytes;
+    if (n != 10 || !get_ptr(a[0], &f) || !get_ptrs(a + 2, 2, p) || !get_size(a[4], &R) || !get_ptrs(a + 5, 3, more) || !get_int(a[8], &bytes) ||
+        !get_stream(a[9], &stream))
+        return through_ctypes(a, n);
+    CALL(status, ((int (*)(const void*, void*, int, const void*, void*, void*, size_t, void*))f)(p[0], p[1], R, more[0], more[1], more[2], (size_t)bytes,
+                                                                                             stream));
+    return PyLong_FromLong(status);
+}
+
 static PyMethodDef methods[] = {
     {"plain", (PyCFunction)(void (*)(void))plain, METH_FASTCALL, NULL},
     {"whole", (PyCFunction)(void (*)(void))whole, METH_FASTCALL, NULL},
@@ -273,6 +341,10 @@ static PyMethodDef methods[] = {
     {"cache_read", (PyCFunction)(void (*)(void))cache_read, METH_FASTCALL, NULL},
     {"cache_choose", (PyCFunction)(void (*)(void))cache_choose, METH_FASTCALL, NULL},
     {"attn_cache", (PyCFunction)(void (*)(void))attn_cache, METH_FASTCALL, NULL},
+    {"rotate", (PyCFunction)(void (*)(void))rotate, METH_FASTCALL, NULL},
+    {"cache_rotate", (PyCFunction)(void (*)(void))cache_rotate, METH_FASTCALL, NULL},
+    {"cache_fork", (PyCFunction)(void (*)(void))cache_fork, METH_FASTCALL, NULL},
+    {"cache_room", (PyCFunction)(void (*)(void))cache_room, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL},
 };
 

@@ -37,6 +37,8 @@ struct MergeRecord {
 };
 __host__ __device__ inline size_t cache_slot_floats(int row_blocks, int d) { return (size_t)16 * row_blocks * (d + 2); }
 
+int pasa_check_cache(const pasa_cache* c);       // a pasa_status
+
 hipError_t pasa_launch_cache_write(const pasa_cache& c, const void* k, const void* v, int R, long long row_stride, const int* row_start,
                                    int io_bf16, hipStream_t stream);
 hipError_t pasa_launch_cache_read(const pasa_cache& c, void* k, void* v, const int* first, int N, int io_bf16, hipStream_t stream);

@@ -73,6 +73,8 @@ int status(hipError_t e) { return e == hipSuccess ? PASA_OK : PASA_ELAUNCH; }
 
 }  // namespace
 
+int pasa_check_cache(const pasa_cache* c) { return check_cache(c); }
+
 extern "C" {
 
 int pasa_cache_write(const pasa_cache* cache, const void* k, const void* v, int R, long long row_stride, const int* row_start, int io_dtype,

@@ -1,0 +1,570 @@
+// Pages of a cache: copied, shared between sequences, given out, taken back and packed.  Entry points and kernels.
+#include <hip/hip_runtime.h>
+#include <limits.h>
+#include <stdint.h>
+#include <type_traits>
+
+#include "pasa.h"
+#include "pasa_cache.h"
+
+namespace {
+
+constexpr int kPlanThreads = 1024;               // of the workgroups that look through holders
+constexpr int kEach = 16;                        // holders of a thread at a time
+constexpr int kSpan = kPlanThreads * kEach;      // of a workgroup
+constexpr int kCopyAtOnce = 4;                   // 16-byte units of a thread that are on their way together
+constexpr int kCopyUnits = kCacheThreads * kCopyAtOnce;
+constexpr int kCopyGroups = 2048;                // workgroups of a copy whose length only the device knows
+
+// ---- copies ----
+
+// A page is up to five stretches of memory, whole heads behind one another: codes, scales, the mean.  `ends` counts 16-byte units up to and with each.
+struct CopyArgs {
+    const uint4* from[5];
+    uint4* to[5];
+    unsigned ends[5], chunks;                    // chunks: of kCopyUnits, of a page
+    int pages_from, pages_to;
+};
+
+CopyArgs copy_args(const pasa_cache& to, const pasa_cache& from)
+{
+    CopyArgs a = {};
+    const unsigned codes = (unsigned)((size_t)from.Hkv * from.page * cache_token_bytes(from) / 16), scales = (unsigned)((size_t)from.Hkv * from.page / 4);
+    const unsigned mean = to.kmean != nullptr ? (unsigned)((size_t)from.Hkv * from.d / 4) : 0;
+    const unsigned size[5] = {codes, codes, scales, scales, mean};
+    const void* of[5] = {from.k, from.v, from.kscale, from.vscale, from.kmean};
+    void* at[5] = {to.k, to.v, to.kscale, to.vscale, to.kmean};
+    unsigned end = 0;
+    for (int i = 0; i < 5; ++i) {
+        a.from[i] = static_cast<const uint4*>(of[i]);
+        a.to[i] = static_cast<uint4*>(at[i]);
+        a.ends[i] = end += size[i];
+    }
+    a.chunks = (end + kCopyUnits - 1) / kCopyUnits;
+    a.pages_from = from.pages;
+    a.pages_to = to.pages;
+    return a;
+}
+
+__device__ inline void copy_chunk(const CopyArgs& a, int from, int to, unsigned chunk)
+{
+    uint4 x[kCopyAtOnce];
+    uint4* dst[kCopyAtOnce];
+#pragma unroll
+    for (int j = 0; j < kCopyAtOnce; ++j) {
+        const unsigned unit = chunk * kCopyUnits + j * kCacheThreads + threadIdx.x;
+        const uint4* src = nullptr;
+        dst[j] = nullptr;
+        unsigned begin = 0;
+#pragma unroll
+        for (int i = 0; i < 5; ++i) {
+            const unsigned size = a.ends[i] - begin;
+            if (unit >= begin && unit < a.ends[i]) {
+                src = a.from[i] + (size_t)(unsigned)from * size + (unit - begin);
+                dst[j] = a.to[i] + (size_t)(unsigned)to * size + (unit - begin);
+            }
+            begin = a.ends[i];
+        }
+        if (src != nullptr) x[j] = *src;
+    }
+#pragma unroll
+    for (int j = 0; j < kCopyAtOnce; ++j)
+        if (dst[j] != nullptr) *dst[j] = x[j];
+}
+
+// Pair blockIdx / chunks of two lists
+__global__ __launch_bounds__(kCacheThreads)
+void pasa_copy_pages_k(CopyArgs a, const int* __restrict__ from_pages, const int* __restrict__ to_pages, FastDiv chunks)
+{
+    const unsigned pair = chunks.quotient(blockIdx.x);
+    const int from = from_pages[pair], to = to_pages[pair];
+    if (from < 0 || from >= a.pages_from || to < 0 || to >= a.pages_to) return;
+    copy_chunk(a, from, to, chunks.rest(blockIdx.x, pair));
+}
+
+// ---- sequences go on as others ----
+
+struct Tables {
+    int* table;
+    int* length;
+    int* refs;
+    int S, width, pages, page_log2, page;
+};
+Tables tables_of(const pasa_cache& c, int* refs)
+{
+    return {const_cast<int*>(c.table), const_cast<int*>(c.length), refs, c.S, c.table_width, c.pages, log2_of(c.page), c.page};
+}
+__device__ inline bool in_pool(const Tables& t, int page) { return page >= 0 && page < t.pages; }
+__device__ inline int length_of(const Tables& t, int b) { return clamp_int(t.length[b], 0, t.width << t.page_log2); }
+
+// What sequences that go on as others will hold, beside the tables; they let go of what they hold.
+__global__ __launch_bounds__(kCacheThreads)
+void pasa_fork_out_k(Tables t, const int* __restrict__ source, int* __restrict__ table_next, int* __restrict__ length_next, FastDiv chunks)
+{
+    const int b = (int)chunks.quotient(blockIdx.x), p = (int)chunks.rest(blockIdx.x, (unsigned)b) * kCacheThreads + (int)threadIdx.x;
+    const int from = source[b];
+    if (from == b || p >= t.width) return;
+    const bool ends = from < 0 || from >= t.S;
+    const int length = ends ? 0 : length_of(t, from), places = (length + t.page - 1) >> t.page_log2;
+    const size_t at = (size_t)b * t.width + p;
+    const int old = t.table[at];
+    table_next[at] = p < places ? t.table[(size_t)from * t.width + p] : -1;
+    if (p == 0) length_next[b] = length;
+    if (in_pool(t, old)) atomicSub(t.refs + old, 1);
+}
+
+__global__ __launch_bounds__(kCacheThreads)
+void pasa_fork_in_k(Tables t, const int* __restrict__ source, const int* __restrict__ table_next, const int* __restrict__ length_next, FastDiv chunks)
+{
+    const int b = (int)chunks.quotient(blockIdx.x), p = (int)chunks.rest(blockIdx.x, (unsigned)b) * kCacheThreads + (int)threadIdx.x;
+    if (source[b] == b || p >= t.width) return;
+    const size_t at = (size_t)b * t.width + p;
+    const int page = table_next[at];
+    t.table[at] = page;
+    if (p == 0) t.length[b] = length_next[b];
+    if (in_pool(t, page)) atomicAdd(t.refs + page, 1);
+}
+
+// Pages behind the lengths are let go of.
+__global__ __launch_bounds__(kCacheThreads)
+void pasa_free_k(Tables t, FastDiv chunks)
+{
+    const int b = (int)chunks.quotient(blockIdx.x), p = (int)chunks.rest(blockIdx.x, (unsigned)b) * kCacheThreads + (int)threadIdx.x;
+    if (p >= t.width || p < (length_of(t, b) + t.page - 1) >> t.page_log2) return;
+    const size_t at = (size_t)b * t.width + p;
+    const int old = t.table[at];
+    t.table[at] = -1;
+    if (in_pool(t, old)) atomicSub(t.refs + old, 1);
+}
+
+// ---- room for rows ----
+
+// Sum over the threads of a workgroup before one's own, and over all
+template <int NT>
+__device__ inline unsigned scan_workgroup(unsigned x, unsigned* sums, unsigned& all)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const unsigned upto = scan64(x);
+    __syncthreads();                             // the sums of the last time are read
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    unsigned before = upto - x;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+        if (w < wave) before += sums[w];
+        all += sums[w];
+    }
+    return before;
+}
+
+__device__ inline int holders(const int* refs, int page) { return __hip_atomic_load(refs + page, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// One workgroup.  The places that rows are written to are gone through in order of sequences: a place without a page takes a free one, and so does one whose page
+// others hold too, unless they all are written to here as well and this is the last.  Who holds a page shows in its count: all places here let go first; what is
+// left above 0 belongs to others; otherwise the places take the number of their sequence down to the last one's, which keeps the page.
+// Free pages are looked for from the first on, 16384 at a time, and only as many as are needed: most steps need none and end before that.
+struct RoomArgs {
+    Tables t;
+    const int* row_start;
+    int* lacking;
+    int* begin;                                  // [S + 1] places before each sequence's
+    int* copies;                                 // [2][S] page to be copied and where to, or -1
+    int* free_pages;                             // [most_free]
+    int R, most_free;
+};
+__global__ __launch_bounds__(kPlanThreads)
+void pasa_room_k(RoomArgs a)
+{
+    constexpr int NT = kPlanThreads;
+    __shared__ unsigned sums[NT / 64];
+    const int tid = threadIdx.x;
+    const Tables& t = a.t;
+    const int most = t.width << t.page_log2;
+    auto first_token = [&](const Sequence& s) { return s.length > s.rows ? s.length - s.rows : 0; };
+
+    unsigned total = 0;
+    for (int b0 = 0; b0 < t.S; b0 += NT) {
+        const int b = b0 + tid;
+        unsigned places = 0;
+        if (b < t.S) {
+            const Sequence s = sequence_at(t.length, a.row_start, b, a.R, most);
+            if (s.rows > 0 && s.length > 0) places = (unsigned)(((s.length - 1) >> t.page_log2) - (first_token(s) >> t.page_log2) + 1);
+        }
+        unsigned all;
+        const unsigned before = scan_workgroup<NT>(places, sums, all);
+        if (b < t.S) {
+            a.begin[b] = (int)(total + before);
+            a.copies[b] = -1;
+        }
+        total += all;
+    }
+    if (tid == 0) a.begin[t.S] = (int)total;
+    __syncthreads();
+
+    struct Place {
+        int b, first;                            // sequence, its first new token
+        size_t at;                               // in the table
+        int place, page;                         // the page that is there, or -1
+    };
+    auto place_of = [&](unsigned i) {
+        int low = 0, high = t.S;                 // the last sequence whose places begin at i or before, and that has some
+        while (high - low > 1) {
+            const int middle = (low + high) / 2;
+            if ((unsigned)a.begin[middle] <= i) low = middle;
+            else high = middle;
+        }
+        const Sequence s = sequence_at(t.length, a.row_start, low, a.R, most);
+        Place p;
+        p.b = low;
+        p.first = first_token(s);
+        p.place = clamp_int((p.first >> t.page_log2) + (int)(i - (unsigned)a.begin[low]), 0, t.width - 1);
+        p.at = (size_t)low * t.width + p.place;
+        const int page = t.table[p.at];
+        p.page = in_pool(t, page) ? page : -1;
+        return p;
+    };
+    const bool few = total <= NT;                // a place a thread, looked up once
+    Place mine = {};
+    if (few && (unsigned)tid < total) mine = place_of(tid);
+    auto place_at = [&](unsigned i) { return few ? mine : place_of(i); };
+
+    for (unsigned i = tid; i < total; i += NT) {
+        const Place p = place_at(i);
+        if (p.page >= 0) atomicSub(t.refs + p.page, 1);
+    }
+    __syncthreads();
+    for (unsigned i = tid; i < total; i += NT) {
+        const Place p = place_at(i);
+        if (p.page >= 0 && holders(t.refs, p.page) <= 0) atomicMin(t.refs + p.page, -(p.b + 1));
+    }
+    __syncthreads();
+    auto needs = [&](const Place& p) { return p.page < 0 || holders(t.refs, p.page) != -(p.b + 1); };
+    unsigned wanted = 0;
+    for (unsigned i0 = 0; i0 < total; i0 += NT) {
+        const unsigned i = i0 + tid;
+        unsigned all;
+        scan_workgroup<NT>(i < total && needs(place_at(i)) ? 1u : 0u, sums, all);
+        wanted += all;
+    }
+    unsigned found = 0;
+    const unsigned enough = wanted < (unsigned)a.most_free ? wanted : (unsigned)a.most_free;
+    for (int p0 = 0; p0 < t.pages && found < enough; p0 += kSpan) {
+        const int p = p0 + tid * kEach;
+        unsigned free = 0;                       // bits
+        int4 x[kEach / 4];
+#pragma unroll
+        for (int i = 0; i < kEach / 4; ++i) {
+            x[i] = make_int4(1, 1, 1, 1);
+            if (p + 4 * i + 3 < t.pages) {
+                x[i] = *reinterpret_cast<const int4*>(t.refs + p + 4 * i);
+            } else {
+                if (p + 4 * i < t.pages) x[i].x = t.refs[p + 4 * i];
+                if (p + 4 * i + 1 < t.pages) x[i].y = t.refs[p + 4 * i + 1];
+                if (p + 4 * i + 2 < t.pages) x[i].z = t.refs[p + 4 * i + 2];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kEach / 4; ++i)
+            free |= (unsigned)((x[i].x == 0) | (x[i].y == 0) << 1 | (x[i].z == 0) << 2 | (x[i].w == 0) << 3) << (4 * i);
+        unsigned all, rank = found + scan_workgroup<NT>((unsigned)__builtin_popcount(free), sums, all);
+        for (; free != 0 && rank < enough; free &= free - 1) a.free_pages[rank++] = p + __builtin_ctz(free);
+        found += all;
+    }
+    if (found > enough) found = enough;
+    __syncthreads();
+    unsigned given = 0;
+    for (unsigned i0 = 0; i0 < total; i0 += NT) {
+        const unsigned i = i0 + tid;
+        Place p = {};
+        bool need = false;
+        if (i < total) {
+            p = place_at(i);
+            need = needs(p);
+        }
+        unsigned all;
+        const unsigned rank = given + scan_workgroup<NT>(need ? 1u : 0u, sums, all);
+        given += all;
+        if (i >= total) continue;
+        if (!need) {
+            t.refs[p.page] = 1;                  // all others have let go
+            continue;
+        }
+        const int fresh = rank < found ? a.free_pages[rank] : -1;
+        t.table[p.at] = fresh;
+        if (fresh < 0) continue;
+        t.refs[fresh] = 1;
+        if (p.page >= 0 && p.place << t.page_log2 < p.first) {       // older tokens are in it: the sequence's first place
+            a.copies[p.b] = p.page;
+            a.copies[t.S + p.b] = fresh;
+        }
+    }
+    if (tid == 0 && a.lacking != nullptr) *a.lacking = (int)(wanted - found);
+}
+
+// ---- a pool is packed ----
+
+struct PackArgs {
+    Tables t;
+    int* used;
+    int* counts;                                 // of the workgroups
+    int* header;                                 // pages in use, pages that move
+    int* to;                                     // [pages / 2 + 1] free pages below the number of those in use, ascending
+    int* from;                                   // pages in use from that number on, ascending
+    int* rank;                                   // [pages] which of those a page is, or -1
+    int groups;
+};
+
+// Bit i: whether page p + i is in use
+__device__ inline unsigned in_use(const Tables& t, int p)
+{
+    unsigned live = 0;
+#pragma unroll
+    for (int i = 0; i < kEach / 4; ++i) {
+        int4 x = make_int4(0, 0, 0, 0);
+        if (p + 4 * i + 3 < t.pages) {
+            x = *reinterpret_cast<const int4*>(t.refs + p + 4 * i);
+        } else {
+            if (p + 4 * i < t.pages) x.x = t.refs[p + 4 * i];
+            if (p + 4 * i + 1 < t.pages) x.y = t.refs[p + 4 * i + 1];
+            if (p + 4 * i + 2 < t.pages) x.z = t.refs[p + 4 * i + 2];
+        }
+        live |= (unsigned)((x.x != 0) | (x.y != 0) << 1 | (x.z != 0) << 2 | (x.w != 0) << 3) << (4 * i);
+    }
+    return live;
+}
+
+__global__ __launch_bounds__(kPlanThreads)
+void pasa_pack_count_k(PackArgs a)
+{
+    __shared__ unsigned sums[kPlanThreads / 64];
+    unsigned all;
+    scan_workgroup<kPlanThreads>((unsigned)__builtin_popcount(in_use(a.t, (int)blockIdx.x * kSpan + (int)threadIdx.x * kEach)), sums, all);
+    if (threadIdx.x == 0) a.counts[blockIdx.x] = (int)all;
+}
+
+// With n pages in use, the k-th free one below n takes the k-th used one from n on.  A workgroup has 16384 pages.
+__global__ __launch_bounds__(kPlanThreads)
+void pasa_pack_plan_k(PackArgs a)
+{
+    constexpr int NT = kPlanThreads;
+    __shared__ unsigned sums[NT / 64];
+    const int tid = threadIdx.x, g = (int)blockIdx.x;
+    const int p = g * kSpan + tid * kEach;
+    const unsigned live = in_use(a.t, p);
+    unsigned here;
+    unsigned before = scan_workgroup<NT>((unsigned)__builtin_popcount(live), sums, here);
+    unsigned n = here, others = 0;               // pages in use: of all, of the workgroups before
+    if (a.groups > 1) {
+        unsigned all = 0, first = 0;
+        for (int i = tid; i < a.groups; i += NT) {
+            const unsigned c = (unsigned)a.counts[i];
+            all += c;
+            if (i < g) first += c;
+        }
+        scan_workgroup<NT>(all, sums, n);
+        scan_workgroup<NT>(first, sums, others);
+    }
+    before += others;
+    // of the pages below n those in use: in the workgroup that n lies in, and those before
+    const int at_n = n > 0 ? (int)((n - 1) / kSpan) : 0, q = at_n * kSpan + tid * kEach;
+    unsigned below = q < (int)n ? in_use(a.t, q) : 0u;
+    if ((int)n - q < kEach && q < (int)n) below &= (1u << ((int)n - q)) - 1u;
+    unsigned stay;
+    scan_workgroup<NT>((unsigned)__builtin_popcount(below), sums, stay);
+    if (a.groups > 1) {
+        unsigned first = 0, all;
+        for (int i = tid; i < at_n && i < a.groups; i += NT) first += (unsigned)a.counts[i];
+        scan_workgroup<NT>(first, sums, all);
+        stay += all;
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int page = p + i;
+        if (page >= a.t.pages) break;
+        const bool lives = (live >> i & 1u) != 0u;
+        if (page < (int)n) {
+            if (!lives) a.to[page - (int)before] = page;
+        } else {
+            a.rank[page] = lives ? (int)(before - stay) : -1;
+            if (lives) a.from[before - stay] = page;
+        }
+        before += lives;
+    }
+    if (g == 0 && tid == 0) {
+        a.header[0] = (int)n;
+        a.header[1] = (int)(n - stay);
+        if (a.used != nullptr) *a.used = (int)n;
+    }
+}
+
+// The first workgroups: table entries and holders.  The others: contents.
+__global__ __launch_bounds__(kCacheThreads)
+void pasa_pack_move_k(PackArgs a, CopyArgs c, unsigned entry_groups)
+{
+    const int n = a.header[0], moved = a.header[1];
+    if (blockIdx.x < entry_groups) {
+        const size_t at = (size_t)blockIdx.x * kCacheThreads + threadIdx.x;
+        if (at < (size_t)a.t.S * a.t.width) {
+            const int page = a.t.table[at];
+            if (page >= n && page < a.t.pages) {
+                const int k = a.rank[page];
+                if (k >= 0) a.t.table[at] = a.to[k];
+            }
+        }
+        for (size_t k = at; k < (size_t)moved; k += (size_t)entry_groups * kCacheThreads) {
+            const int of = a.from[k];
+            a.t.refs[a.to[k]] = a.t.refs[of];
+            a.t.refs[of] = 0;
+        }
+        return;
+    }
+    const unsigned long long all = (unsigned long long)moved * c.chunks;
+    for (unsigned long long i = blockIdx.x - entry_groups; i < all; i += gridDim.x - entry_groups) {
+        const unsigned k = (unsigned)(i / c.chunks);
+        copy_chunk(c, a.from[k], a.to[k], (unsigned)(i - (unsigned long long)k * c.chunks));
+    }
+}
+
+bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+bool buffer(const void* p, uintptr_t a) { return p != nullptr && aligned(p, a); }
+size_t rounded_up(size_t bytes) { return (bytes + 255) / 256 * 256; }
+int check_workspace(const void* ws, size_t bytes, size_t need) { return buffer(ws, 256) && bytes >= need ? PASA_OK : PASA_EWORKSPACE; }
+int launched() { return hipGetLastError() == hipSuccess ? PASA_OK : PASA_ELAUNCH; }
+
+constexpr long long kMaxThreads = 0xffffffff;    // of a launch: the hardware counts them in 32 bits
+constexpr int kMaxPages = 1 << 30;               // page numbers and those of a workgroup behind them fit 31 bits
+// units of a page are counted in 32 bits
+bool page_fits(const pasa_cache& c) { return (long long)c.Hkv * c.page * c.d <= 1LL << 30 && c.pages <= kMaxPages; }
+unsigned entry_chunks(const pasa_cache& c) { return (unsigned)((c.table_width + kCacheThreads - 1) / kCacheThreads); }
+
+// The description and the holders of its pages
+int check(const pasa_cache* cache, const int* refs)
+{
+    const int st = pasa_check_cache(cache);
+    if (st != PASA_OK) return st;
+    if (!buffer(refs, 16)) return PASA_EINVAL;
+    if (((long long)cache->table_width + kCacheThreads) * cache->S > kMaxThreads / 2 || !page_fits(*cache)) return PASA_EUNSUPPORTED;
+    return PASA_OK;
+}
+
+long long most_places(const pasa_cache& c, int R)
+{
+    const long long places = (long long)R / c.page + 2LL * c.S;      // a sequence of n rows is written to in (n - 1) / page + 2 places at most, and in n at most
+    return places < R ? places : R;
+}
+int most_free(const pasa_cache& c, int R) { return (int)(most_places(c, R) < c.pages ? most_places(c, R) : c.pages); }
+size_t fork_bytes(const pasa_cache& c) { return rounded_up(((size_t)c.S * c.table_width + c.S) * 4); }
+size_t room_bytes(const pasa_cache& c, int R) { return rounded_up(((size_t)3 * c.S + 1 + most_free(c, R)) * 4); }
+int pack_groups(const pasa_cache& c) { return (int)(((long long)c.pages + kSpan - 1) / kSpan); }
+size_t pack_bytes(const pasa_cache& c) { return rounded_up(((size_t)pack_groups(c) + 2 + 2 * ((size_t)c.pages / 2 + 1) + c.pages) * 4); }
+
+}  // namespace
+
+extern "C" {
+
+int pasa_cache_copy(const pasa_cache* to, const pasa_cache* from, const int* to_pages, const int* from_pages, int n, void* stream)
+{
+    int st = pasa_check_cache(to);
+    if (st != PASA_OK) return st;
+    st = pasa_check_cache(from);
+    if (st != PASA_OK) return st;
+    if (!buffer(to_pages, 4) || !buffer(from_pages, 4) || n <= 0) return PASA_EINVAL;
+    if (to->Hkv != from->Hkv || to->d != from->d || to->page != from->page || to->format != from->format) return PASA_EINVAL;
+    if (to->kmean != nullptr && from->kmean == nullptr) return PASA_EINVAL;
+    if (!page_fits(*to) || !page_fits(*from)) return PASA_EUNSUPPORTED;
+    const CopyArgs a = copy_args(*to, *from);
+    const long long grid = (long long)n * a.chunks;
+    if (grid > kMaxThreads / kCacheThreads) return PASA_EUNSUPPORTED;
+    pasa_copy_pages_k<<<(unsigned)grid, kCacheThreads, 0, static_cast<hipStream_t>(stream)>>>(a, from_pages, to_pages, fast_div(a.chunks));
+    return launched();
+}
+
+size_t pasa_cache_fork_workspace(const pasa_cache* cache) { return pasa_check_cache(cache) == PASA_OK ? fork_bytes(*cache) : 0; }
+
+int pasa_cache_fork(const pasa_cache* cache, int* refs, const int* source, void* workspace, size_t workspace_bytes, void* stream)
+{
+    int st = check(cache, refs);
+    if (st != PASA_OK) return st;
+    if (!buffer(source, 4)) return PASA_EINVAL;
+    st = check_workspace(workspace, workspace_bytes, fork_bytes(*cache));
+    if (st != PASA_OK) return st;
+    const Tables t = tables_of(*cache, refs);
+    const unsigned chunks = entry_chunks(*cache), grid = chunks * (unsigned)cache->S;
+    int* const table_next = static_cast<int*>(workspace);
+    int* const length_next = table_next + (size_t)cache->S * cache->table_width;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    pasa_fork_out_k<<<grid, kCacheThreads, 0, s>>>(t, source, table_next, length_next, fast_div(chunks));
+    if (hipGetLastError() != hipSuccess) return PASA_ELAUNCH;
+    pasa_fork_in_k<<<grid, kCacheThreads, 0, s>>>(t, source, table_next, length_next, fast_div(chunks));
+    return launched();
+}
+
+int pasa_cache_free(const pasa_cache* cache, int* refs, void* stream)
+{
+    const int st = check(cache, refs);
+    if (st != PASA_OK) return st;
+    const unsigned chunks = entry_chunks(*cache);
+    pasa_free_k<<<chunks * (unsigned)cache->S, kCacheThreads, 0, static_cast<hipStream_t>(stream)>>>(tables_of(*cache, refs), fast_div(chunks));
+    return launched();
+}
+
+size_t pasa_cache_room_workspace(const pasa_cache* cache, int R) { return pasa_check_cache(cache) == PASA_OK && R > 0 ? room_bytes(*cache, R) : 0; }
+
+int pasa_cache_room(const pasa_cache* cache, int* refs, int R, const int* row_start, int* lacking, void* workspace, size_t workspace_bytes, void* stream)
+{
+    int st = check(cache, refs);
+    if (st != PASA_OK) return st;
+    if (R <= 0 || !buffer(row_start, 4) || !aligned(lacking, 4)) return PASA_EINVAL;
+    const CopyArgs c = copy_args(*cache, *cache);
+    if ((long long)cache->S * c.chunks > kMaxThreads / kCacheThreads) return PASA_EUNSUPPORTED;
+    st = check_workspace(workspace, workspace_bytes, room_bytes(*cache, R));
+    if (st != PASA_OK) return st;
+    RoomArgs a;
+    a.t = tables_of(*cache, refs);
+    a.row_start = row_start;
+    a.lacking = lacking;
+    a.begin = static_cast<int*>(workspace);
+    a.copies = a.begin + cache->S + 1;
+    a.free_pages = a.copies + 2 * (size_t)cache->S;
+    a.R = R;
+    a.most_free = most_free(*cache, R);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    pasa_room_k<<<1, kPlanThreads, 0, s>>>(a);
+    if (hipGetLastError() != hipSuccess) return PASA_ELAUNCH;
+    pasa_copy_pages_k<<<(unsigned)cache->S * c.chunks, kCacheThreads, 0, s>>>(c, a.copies, a.copies + cache->S, fast_div(c.chunks));
+    return launched();
+}
+
+size_t pasa_cache_compact_workspace(const pasa_cache* cache) { return pasa_check_cache(cache) == PASA_OK ? pack_bytes(*cache) : 0; }
+
+int pasa_cache_compact(const pasa_cache* cache, int* refs, int* used, void* workspace, size_t workspace_bytes, void* stream)
+{
+    int st = check(cache, refs);
+    if (st != PASA_OK) return st;
+    if (!aligned(used, 4)) return PASA_EINVAL;
+    st = check_workspace(workspace, workspace_bytes, pack_bytes(*cache));
+    if (st != PASA_OK) return st;
+    PackArgs a;
+    a.t = tables_of(*cache, refs);
+    a.used = used;
+    a.groups = pack_groups(*cache);
+    a.counts = static_cast<int*>(workspace);
+    a.header = a.counts + a.groups;
+    a.to = a.header + 2;
+    a.from = a.to + (size_t)cache->pages / 2 + 1;
+    a.rank = a.from + (size_t)cache->pages / 2 + 1;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (a.groups > 1) {
+        pasa_pack_count_k<<<(unsigned)a.groups, kPlanThreads, 0, s>>>(a);
+        if (hipGetLastError() != hipSuccess) return PASA_ELAUNCH;
+    }
+    pasa_pack_plan_k<<<(unsigned)a.groups, kPlanThreads, 0, s>>>(a);
+    if (hipGetLastError() != hipSuccess) return PASA_ELAUNCH;
+    const CopyArgs c = copy_args(*cache, *cache);
+    const unsigned entry_groups = (unsigned)(((long long)cache->S * cache->table_width + kCacheThreads - 1) / kCacheThreads);
+    pasa_pack_move_k<<<entry_groups + kCopyGroups, kCacheThreads, 0, s>>>(a, c, entry_groups);
+    return launched();
+}
+
+}  // extern "C"
