@@ -531,9 +531,13 @@ def prepare(c, seed):
                                        "waves": P.ROTARY_WAVES}[c["scaling"]],
                               factor=c["factor"], original=c["original"], slow=1.0, fast=4.0 if c["scaling"] == "waves" else 32.0, magnitude=c["magnitude"])
         if work != "rotate":
+            table = s["table"]
+            if table.shape[1] * c["page"] > 262144:             # the longest sequence has no room for a token more
+                table = table[:, :262144 // c["page"]].contiguous()
+
             def described(t, pages):
-                return P.pasa_cache(t["k"], t["v"], t["kscale"], t["vscale"], s["table"], s["length"], S=c["S"], Hkv=c["Hkv"], d=c["d"],
-                                    page=c["page"], pages=pages, table_width=s["table"].shape[1], format=P.CACHE_I4, kmean=t.get("kmean"),
+                return P.pasa_cache(t["k"], t["v"], t["kscale"], t["vscale"], table, s["length"], S=c["S"], Hkv=c["Hkv"], d=c["d"],
+                                    page=c["page"], pages=pages, table_width=table.shape[1], format=P.CACHE_I4, kmean=t.get("kmean"),
                                     kshift=s["kshift"] if c["shift"] else None)
             if work == "place":                                 # positions come from lengths alone: any buffers
                 s.update({n: torch.empty(64, dtype=torch.uint8, device=dev) for n in ("k", "v", "kscale", "vscale")})
