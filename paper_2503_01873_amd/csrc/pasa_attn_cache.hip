@@ -33,12 +33,21 @@ __device__ inline h2 widen2(unsigned w)
 // Eight codes of 4 bits -> (code - 8) * factor, exactly, as four pairs of fp16: elements i and i + 4.  A code put into bits 4 .. 7 of 64.0 adds itself; the products are whole
 // numbers of 11 bits, and so is 72 * factor over 8, so the multiply-add that takes the 8 off is exact.  1.4 instructions a value.
 __device__ inline h2 times72(h2 factor) { return factor * h2{(_Float16)-72, (_Float16)-72}; }
-template <int I>
-__device__ inline h2 widen4bit(unsigned w, h2 factor, h2 off)
-{
-    const unsigned x = I == 0 ? w << 4 : I == 1 ? w : I == 2 ? w >> 4 : w >> 8;
-    return __builtin_elementwise_fma(__builtin_bit_cast(h2, (x & 0x00f000f0u) | 0x54005400u), factor, off);
-}
+// (The two constants in registers, where one v_and_or_b32 takes both; as literals they would be two instructions.)
+struct Widen4 {
+    unsigned mask = 0x00f000f0u, sixty_four = 0x54005400u;
+    __device__ inline Widen4()
+    {
+        asm("" : "+s"(mask));
+        asm("" : "+v"(sixty_four));
+    }
+    template <int I>
+    __device__ inline h2 at(unsigned w, h2 factor, h2 off) const
+    {
+        const unsigned x = I == 0 ? w << 4 : I == 1 ? w : I == 2 ? w >> 4 : w >> 8;
+        return __builtin_elementwise_fma(__builtin_bit_cast(h2, (x & mask) | sixty_four), factor, off);
+    }
+};
 // Two bytes -> fp16: 1024 + byte, less 1024
 template <int I>
 __device__ inline h2 factors2(unsigned w)
@@ -546,6 +555,7 @@ void pasa_cache_rows(RowsArgs a)
             }
             auto Q = [&](int rb, int ks) { return QLDS ? lds_q[(rb * KS + ks) * 64 + lane] : Qr[rb][ks]; };
 
+            const Widen4 four;
             int n = 0;
             do {
                 const bool whole = __builtin_amdgcn_ballot_w64(page_now >= 0 && pos_now + 16 <= new0) == ~0ull;      // all rows see all keys of the unit
@@ -586,7 +596,7 @@ void pasa_cache_rows(RowsArgs a)
 #pragma unroll
                         for (int ks = 0; ks < KS; ++ks) {
                             const unsigned w = ks == 0 ? K[blk][0].x : ks == 1 ? K[blk][0].y : ks == 2 ? K[blk][0].z : K[blk][0].w;
-                            const h2 y[4] = {widen4bit<0>(w, factor, off), widen4bit<1>(w, factor, off), widen4bit<2>(w, factor, off), widen4bit<3>(w, factor, off)};
+                            const h2 y[4] = {four.at<0>(w, factor, off), four.at<1>(w, factor, off), four.at<2>(w, factor, off), four.at<3>(w, factor, off)};
                             h8 f;
 #pragma unroll
                             for (int e = 0; e < 4; ++e) f[2 * e] = y[e][0], f[2 * e + 1] = y[e][1];
@@ -709,8 +719,8 @@ void pasa_cache_rows(RowsArgs a)
                         h2 factor[4], off[4];    // of pairs of keys
 #pragma unroll
                         for (int e = 0; e < 4; e += 2) {
-                            const h4 four = *reinterpret_cast<const h4*>(lds_fv + lq / (16 / GROUPS) * kUnit + 32 * st + 8 * e + 4 * g);
-                            factor[e] = h2{four[0], four[1]}, factor[e + 1] = h2{four[2], four[3]};
+                            const h4 of = *reinterpret_cast<const h4*>(lds_fv + lq / (16 / GROUPS) * kUnit + 32 * st + 8 * e + 4 * g);
+                            factor[e] = h2{of[0], of[1]}, factor[e + 1] = h2{of[2], of[3]};
                         }
 #pragma unroll
                         for (int e = 0; e < 4; ++e) off[e] = times72(factor[e]);
@@ -724,7 +734,7 @@ void pasa_cache_rows(RowsArgs a)
                                 h8 f;
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) {
-                                    const h2 y = widen4bit<I>(two[e], factor[e], off[e]);
+                                    const h2 y = four.template at<I>(two[e], factor[e], off[e]);
                                     f[2 * e] = y[0];
                                     f[2 * e + 1] = y[1];
                                 }

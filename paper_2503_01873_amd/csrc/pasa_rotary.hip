@@ -12,8 +12,9 @@ namespace {
 
 constexpr int kMaxPairs = 64;
 constexpr int kThreads = 256;
-constexpr int kTokens = 4;                       // of a workgroup at most
-constexpr int kAtOnce = 4;                       // items of a thread whose loads are on their way together
+constexpr int kTokens = 32;                      // of a workgroup at most
+constexpr long long kStreamBytes = 32 << 20;     // of y: more than the L2s would keep
+constexpr int kAtOnce = 2;                       // heads of a thread that are on their way together
 
 // Where a call's tokens are and what their positions are made of.  A token is a row of `heads` heads; b its batch entry, n its number there.
 struct RotaryArgs {
@@ -26,12 +27,13 @@ struct RotaryArgs {
     const int* row_start;
     const unsigned long long* tree;
     int S, most;
-    int row0, tokens, heads, d, rot, io_bf16, pairs_layout;
-    int items, turned, each_heads;               // items of a head, those among them that are turned, heads of a workgroup
-    int each_tokens;                             // tokens of a workgroup
+    int row0, tokens, heads, rot, io_bf16;
+    int turned;                                  // items of a head that are turned
+    // A workgroup's threads: `items` of a head, times `lanes` heads at a time, times each_tokens tokens; and the heads of a workgroup
+    int items, lanes, each_tokens, each_heads;
     float sign;
     double magnitude;
-    FastDiv N, of_item, of_head, parts;
+    FastDiv N, of_item, of_lane, of_pair, parts;
     double freq[kMaxPairs];
 };
 
@@ -101,132 +103,118 @@ __device__ inline float widen(unsigned short raw, int io_bf16)
 }
 __device__ inline unsigned pack(float lo, float hi, int io_bf16) { return io_bf16 ? pack_bf16(lo, hi) : pack_f16(lo, hi); }
 
-// A workgroup takes up to four tokens and some of their heads: cos and sin once a token and pair, in 64 bits, into LDS; then the heads in items of 16 bytes a load,
-// four items of a thread on their way at a time, the first of them before the positions are known.
-// WIDE: items are eight channels (neighbouring pairs) or twice eight (halves); otherwise a pair of channels.
-template <bool PAIRS, bool WIDE>
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
+
+// A thread has an item of a token, 16 bytes (neighbouring pairs) or twice 16 (halves), and takes it of one head after the other: cos and sin, which a workgroup works out
+// once a token and pair, in 64 bits, stay in its registers.  Two heads of a thread are on their way at a time, the first ones before the positions are known.
+// WIDE: items are eight channels (neighbouring pairs) or twice eight (halves); otherwise a pair of channels.  CACHE: rows of a step.
+// STREAM: y is stored past the L2s.
+template <bool PAIRS, bool WIDE, bool CACHE, bool STREAM>
 __global__ __launch_bounds__(kThreads)
 void pasa_rotate_k(RotaryArgs a)
 {
-    __shared__ __attribute__((aligned(16))) float2 lds_cs[kTokens][kMaxPairs];
-    __shared__ int lds_there[kTokens];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    constexpr int CS = !WIDE ? 1 : PAIRS ? 4 : 8;        // pairs of an item
+    __shared__ __attribute__((aligned(16))) float2 lds_cs[kTokens * kMaxPairs];
+    __shared__ int lds_position[kTokens], lds_there[kTokens];
+    const int tid = threadIdx.x, half = a.rot / 2;
     const unsigned group = a.parts.quotient(blockIdx.x);
     const int h0 = (int)a.parts.rest(blockIdx.x, group) * a.each_heads;
     const int token0 = (int)group * a.each_tokens;
     const int tokens = a.tokens - token0 < a.each_tokens ? a.tokens - token0 : a.each_tokens;
-    const int heads = a.heads - h0 < a.each_heads ? a.heads - h0 : a.each_heads;
-    const int all = tokens * a.each_heads * a.items, half = a.rot / 2;
+    const int end = a.heads - h0 < a.each_heads ? a.heads : h0 + a.each_heads;
 
-    struct Item {
-        size_t x, y;
-        int token, item;
-        bool there;
-    };
-    auto item_at = [&](int i) {
-        Item m;
-        const unsigned up = a.of_item.quotient((unsigned)i);
-        m.item = (int)a.of_item.rest((unsigned)i, up);
-        m.token = (int)a.of_head.quotient(up);
-        const int h = (int)a.of_head.rest(up, (unsigned)m.token);
-        m.there = i < all && h < heads;
-        const int token = token0 + (m.there ? m.token : 0);
-        const long long b = (long long)a.N.quotient((unsigned)token), n = (long long)a.N.rest((unsigned)token, (unsigned)b);
-        const long long head = h0 + (m.there ? h : 0);
-        if (!m.there) m.token = 0, m.item = 0;
-        m.x = (size_t)(b * a.xs[0] + head * a.xs[1] + n * a.xs[2]);
-        m.y = (size_t)(b * a.ys[0] + head * a.ys[1] + n * a.ys[2]);
-        return m;
-    };
-    // channels of an item's first and second part
-    auto first_of = [&](int item) { return WIDE ? 8 * item + (PAIRS || item < a.turned ? 0 : a.rot - 8 * a.turned) : item < a.turned ? (PAIRS ? 2 * item : item) : a.rot + 2 * (item - a.turned); };
-    auto second_of = [&](int item) { return WIDE ? first_of(item) + half : item < a.turned && !PAIRS ? item + half : first_of(item) + 1; };
+    const unsigned up = a.of_item.quotient((unsigned)tid);
+    const int item = (int)a.of_item.rest((unsigned)tid, up);
+    const int t = (int)a.of_lane.quotient(up), lane = (int)a.of_lane.rest(up, (unsigned)t);
+    const bool there = t < tokens;
+    const unsigned token = (unsigned)(token0 + (there ? t : 0)), b = a.N.quotient(token), n = a.N.rest(token, b);
+    const bool turned = item < a.turned;
+    // channels of the item's first and second part
+    const int c0 = WIDE ? 8 * item + (PAIRS || turned ? 0 : a.rot - 8 * a.turned) : !turned ? a.rot + 2 * (item - a.turned) : PAIRS ? 2 * item : item;
+    const int c1 = WIDE ? (turned ? c0 + half : c0) : turned && !PAIRS ? c0 + half : c0 + 1;
+    const unsigned short* x = a.x + (long long)b * a.xs[0] + (long long)n * a.xs[2];
+    unsigned short* y = a.y + (long long)b * a.ys[0] + (long long)n * a.ys[2];
 
-    Item m[kAtOnce];
     u16x8 lo[kAtOnce], hi[kAtOnce];
-    auto load = [&](int base) {
+    auto load = [&](int h) {
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
-            m[j] = item_at(base + j * kThreads + tid);
-            const unsigned short* x = a.x + m[j].x;
+            const int at = h + j * a.lanes < end ? h + j * a.lanes : h0;         // a head again, for nothing
+            const unsigned short* from = x + (long long)at * a.xs[1];
             if constexpr (WIDE) {
-                lo[j] = *reinterpret_cast<const u16x8*>(x + first_of(m[j].item));
-                if (!PAIRS) hi[j] = *reinterpret_cast<const u16x8*>(x + (m[j].item < a.turned ? second_of(m[j].item) : first_of(m[j].item)));
+                lo[j] = *reinterpret_cast<const u16x8*>(from + c0);
+                if (!PAIRS) hi[j] = *reinterpret_cast<const u16x8*>(from + c1);
             } else {
-                lo[j][0] = x[first_of(m[j].item)];
-                hi[j][0] = x[second_of(m[j].item)];
+                lo[j][0] = from[c0];
+                hi[j][0] = from[c1];
             }
         }
     };
-    load(0);
-    for (int t = wave; t < tokens; t += kThreads / 64) {
-        int position = 0;
-        bool there = true;
-        const int token = token0 + t;
-        if (a.row_start != nullptr) there = place_of_row(a, token, position);
-        else if (a.positions != nullptr) position = a.positions[token];
-        else position = a.row0 + (int)a.N.rest((unsigned)token, a.N.quotient((unsigned)token));
-        if (lane < half) {
-            double c, s;
-            turn((double)position * a.freq[lane] * 0.159154943091895335769, c, s);
-            lds_cs[t][lane] = make_float2((float)(a.magnitude * c), a.sign * (float)(a.magnitude * s));
+    load(h0 + lane);
+    if constexpr (CACHE) {
+        for (int i = tid >> 6; i < tokens; i += kThreads / 64) {
+            int position = 0;
+            const bool found = place_of_row(a, token0 + i, position);
+            if ((tid & 63) == 0) lds_position[i] = position, lds_there[i] = found;
         }
-        if (lane == 0) lds_there[t] = there;
+        __syncthreads();
+    }
+    for (int i = tid; i < tokens * half; i += kThreads) {
+        const unsigned at = a.of_pair.quotient((unsigned)i), pair = a.of_pair.rest((unsigned)i, at);
+        const unsigned of = (unsigned)token0 + at;
+        int position;
+        if constexpr (CACHE) position = lds_position[at];
+        else position = a.positions != nullptr ? a.positions[of] : a.row0 + (int)a.N.rest(of, a.N.quotient(of));
+        double c, s;
+        turn((double)position * a.freq[pair] * 0.159154943091895335769, c, s);
+        lds_cs[at * kMaxPairs + pair] = make_float2((float)(a.magnitude * c), a.sign * (float)(a.magnitude * s));
     }
     __syncthreads();
-    for (int base = 0; base < all; base += kAtOnce * kThreads) {
-        if (base > 0) load(base);
+    if (!there || (CACHE && lds_there[t] == 0)) return;
+    float2 cs[CS];
+#pragma unroll
+    for (int i = 0; i < CS; ++i) cs[i] = lds_cs[t * kMaxPairs + (turned ? CS * item + i : 0)];
+    auto store = [&](unsigned short* at, u4 v) {
+        if (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<u4*>(at));
+        else *reinterpret_cast<u4*>(at) = v;
+    };
+    for (int h = h0 + lane; h < end; h += kAtOnce * a.lanes) {
+        if (h != h0 + lane) load(h);
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
-            if (!m[j].there || lds_there[m[j].token] == 0) continue;
-            unsigned short* y = a.y + m[j].y;
-            const int c0 = first_of(m[j].item), c1 = second_of(m[j].item);
-            const bool turned = m[j].item < a.turned;
-            if constexpr (WIDE && PAIRS) {
-                if (turned) {
-                    unsigned out[4];
+            if (h + j * a.lanes >= end) break;
+            unsigned short* to = y + (long long)(h + j * a.lanes) * a.ys[1];
+            if constexpr (!WIDE) {
+                const float p = widen(lo[j][0], a.io_bf16), q = widen(hi[j][0], a.io_bf16);
+                const unsigned out = pack(__builtin_fmaf(p, cs[0].x, -(q * cs[0].y)), __builtin_fmaf(q, cs[0].x, p * cs[0].y), a.io_bf16);
+                to[c0] = turned ? (unsigned short)out : lo[j][0];
+                to[c1] = turned ? (unsigned short)(out >> 16) : hi[j][0];
+            } else if (!turned) {
+                store(to + c0, __builtin_bit_cast(u4, lo[j]));
+            } else if constexpr (PAIRS) {
+                u4 out;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 cs = lds_cs[m[j].token][c0 / 2 + e];
-                        const float p = widen(lo[j][2 * e], a.io_bf16), q = widen(lo[j][2 * e + 1], a.io_bf16);
-                        out[e] = pack(__builtin_fmaf(p, cs.x, -(q * cs.y)), __builtin_fmaf(q, cs.x, p * cs.y), a.io_bf16);
-                    }
-                    *reinterpret_cast<uint4*>(y + c0) = make_uint4(out[0], out[1], out[2], out[3]);
-                } else {
-                    *reinterpret_cast<u16x8*>(y + c0) = lo[j];
+                for (int e = 0; e < 4; ++e) {
+                    const float p = widen(lo[j][2 * e], a.io_bf16), q = widen(lo[j][2 * e + 1], a.io_bf16);
+                    out[e] = pack(__builtin_fmaf(p, cs[e].x, -(q * cs[e].y)), __builtin_fmaf(q, cs[e].x, p * cs[e].y), a.io_bf16);
                 }
-            } else if constexpr (WIDE) {
-                if (turned) {
-                    unsigned out[2][4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float p[2], q[2];
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const float2 cs = lds_cs[m[j].token][c0 + 2 * e + i];
-                            const float u = widen(lo[j][2 * e + i], a.io_bf16), v = widen(hi[j][2 * e + i], a.io_bf16);
-                            p[i] = __builtin_fmaf(u, cs.x, -(v * cs.y));
-                            q[i] = __builtin_fmaf(v, cs.x, u * cs.y);
-                        }
-                        out[0][e] = pack(p[0], p[1], a.io_bf16);
-                        out[1][e] = pack(q[0], q[1], a.io_bf16);
-                    }
-                    *reinterpret_cast<uint4*>(y + c0) = make_uint4(out[0][0], out[0][1], out[0][2], out[0][3]);
-                    *reinterpret_cast<uint4*>(y + c1) = make_uint4(out[1][0], out[1][1], out[1][2], out[1][3]);
-                } else {
-                    *reinterpret_cast<u16x8*>(y + c0) = lo[j];
-                }
+                store(to + c0, out);
             } else {
-                if (turned) {
-                    const float2 cs = lds_cs[m[j].token][m[j].item];
-                    const float p = widen(lo[j][0], a.io_bf16), q = widen(hi[j][0], a.io_bf16);
-                    const unsigned out = pack(__builtin_fmaf(p, cs.x, -(q * cs.y)), __builtin_fmaf(q, cs.x, p * cs.y), a.io_bf16);
-                    y[c0] = (unsigned short)out;
-                    y[c1] = (unsigned short)(out >> 16);
-                } else {
-                    y[c0] = lo[j][0];
-                    y[c1] = hi[j][0];
+                u4 out[2];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float p[2], q[2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float u = widen(lo[j][2 * e + i], a.io_bf16), v = widen(hi[j][2 * e + i], a.io_bf16);
+                        p[i] = __builtin_fmaf(u, cs[2 * e + i].x, -(v * cs[2 * e + i].y));
+                        q[i] = __builtin_fmaf(v, cs[2 * e + i].x, u * cs[2 * e + i].y);
+                    }
+                    out[0][e] = pack(p[0], p[1], a.io_bf16);
+                    out[1][e] = pack(q[0], q[1], a.io_bf16);
                 }
+                store(to + c0, out[0]);
+                store(to + c1, out[1]);
             }
         }
     }
@@ -246,31 +234,55 @@ int check_rotary(const pasa_rotary* r, int d, int transposed, int io_dtype)
 }
 
 // The rest of the arguments, and the launch
-int launch(RotaryArgs& a, const pasa_rotary* r, int transposed, int io_dtype, bool in_place, hipStream_t stream)
+int launch(RotaryArgs& a, const pasa_rotary* r, int d, int transposed, int io_dtype, bool in_place, hipStream_t stream)
 {
     a.rot = r->rot;
     a.io_bf16 = io_dtype == PASA_IO_BF16;
-    a.pairs_layout = r->layout == PASA_ROTARY_PAIRS;
     a.sign = transposed ? -1.f : 1.f;
     a.magnitude = r->magnitude;
     for (int i = 0; i < a.rot / 2; ++i) a.freq[i] = r->freq[i];
+    const bool pairs = r->layout == PASA_ROTARY_PAIRS, cache = a.row_start != nullptr;
     // Items of eight channels where pairs keep to them.
-    const bool wide = a.pairs_layout ? a.rot % 8 == 0 : a.rot % 16 == 0;
-    a.turned = !wide ? a.rot / 2 : a.pairs_layout ? a.rot / 8 : a.rot / 16;
-    a.items = a.turned + (in_place ? 0 : (a.d - a.rot) / (wide ? 8 : 2));
-    // Four tokens a workgroup where that leaves every compute unit several workgroups, with heads for four to eight items a thread; otherwise one, with an item a thread.
-    const long long total = (long long)a.tokens * a.heads * a.items;
-    a.each_tokens = total >= 8LL * 256 * kThreads * kAtOnce ? kTokens : 1;
-    const int target = (a.each_tokens == 1 ? 1 : 2 * kAtOnce) * kThreads / (a.each_tokens * a.items);
-    a.each_heads = target < 1 ? 1 : target < a.heads ? target : a.heads;
+    const bool wide = a.rot % (pairs ? 8 : 16) == 0;
+    a.turned = !wide ? a.rot / 2 : pairs ? a.rot / 8 : a.rot / 16;
+    a.items = a.turned + (in_place ? 0 : (d - a.rot) / (wide ? 8 : 2));
+    // Heads at a time: so that a thread takes two or three of them, where there are workgroups enough for that, and few threads are left over; one each otherwise.
+    const int groups = kThreads / a.items;
+    const long long threads = (long long)a.tokens * a.heads * a.items;
+    const int most_tokens = cache ? 4 : kTokens;
+    if (threads >= 4LL * kAtOnce * kThreads * 256) {
+        long best = -1;
+        for (int lanes = 1; lanes <= groups && lanes <= a.heads; ++lanes) {
+            const int turns = (a.heads + lanes - 1) / lanes;
+            const int tokens = groups / lanes < most_tokens ? groups / lanes : most_tokens;
+            const int used = turns < kAtOnce ? kAtOnce : turns;          // a thread of fewer waits as long
+            const long worth = 4096L * tokens * a.heads / used;
+            if (worth > best && (turns < 2 * kAtOnce || lanes == groups)) best = worth, a.lanes = lanes, a.each_tokens = tokens;
+        }
+        a.each_heads = (a.heads + a.lanes - 1) / a.lanes * a.lanes;
+        if (a.each_heads > 2 * kAtOnce * a.lanes) a.each_heads = 2 * kAtOnce * a.lanes;
+    } else {
+        a.lanes = groups < a.heads ? groups : a.heads;
+        a.each_tokens = groups / a.lanes < most_tokens ? groups / a.lanes : most_tokens;
+        a.each_heads = a.lanes;
+    }
     const long long parts = (a.heads + a.each_heads - 1) / a.each_heads, grid = ((long long)a.tokens + a.each_tokens - 1) / a.each_tokens * parts;
     if (grid * kThreads > 0xffffffffLL) return PASA_EUNSUPPORTED;
     a.of_item = fast_div((unsigned)a.items);
-    a.of_head = fast_div((unsigned)a.each_heads);
+    a.of_lane = fast_div((unsigned)a.lanes);
+    a.of_pair = fast_div((unsigned)a.rot / 2);
     a.parts = fast_div((unsigned)parts);
     auto go = [&](auto kernel) { kernel<<<(unsigned)grid, kThreads, 0, stream>>>(a); };
-    if (a.pairs_layout) wide ? go(pasa_rotate_k<true, true>) : go(pasa_rotate_k<true, false>);
-    else wide ? go(pasa_rotate_k<false, true>) : go(pasa_rotate_k<false, false>);
+    auto of_layout = [&](auto p, auto w) {
+        constexpr bool P = decltype(p)::value, W = decltype(w)::value;
+        if (cache) go(pasa_rotate_k<P, W, true, false>);
+        else if (W && threads * (P ? 16 : 32) > kStreamBytes) go(pasa_rotate_k<P, W, false, W>);
+        else go(pasa_rotate_k<P, W, false, false>);
+    };
+    using yes = std::true_type;
+    using no = std::false_type;
+    if (pairs) wide ? of_layout(yes{}, yes{}) : of_layout(yes{}, no{});
+    else wide ? of_layout(no{}, yes{}) : of_layout(no{}, no{});
     return hipGetLastError() == hipSuccess ? PASA_OK : PASA_ELAUNCH;
 }
 
@@ -342,9 +354,8 @@ int pasa_rotate(const pasa_rotary* rotary, const void* x, void* y, int B, int H,
     a.row0 = row0;
     a.tokens = B * N;
     a.heads = H;
-    a.d = d;
     a.N = fast_div((unsigned)N);
-    return launch(a, rotary, transposed, io_dtype, x == y, static_cast<hipStream_t>(stream));
+    return launch(a, rotary, d, transposed, io_dtype, x == y, static_cast<hipStream_t>(stream));
 }
 
 int pasa_cache_rotate(const pasa_cache* cache, const pasa_rotary* rotary, const void* x, void* y, int heads, int R, long long x_stride, long long y_stride,
@@ -371,9 +382,8 @@ int pasa_cache_rotate(const pasa_cache* cache, const pasa_rotary* rotary, const 
     a.most = cache->table_width * cache->page;
     a.tokens = R;
     a.heads = heads;
-    a.d = cache->d;
     a.N = fast_div((unsigned)R);
-    return launch(a, rotary, transposed, io_dtype, x == y, static_cast<hipStream_t>(stream));
+    return launch(a, rotary, cache->d, transposed, io_dtype, x == y, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"
