@@ -30,31 +30,27 @@ __device__ inline h2 widen2(unsigned w)
     }
 }
 
-// Eight codes of 4 bits -> (code - 8) * factor, exactly, as four pairs of fp16: elements i and i + 4.  A code put into bits 4 .. 7 of 64.0 adds itself; the products are whole
-// numbers of 11 bits, and so is 72 * factor over 8, so the multiply-add that takes the 8 off is exact.  1.4 instructions a value.
-__device__ inline h2 times72(h2 factor) { return factor * h2{(_Float16)-72, (_Float16)-72}; }
-// (The two constants in registers, where one v_and_or_b32 takes both; as literals they would be two instructions.)
-struct Widen4 {
-    unsigned mask = 0x00f000f0u, sixty_four = 0x54005400u;
-    __device__ inline Widen4()
-    {
-        asm("" : "+s"(mask));
-        asm("" : "+v"(sixty_four));
-    }
+// Codes of 4 bits -> (code - 8) * factor * 2^-16, exactly, two at a time.  A code in bits 0 .. 3 of an fp16 number is code 2^-24 as it lies there, in bits 4 .. 7 code 2^-20 (both
+// below the normal numbers); one multiply-add by factor 2^8, or 2^4, takes 8 factor 2^-16 off.  Results are whole multiples of 2^-16 of 11 bits.  So a word of eight takes a
+// shift, four masks and four multiply-adds (put into 64.0 by an or, all in bits 4 .. 7: two shifts more).
+constexpr float kTiny = 0x1p-16f;
+struct Factor4 {
+    h2 low, high, off;                           // of codes in bits 0 .. 3, in bits 4 .. 7
+    __device__ inline explicit Factor4(h2 f) : low(f), high(f * h2{(_Float16)0x1p-4, (_Float16)0x1p-4}), off(f * h2{(_Float16)-0x1p-21, (_Float16)-0x1p-21}) {}
     template <int I>
-    __device__ inline h2 at(unsigned w, h2 factor, h2 off) const
+    __device__ inline h2 widen(unsigned w) const
     {
-        const unsigned x = I == 0 ? w << 4 : I == 1 ? w : I == 2 ? w >> 4 : w >> 8;
-        return __builtin_elementwise_fma(__builtin_bit_cast(h2, (x & mask) | sixty_four), factor, off);
+        const unsigned x = I < 2 ? w : w >> 8;
+        return __builtin_elementwise_fma(__builtin_bit_cast(h2, x & (I % 2 == 0 ? 0x000f000fu : 0x00f000f0u)), I % 2 == 0 ? low : high, off);
     }
 };
-// Two bytes -> fp16: 1024 + byte, less 1024
+// Two bytes -> fp16 times 2^8: 1024 + byte, less 1024
 template <int I>
 __device__ inline h2 factors2(unsigned w)
 {
-    return __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w, I == 0 ? 0x04010400u : 0x04030402u)) - h2{(_Float16)1024, (_Float16)1024};
+    const h2 x = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w, I == 0 ? 0x04010400u : 0x04030402u)) - h2{(_Float16)1024, (_Float16)1024};
+    return x * h2{(_Float16)256, (_Float16)256};
 }
-
 typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 
 struct RowsArgs {
@@ -555,13 +551,12 @@ void pasa_cache_rows(RowsArgs a)
             }
             auto Q = [&](int rb, int ks) { return QLDS ? lds_q[(rb * KS + ks) * 64 + lane] : Qr[rb][ks]; };
 
-            const Widen4 four;
             int n = 0;
             do {
                 const bool whole = __builtin_amdgcn_ballot_w64(page_now >= 0 && pos_now + 16 <= new0) == ~0ull;      // all rows see all keys of the unit
                 const bool vs_one = vs_raw == 1.f;
                 // per key: what its score is multiplied by, log2 of the value's scale and kSum over it; in the lanes' order of keys
-                key_f[lane] = ks_raw * a.scale2;
+                key_f[lane] = ks_raw * (I4 ? a.scale2 / kTiny : a.scale2);
                 key_f[kUnit + lane] = __builtin_amdgcn_logf(vs_raw);
                 // finite, so that 0 times it is 0: a key that is not there may have any scale, and a NaN shows in the score of the rows that see it
                 key_f[2 * kUnit + lane] = kSum * __builtin_fminf(__builtin_fmaxf(__builtin_amdgcn_rcpf(vs_raw), 0.f), 3e38f);
@@ -592,11 +587,11 @@ void pasa_cache_rows(RowsArgs a)
                 if constexpr (I4) {
 #pragma unroll
                     for (int blk = 0; blk < 4; ++blk) {
-                        const h2 factor = lds_fk[(GROUPS == 4 ? g : g >> 1) * KLD + 16 * blk + lq], off = times72(factor);
+                        const Factor4 factor(lds_fk[(GROUPS == 4 ? g : g >> 1) * KLD + 16 * blk + lq]);
 #pragma unroll
                         for (int ks = 0; ks < KS; ++ks) {
                             const unsigned w = ks == 0 ? K[blk][0].x : ks == 1 ? K[blk][0].y : ks == 2 ? K[blk][0].z : K[blk][0].w;
-                            const h2 y[4] = {four.at<0>(w, factor, off), four.at<1>(w, factor, off), four.at<2>(w, factor, off), four.at<3>(w, factor, off)};
+                            const h2 y[4] = {factor.widen<0>(w), factor.widen<1>(w), factor.widen<2>(w), factor.widen<3>(w)};
                             h8 f;
 #pragma unroll
                             for (int e = 0; e < 4; ++e) f[2 * e] = y[e][0], f[2 * e + 1] = y[e][1];
@@ -716,14 +711,11 @@ void pasa_cache_rows(RowsArgs a)
                 if constexpr (I4) {
 #pragma unroll
                     for (int st = 0; st < 2; ++st) {
-                        h2 factor[4], off[4];    // of pairs of keys
-#pragma unroll
-                        for (int e = 0; e < 4; e += 2) {
-                            const h4 of = *reinterpret_cast<const h4*>(lds_fv + lq / (16 / GROUPS) * kUnit + 32 * st + 8 * e + 4 * g);
-                            factor[e] = h2{of[0], of[1]}, factor[e + 1] = h2{of[2], of[3]};
-                        }
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) off[e] = times72(factor[e]);
+                        const _Float16* const of = lds_fv + lq / (16 / GROUPS) * kUnit + 32 * st + 4 * g;
+                        const h4 first = *reinterpret_cast<const h4*>(of), second = *reinterpret_cast<const h4*>(of + 16);
+                        // of pairs of keys
+                        const Factor4 factor[4] = {Factor4(h2{first[0], first[1]}), Factor4(h2{first[2], first[3]}), Factor4(h2{second[0], second[1]}),
+                                                   Factor4(h2{second[2], second[3]})};
 #pragma unroll
                         for (int half = 0; half < D / 64; ++half) {
                             unsigned two[4];     // four channels of a pair of keys
@@ -734,7 +726,7 @@ void pasa_cache_rows(RowsArgs a)
                                 h8 f;
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) {
-                                    const h2 y = four.template at<I>(two[e], factor[e], off[e]);
+                                    const h2 y = factor[e].template widen<I>(two[e]);
                                     f[2 * e] = y[0];
                                     f[2 * e + 1] = y[1];
                                 }
@@ -780,6 +772,12 @@ void pasa_cache_rows(RowsArgs a)
         }
 
         // ---- the wavefronts' states brought to the highest of their levels and added ----
+        if constexpr (I4) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) O[rb][cb] *= 1.f / kTiny;
+        }
         int ln = lane;
         asm volatile("" : "+v"(ln));             // no address is to be worked out before the main loop and kept through it
 #pragma unroll
