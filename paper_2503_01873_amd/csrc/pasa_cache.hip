@@ -103,7 +103,7 @@ __device__ inline float nearest(float x, float unit, float inverse)
 
 // Eight values of a token -> eight codes of 4 bits, and the numbers factor * code that they hold.  top: the largest magnitude of the token, NaN where one is; of_group: that
 // of the 32 channels that the factor is for.  All of it exact: scale has 8 significant bits, factor 8, code 3 and a half 4, so that limits are products
-// that fp32 holds.
+// that fp32 holds.  Codes from products with 1 / unit, off by 2^-18 at most, unless one of the wavefront is next to a tie.
 __device__ inline unsigned encode4(const float (&x)[8], float top, float of_group, float& scale, unsigned& factor, float (&held)[8])
 {
     const bool finite = top < __builtin_inff();
@@ -116,16 +116,30 @@ __device__ inline unsigned encode4(const float (&x)[8], float top, float of_grou
     if (!finite) scale = __builtin_nanf(""), m = 1.f;
     factor = (unsigned)m;
     const float unit = m * scale, inverse = __builtin_amdgcn_rcpf(unit);
-    unsigned word = 0x88888888u;
-    if (finite) {
-        word = 0u;
+    constexpr float shift = 12582912.f + 8.f;    // 1.5 2^23: a sum with it is rounded to whole numbers, and its low bits are number + 8
+    float q[8], off = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float y = __builtin_amdgcn_fmed3f(x[i] * inverse, -7.f, 7.f);
+        q[i] = y + shift;
+        held[i] = q[i] - shift;
+        off = __builtin_fmaxf(off, __builtin_fabsf(y - held[i]));
+    }
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(off > 0.5f - 0x1p-15f && finite) != 0ull, 0)) {     // next to a tie somewhere
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float n = __builtin_fminf(__builtin_fmaxf(nearest(x[i], unit, inverse), -7.f), 7.f);
-            held[i] = n * m;
-            word |= (unsigned)((int)n + 8) << (4 * i);
+            held[i] = __builtin_amdgcn_fmed3f(nearest(x[i], unit, inverse), -7.f, 7.f);
+            q[i] = held[i] + shift;
         }
-    } else {
+    }
+    unsigned word = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        word |= (__float_as_uint(q[i]) & 15u) << (4 * i);
+        held[i] *= m;
+    }
+    if (!finite) {
+        word = 0x88888888u;
 #pragma unroll
         for (int i = 0; i < 8; ++i) held[i] = 0.f;
     }

@@ -12,18 +12,20 @@ namespace {
 constexpr int kPlanThreads = 1024;               // of the workgroups that look through holders
 constexpr int kEach = 16;                        // holders of a thread at a time
 constexpr int kSpan = kPlanThreads * kEach;      // of a workgroup
-constexpr int kCopyAtOnce = 4;                   // 16-byte units of a thread that are on their way together
-constexpr int kCopyUnits = kCacheThreads * kCopyAtOnce;
-constexpr int kCopyGroups = 2048;                // workgroups of a copy whose length only the device knows
+constexpr int kCopyAtOnce = 2;                   // chunks of a workgroup that are on their way together
+constexpr int kCopyGroups = 8192;                // workgroups of a copy whose length only the device knows
 
 // ---- copies ----
 
-// A page is up to five stretches of memory, whole heads behind one another: codes, scales, the mean.  `ends` counts 16-byte units up to and with each.
+// A page is up to five stretches of memory, whole heads behind one another: codes, scales, the mean.  Each is cut into chunks of 4 KiB, 16 bytes a thread, the last of them
+// shorter: what a chunk is goes through the scalar unit.  `ends` counts chunks up to and with each stretch, `units` its 16-byte units.
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
 struct CopyArgs {
-    const uint4* from[5];
-    uint4* to[5];
-    unsigned ends[5], chunks;                    // chunks: of kCopyUnits, of a page
+    const u4* from[5];
+    u4* to[5];
+    unsigned ends[5], units[5];
     int pages_from, pages_to;
+    FastDiv chunks;                              // of a page
 };
 
 CopyArgs copy_args(const pasa_cache& to, const pasa_cache& from)
@@ -36,50 +38,52 @@ CopyArgs copy_args(const pasa_cache& to, const pasa_cache& from)
     void* at[5] = {to.k, to.v, to.kscale, to.vscale, to.kmean};
     unsigned end = 0;
     for (int i = 0; i < 5; ++i) {
-        a.from[i] = static_cast<const uint4*>(of[i]);
-        a.to[i] = static_cast<uint4*>(at[i]);
-        a.ends[i] = end += size[i];
+        a.from[i] = static_cast<const u4*>(of[i]);
+        a.to[i] = static_cast<u4*>(at[i]);
+        a.units[i] = size[i];
+        a.ends[i] = end += (size[i] + kCacheThreads - 1) / kCacheThreads;
     }
-    a.chunks = (end + kCopyUnits - 1) / kCopyUnits;
     a.pages_from = from.pages;
     a.pages_to = to.pages;
+    a.chunks = fast_div(end);
     return a;
 }
 
-__device__ inline void copy_chunk(const CopyArgs& a, int from, int to, unsigned chunk)
+// Chunks first .. first + kCopyAtOnce - 1 of `all`, pair_of giving the pages of a pair (a page outside its pool: nothing to be done).  All loads go out before the first store.
+// Stores go past the L2s, which would have to bring what they hold to memory before the kernel ends: half of 8400 pages of 37 KB packed, 82 MB, in 39.2 us with the plan, through them
+// 60.5 (one to eight chunks at once 39 to 41.6, 1024 workgroups in place of 8192 44.4).
+template <class PairOf>
+__device__ inline void copy_chunks(const CopyArgs& a, unsigned first, unsigned all, PairOf pair_of)
 {
-    uint4 x[kCopyAtOnce];
-    uint4* dst[kCopyAtOnce];
+    u4 x[kCopyAtOnce];
+    u4* dst[kCopyAtOnce];
+    unsigned size[kCopyAtOnce];
 #pragma unroll
     for (int j = 0; j < kCopyAtOnce; ++j) {
-        const unsigned unit = chunk * kCopyUnits + j * kCacheThreads + threadIdx.x;
-        const uint4* src = nullptr;
-        dst[j] = nullptr;
-        unsigned begin = 0;
-#pragma unroll
-        for (int i = 0; i < 5; ++i) {
-            const unsigned size = a.ends[i] - begin;
-            if (unit >= begin && unit < a.ends[i]) {
-                src = a.from[i] + (size_t)(unsigned)from * size + (unit - begin);
-                dst[j] = a.to[i] + (size_t)(unsigned)to * size + (unit - begin);
-            }
-            begin = a.ends[i];
-        }
-        if (src != nullptr) x[j] = *src;
+        const unsigned chunk = first + j < all ? first + j : all - 1;
+        const unsigned pair = a.chunks.quotient(chunk), c = a.chunks.rest(chunk, pair);
+        int from, to;
+        pair_of(pair, from, to);
+        const bool in = from >= 0 && from < a.pages_from && to >= 0 && to < a.pages_to;
+        int i = 0;
+        while (i < 4 && c >= a.ends[i]) ++i;
+        const unsigned units = a.units[i], at = (c - (i > 0 ? a.ends[i - 1] : 0u)) * kCacheThreads;
+        const unsigned left = units - at < kCacheThreads ? units - at : kCacheThreads;
+        const unsigned mine = at + (threadIdx.x < left ? threadIdx.x : left - 1);
+        x[j] = a.from[i][(size_t)(unsigned)(in ? from : 0) * units + mine];
+        dst[j] = a.to[i] + (size_t)(unsigned)(in ? to : 0) * units + mine;
+        size[j] = in && first + j < all ? left : 0u;
     }
 #pragma unroll
     for (int j = 0; j < kCopyAtOnce; ++j)
-        if (dst[j] != nullptr) *dst[j] = x[j];
+        if (threadIdx.x < size[j]) __builtin_nontemporal_store(x[j], dst[j]);
 }
 
-// Pair blockIdx / chunks of two lists
+// Pairs of two lists
 __global__ __launch_bounds__(kCacheThreads)
-void pasa_copy_pages_k(CopyArgs a, const int* __restrict__ from_pages, const int* __restrict__ to_pages, FastDiv chunks)
+void pasa_copy_pages_k(CopyArgs a, const int* __restrict__ from_pages, const int* __restrict__ to_pages, unsigned all)
 {
-    const unsigned pair = chunks.quotient(blockIdx.x);
-    const int from = from_pages[pair], to = to_pages[pair];
-    if (from < 0 || from >= a.pages_from || to < 0 || to >= a.pages_to) return;
-    copy_chunk(a, from, to, chunks.rest(blockIdx.x, pair));
+    copy_chunks(a, blockIdx.x * kCopyAtOnce, all, [&](unsigned pair, int& from, int& to) { from = from_pages[pair], to = to_pages[pair]; });
 }
 
 // ---- sequences go on as others ----
@@ -125,6 +129,43 @@ void pasa_fork_in_k(Tables t, const int* __restrict__ source, const int* __restr
     if (in_pool(t, page)) atomicAdd(t.refs + page, 1);
 }
 
+// Both in one launch of one workgroup, for tables of few entries.
+constexpr long long kForkEntries = 8 * kPlanThreads;
+__global__ __launch_bounds__(kPlanThreads)
+void pasa_fork_small_k(Tables t, const int* __restrict__ source, FastDiv width)
+{
+    constexpr int EACH = (int)(kForkEntries / kPlanThreads);
+    const int entries = t.S * t.width;
+    int at[EACH], b[EACH], p[EACH], from[EACH], length[EACH], next[EACH], old[EACH];
+    // step by step for all of a thread's entries, without branches between: what is not there stands for the last entry
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        at[i] = i * kPlanThreads + (int)threadIdx.x < entries ? i * kPlanThreads + (int)threadIdx.x : entries - 1;
+        b[i] = (int)width.quotient((unsigned)at[i]);
+        p[i] = (int)width.rest((unsigned)at[i], (unsigned)b[i]);
+        from[i] = source[b[i]];
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const bool ends = from[i] < 0 || from[i] >= t.S;
+        length[i] = length_of(t, ends ? b[i] : from[i]);
+        next[i] = t.table[(size_t)(ends ? b[i] : from[i]) * t.width + p[i]];
+        old[i] = t.table[at[i]];
+        if (ends) length[i] = 0;
+    }
+    __syncthreads();                             // all have read
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        if (i * kPlanThreads + (int)threadIdx.x >= entries || from[i] == b[i]) continue;
+        if (p[i] >= (length[i] + t.page - 1) >> t.page_log2) next[i] = -1;
+        t.table[at[i]] = next[i];
+        if (p[i] == 0) t.length[b[i]] = length[i];
+        if (old[i] == next[i]) continue;
+        if (in_pool(t, old[i])) atomicSub(t.refs + old[i], 1);
+        if (in_pool(t, next[i])) atomicAdd(t.refs + next[i], 1);
+    }
+}
+
 // Pages behind the lengths are let go of.
 __global__ __launch_bounds__(kCacheThreads)
 void pasa_free_k(Tables t, FastDiv chunks)
@@ -138,6 +179,25 @@ void pasa_free_k(Tables t, FastDiv chunks)
 }
 
 // ---- room for rows ----
+
+// Bit i: whether page p + i is in use
+__device__ inline unsigned in_use(const Tables& t, int p)
+{
+    unsigned live = 0;
+#pragma unroll
+    for (int i = 0; i < kEach / 4; ++i) {
+        int4 x = make_int4(0, 0, 0, 0);
+        if (p + 4 * i + 3 < t.pages) {
+            x = *reinterpret_cast<const int4*>(t.refs + p + 4 * i);
+        } else {
+            if (p + 4 * i < t.pages) x.x = t.refs[p + 4 * i];
+            if (p + 4 * i + 1 < t.pages) x.y = t.refs[p + 4 * i + 1];
+            if (p + 4 * i + 2 < t.pages) x.z = t.refs[p + 4 * i + 2];
+        }
+        live |= (unsigned)((x.x != 0) | (x.y != 0) << 1 | (x.z != 0) << 2 | (x.w != 0) << 3) << (4 * i);
+    }
+    return live;
+}
 
 // Sum over the threads of a workgroup before one's own, and over all
 template <int NT>
@@ -173,33 +233,43 @@ struct RoomArgs {
     int* free_pages;                             // [most_free]
     int R, most_free;
 };
+// In most steps nobody needs a page: every place has one, whose count was 1 when it was let go of.  That is known after one trip to the counts.
 __global__ __launch_bounds__(kPlanThreads)
 void pasa_room_k(RoomArgs a)
 {
     constexpr int NT = kPlanThreads;
     __shared__ unsigned sums[NT / 64];
+    __shared__ int lds_begin[NT + 1], lds_first[NT];
     const int tid = threadIdx.x;
     const Tables& t = a.t;
     const int most = t.width << t.page_log2;
+    const bool in_lds = t.S <= NT;               // what is kept of the sequences; otherwise in the workspace, and read again
     auto first_token = [&](const Sequence& s) { return s.length > s.rows ? s.length - s.rows : 0; };
 
     unsigned total = 0;
     for (int b0 = 0; b0 < t.S; b0 += NT) {
         const int b = b0 + tid;
         unsigned places = 0;
+        int first = 0;
         if (b < t.S) {
             const Sequence s = sequence_at(t.length, a.row_start, b, a.R, most);
-            if (s.rows > 0 && s.length > 0) places = (unsigned)(((s.length - 1) >> t.page_log2) - (first_token(s) >> t.page_log2) + 1);
+            first = first_token(s);
+            if (s.rows > 0 && s.length > 0) places = (unsigned)(((s.length - 1) >> t.page_log2) - (first >> t.page_log2) + 1);
+            a.copies[b] = -1;
         }
         unsigned all;
         const unsigned before = scan_workgroup<NT>(places, sums, all);
-        if (b < t.S) {
+        if (in_lds) {
+            if (b < t.S) lds_begin[b] = (int)before, lds_first[b] = first;
+        } else if (b < t.S) {
             a.begin[b] = (int)(total + before);
-            a.copies[b] = -1;
         }
         total += all;
     }
-    if (tid == 0) a.begin[t.S] = (int)total;
+    if (tid == 0) {
+        if (in_lds) lds_begin[t.S] = (int)total;
+        else a.begin[t.S] = (int)total;
+    }
     __syncthreads();
 
     struct Place {
@@ -208,17 +278,17 @@ void pasa_room_k(RoomArgs a)
         int place, page;                         // the page that is there, or -1
     };
     auto place_of = [&](unsigned i) {
+        auto begin = [&](int b) { return in_lds ? lds_begin[b] : a.begin[b]; };
         int low = 0, high = t.S;                 // the last sequence whose places begin at i or before, and that has some
         while (high - low > 1) {
             const int middle = (low + high) / 2;
-            if ((unsigned)a.begin[middle] <= i) low = middle;
+            if ((unsigned)begin(middle) <= i) low = middle;
             else high = middle;
         }
-        const Sequence s = sequence_at(t.length, a.row_start, low, a.R, most);
         Place p;
         p.b = low;
-        p.first = first_token(s);
-        p.place = clamp_int((p.first >> t.page_log2) + (int)(i - (unsigned)a.begin[low]), 0, t.width - 1);
+        p.first = in_lds ? lds_first[low] : first_token(sequence_at(t.length, a.row_start, low, a.R, most));
+        p.place = clamp_int((p.first >> t.page_log2) + (int)(i - (unsigned)begin(low)), 0, t.width - 1);
         p.at = (size_t)low * t.width + p.place;
         const int page = t.table[p.at];
         p.page = in_pool(t, page) ? page : -1;
@@ -229,44 +299,37 @@ void pasa_room_k(RoomArgs a)
     if (few && (unsigned)tid < total) mine = place_of(tid);
     auto place_at = [&](unsigned i) { return few ? mine : place_of(i); };
 
+    bool alone = true;
     for (unsigned i = tid; i < total; i += NT) {
         const Place p = place_at(i);
-        if (p.page >= 0) atomicSub(t.refs + p.page, 1);
+        if (p.page < 0 || atomicSub(t.refs + p.page, 1) != 1) alone = false;
     }
-    __syncthreads();
+    if (__syncthreads_and(alone)) {
+        for (unsigned i = tid; i < total; i += NT) t.refs[place_at(i).page] = 1;
+        if (tid == 0 && a.lacking != nullptr) *a.lacking = 0;
+        return;
+    }
     for (unsigned i = tid; i < total; i += NT) {
         const Place p = place_at(i);
         if (p.page >= 0 && holders(t.refs, p.page) <= 0) atomicMin(t.refs + p.page, -(p.b + 1));
     }
     __syncthreads();
     auto needs = [&](const Place& p) { return p.page < 0 || holders(t.refs, p.page) != -(p.b + 1); };
+    bool my_need = false;                        // where there are few: looked up once, before anything is written
+    if (few && (unsigned)tid < total) my_need = needs(mine);
     unsigned wanted = 0;
     for (unsigned i0 = 0; i0 < total; i0 += NT) {
         const unsigned i = i0 + tid;
         unsigned all;
-        scan_workgroup<NT>(i < total && needs(place_at(i)) ? 1u : 0u, sums, all);
+        scan_workgroup<NT>(i < total && (few ? my_need : needs(place_at(i))) ? 1u : 0u, sums, all);
         wanted += all;
     }
     unsigned found = 0;
     const unsigned enough = wanted < (unsigned)a.most_free ? wanted : (unsigned)a.most_free;
     for (int p0 = 0; p0 < t.pages && found < enough; p0 += kSpan) {
         const int p = p0 + tid * kEach;
-        unsigned free = 0;                       // bits
-        int4 x[kEach / 4];
-#pragma unroll
-        for (int i = 0; i < kEach / 4; ++i) {
-            x[i] = make_int4(1, 1, 1, 1);
-            if (p + 4 * i + 3 < t.pages) {
-                x[i] = *reinterpret_cast<const int4*>(t.refs + p + 4 * i);
-            } else {
-                if (p + 4 * i < t.pages) x[i].x = t.refs[p + 4 * i];
-                if (p + 4 * i + 1 < t.pages) x[i].y = t.refs[p + 4 * i + 1];
-                if (p + 4 * i + 2 < t.pages) x[i].z = t.refs[p + 4 * i + 2];
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < kEach / 4; ++i)
-            free |= (unsigned)((x[i].x == 0) | (x[i].y == 0) << 1 | (x[i].z == 0) << 2 | (x[i].w == 0) << 3) << (4 * i);
+        const int there = t.pages - p < kEach ? t.pages - p : kEach;             // pages of this thread
+        unsigned free = there > 0 ? ~in_use(t, p) & ((1u << there) - 1u) : 0u;
         unsigned all, rank = found + scan_workgroup<NT>((unsigned)__builtin_popcount(free), sums, all);
         for (; free != 0 && rank < enough; free &= free - 1) a.free_pages[rank++] = p + __builtin_ctz(free);
         found += all;
@@ -280,7 +343,7 @@ void pasa_room_k(RoomArgs a)
         bool need = false;
         if (i < total) {
             p = place_at(i);
-            need = needs(p);
+            need = few ? my_need : needs(p);
         }
         unsigned all;
         const unsigned rank = given + scan_workgroup<NT>(need ? 1u : 0u, sums, all);
@@ -314,25 +377,6 @@ struct PackArgs {
     int* rank;                                   // [pages] which of those a page is, or -1
     int groups;
 };
-
-// Bit i: whether page p + i is in use
-__device__ inline unsigned in_use(const Tables& t, int p)
-{
-    unsigned live = 0;
-#pragma unroll
-    for (int i = 0; i < kEach / 4; ++i) {
-        int4 x = make_int4(0, 0, 0, 0);
-        if (p + 4 * i + 3 < t.pages) {
-            x = *reinterpret_cast<const int4*>(t.refs + p + 4 * i);
-        } else {
-            if (p + 4 * i < t.pages) x.x = t.refs[p + 4 * i];
-            if (p + 4 * i + 1 < t.pages) x.y = t.refs[p + 4 * i + 1];
-            if (p + 4 * i + 2 < t.pages) x.z = t.refs[p + 4 * i + 2];
-        }
-        live |= (unsigned)((x.x != 0) | (x.y != 0) << 1 | (x.z != 0) << 2 | (x.w != 0) << 3) << (4 * i);
-    }
-    return live;
-}
 
 __global__ __launch_bounds__(kPlanThreads)
 void pasa_pack_count_k(PackArgs a)
@@ -419,11 +463,9 @@ void pasa_pack_move_k(PackArgs a, CopyArgs c, unsigned entry_groups)
         }
         return;
     }
-    const unsigned long long all = (unsigned long long)moved * c.chunks;
-    for (unsigned long long i = blockIdx.x - entry_groups; i < all; i += gridDim.x - entry_groups) {
-        const unsigned k = (unsigned)(i / c.chunks);
-        copy_chunk(c, a.from[k], a.to[k], (unsigned)(i - (unsigned long long)k * c.chunks));
-    }
+    const unsigned all = (unsigned)moved * c.chunks.d;
+    for (unsigned i = (blockIdx.x - entry_groups) * kCopyAtOnce; i < all; i += kCopyGroups * kCopyAtOnce)
+        copy_chunks(c, i, all, [&](unsigned pair, int& from, int& to) { from = a.from[pair], to = a.to[pair]; });
 }
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -434,6 +476,8 @@ int launched() { return hipGetLastError() == hipSuccess ? PASA_OK : PASA_ELAUNCH
 
 constexpr long long kMaxThreads = 0xffffffff;    // of a launch: the hardware counts them in 32 bits
 constexpr int kMaxPages = 1 << 30;               // page numbers and those of a workgroup behind them fit 31 bits
+constexpr long long kMaxChunks = 1LL << 25;      // of a copy: 32-bit threads of a launch, also where a chunk is a workgroup
+unsigned copy_grid(long long chunks) { return (unsigned)((chunks + kCopyAtOnce - 1) / kCopyAtOnce); }
 // units of a page are counted in 32 bits
 bool page_fits(const pasa_cache& c) { return (long long)c.Hkv * c.page * c.d <= 1LL << 30 && c.pages <= kMaxPages; }
 unsigned entry_chunks(const pasa_cache& c) { return (unsigned)((c.table_width + kCacheThreads - 1) / kCacheThreads); }
@@ -474,9 +518,9 @@ int pasa_cache_copy(const pasa_cache* to, const pasa_cache* from, const int* to_
     if (to->kmean != nullptr && from->kmean == nullptr) return PASA_EINVAL;
     if (!page_fits(*to) || !page_fits(*from)) return PASA_EUNSUPPORTED;
     const CopyArgs a = copy_args(*to, *from);
-    const long long grid = (long long)n * a.chunks;
-    if (grid > kMaxThreads / kCacheThreads) return PASA_EUNSUPPORTED;
-    pasa_copy_pages_k<<<(unsigned)grid, kCacheThreads, 0, static_cast<hipStream_t>(stream)>>>(a, from_pages, to_pages, fast_div(a.chunks));
+    const long long all = (long long)n * a.chunks.d;
+    if (all > kMaxChunks) return PASA_EUNSUPPORTED;
+    pasa_copy_pages_k<<<copy_grid(all), kCacheThreads, 0, static_cast<hipStream_t>(stream)>>>(a, from_pages, to_pages, (unsigned)all);
     return launched();
 }
 
@@ -490,6 +534,10 @@ int pasa_cache_fork(const pasa_cache* cache, int* refs, const int* source, void*
     st = check_workspace(workspace, workspace_bytes, fork_bytes(*cache));
     if (st != PASA_OK) return st;
     const Tables t = tables_of(*cache, refs);
+    if ((long long)cache->S * cache->table_width <= kForkEntries) {
+        pasa_fork_small_k<<<1, kPlanThreads, 0, static_cast<hipStream_t>(stream)>>>(t, source, fast_div((unsigned)cache->table_width));
+        return launched();
+    }
     const unsigned chunks = entry_chunks(*cache), grid = chunks * (unsigned)cache->S;
     int* const table_next = static_cast<int*>(workspace);
     int* const length_next = table_next + (size_t)cache->S * cache->table_width;
@@ -517,7 +565,8 @@ int pasa_cache_room(const pasa_cache* cache, int* refs, int R, const int* row_st
     if (st != PASA_OK) return st;
     if (R <= 0 || !buffer(row_start, 4) || !aligned(lacking, 4)) return PASA_EINVAL;
     const CopyArgs c = copy_args(*cache, *cache);
-    if ((long long)cache->S * c.chunks > kMaxThreads / kCacheThreads) return PASA_EUNSUPPORTED;
+    const long long all = (long long)cache->S * c.chunks.d;
+    if (all > kMaxChunks) return PASA_EUNSUPPORTED;
     st = check_workspace(workspace, workspace_bytes, room_bytes(*cache, R));
     if (st != PASA_OK) return st;
     RoomArgs a;
@@ -532,7 +581,7 @@ int pasa_cache_room(const pasa_cache* cache, int* refs, int R, const int* row_st
     const hipStream_t s = static_cast<hipStream_t>(stream);
     pasa_room_k<<<1, kPlanThreads, 0, s>>>(a);
     if (hipGetLastError() != hipSuccess) return PASA_ELAUNCH;
-    pasa_copy_pages_k<<<(unsigned)cache->S * c.chunks, kCacheThreads, 0, s>>>(c, a.copies, a.copies + cache->S, fast_div(c.chunks));
+    pasa_copy_pages_k<<<copy_grid(all), kCacheThreads, 0, s>>>(c, a.copies, a.copies + cache->S, (unsigned)all);
     return launched();
 }
 
@@ -543,6 +592,8 @@ int pasa_cache_compact(const pasa_cache* cache, int* refs, int* used, void* work
     int st = check(cache, refs);
     if (st != PASA_OK) return st;
     if (!aligned(used, 4)) return PASA_EINVAL;
+    const CopyArgs c = copy_args(*cache, *cache);
+    if ((long long)cache->pages / 2 * c.chunks.d > kMaxChunks) return PASA_EUNSUPPORTED;     // half of the pages move at most
     st = check_workspace(workspace, workspace_bytes, pack_bytes(*cache));
     if (st != PASA_OK) return st;
     PackArgs a;
@@ -561,7 +612,6 @@ int pasa_cache_compact(const pasa_cache* cache, int* refs, int* used, void* work
     }
     pasa_pack_plan_k<<<(unsigned)a.groups, kPlanThreads, 0, s>>>(a);
     if (hipGetLastError() != hipSuccess) return PASA_ELAUNCH;
-    const CopyArgs c = copy_args(*cache, *cache);
     const unsigned entry_groups = (unsigned)(((long long)cache->S * cache->table_width + kCacheThreads - 1) / kCacheThreads);
     pasa_pack_move_k<<<entry_groups + kCopyGroups, kCacheThreads, 0, s>>>(a, c, entry_groups);
     return launched();

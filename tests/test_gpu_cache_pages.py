@@ -40,7 +40,8 @@ def test_a_pool_without_means_takes_pages_of_one_with():
     gb.same(b)
 
 
-@pytest.mark.parametrize("S,width,page", [(5, 7, 16), (1, 1, 128), (64, 40, 32), (300, 3, 16), (7, 700, 16), (1500, 2, 16)])
+@pytest.mark.parametrize("S,width,page", [(5, 7, 16), (1, 1, 128), (64, 40, 32), (300, 3, 16), (7, 700, 16), (1500, 2, 16), (64, 128, 16), (40, 300, 16),
+                                          (9000, 1, 16)])
 def test_sequences_go_on_as_others(S, width, page):
     g = np.random.default_rng([S, width])
     c = ph.pool(g, S, 1, 64, page, width, S * width + 3, mean=False)
@@ -48,6 +49,11 @@ def test_sequences_go_on_as_others(S, width, page):
     lengths[0], lengths[-1] = width * page, 0
     ph.hold(g, c, lengths, 0.5)
     c["table"][S // 2, width - 1] = 2 ** 30 if c["table"][S // 2, width - 1] < 0 else c["table"][S // 2, width - 1]
+    for b in (0, S // 4):                                                 # entries that hold nothing go on as they are
+        i = (c["length"][b] + page - 1) // page // 2
+        if S > 4 and i < width and c["table"][b, i] >= 0:
+            c["table"][b, i] = -5
+    c["refs"][:] = po.counts(c)
     gpu = ph.OnGpu(c)
     for source in (np.arange(S), np.roll(np.arange(S), 1), g.integers(0, S, S), np.where(g.random(S) < 0.3, -1, np.arange(S)),
                    g.integers(-2, S + 2, S), np.full(S, S // 3), np.full(S, 2 ** 31 - 1)):
