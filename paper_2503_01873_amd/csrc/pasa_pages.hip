@@ -412,7 +412,8 @@ void pasa_pack_plan_k(PackArgs a)
     before += others;
     // of the pages below n those in use: in the workgroup that n lies in, and those before
     const int at_n = n > 0 ? (int)((n - 1) / kSpan) : 0, q = at_n * kSpan + tid * kEach;
-    unsigned below = q < (int)n ? in_use(a.t, q) : 0u;
+    unsigned below = q == p ? live : q < (int)n ? in_use(a.t, q) : 0u;
+    if (q >= (int)n) below = 0u;
     if ((int)n - q < kEach && q < (int)n) below &= (1u << ((int)n - q)) - 1u;
     unsigned stay;
     scan_workgroup<NT>((unsigned)__builtin_popcount(below), sums, stay);
