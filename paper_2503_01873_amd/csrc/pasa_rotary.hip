@@ -28,7 +28,7 @@ struct RotaryArgs {
     const unsigned long long* tree;
     int S, most;
     int row0, tokens, heads, rot, io_bf16;
-    int turned;                                  // items of a head that are turned
+    int turned, in_place;                        // items of a head that are turned, the last one perhaps in part
     // A workgroup's threads: `items` of a head, times `lanes` heads at a time, times each_tokens tokens; and the heads of a workgroup
     int items, lanes, each_tokens, each_heads;
     float sign;
@@ -104,17 +104,23 @@ __device__ inline float widen(unsigned short raw, int io_bf16)
 __device__ inline unsigned pack(float lo, float hi, int io_bf16) { return io_bf16 ? pack_bf16(lo, hi) : pack_f16(lo, hi); }
 
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
+enum { HALVES = 0, PAIRS = 1, ANY_HALVES = 2 };
 
-// A thread has an item of a token, 16 bytes (neighbouring pairs) or twice 16 (halves), and takes it of one head after the other: cos and sin, which a workgroup works out
+// A thread has an item of a token, 16 bytes (HALVES: twice 16), and takes it of one head after the other: cos and sin, which a workgroup works out
 // once a token and pair, in 64 bits, stay in its registers.  Two heads of a thread are on their way at a time, the first ones before the positions are known.
-// WIDE: items are eight channels (neighbouring pairs) or twice eight (halves); otherwise a pair of channels.  CACHE: rows of a step.
-// STREAM: y is stored past the L2s.
-template <bool PAIRS, bool WIDE, bool CACHE, bool STREAM>
+//  HALVES: halves that are whole items; an item is eight channels of each.
+//  PAIRS: eight channels, four pairs, of which the last item may have fewer.
+//  ANY_HALVES: eight channels, with the others of their pairs, which may lie anywhere in the row, by way of LDS: a row's items are neighbouring lanes.
+// CACHE: rows of a step.  STREAM: y is stored past the L2s.
+// What bounds it: memory; 2 x 16384 rows of 28 heads, bf16, out of a joint projection, 470 MB, 86.4 us, 5.4 TB/s (one head at a time 84.0, four 94.5; through the L2s 5 us more; four heads
+// and small workgroups for all 103); 14 x 2305 rows of 5 heads of 64, a quarter of the channels, 41 MB, 9.5 us.  A step of 16 rows of 32 heads, 4.4 us: lengths, then angles, then stores.
+template <int MODE, bool CACHE, bool STREAM>
 __global__ __launch_bounds__(kThreads)
 void pasa_rotate_k(RotaryArgs a)
 {
-    constexpr int CS = !WIDE ? 1 : PAIRS ? 4 : 8;        // pairs of an item
+    constexpr int CS = MODE == PAIRS ? 4 : 8;            // pairs of an item
     __shared__ __attribute__((aligned(16))) float2 lds_cs[kTokens * kMaxPairs];
+    __shared__ __attribute__((aligned(16))) unsigned short lds_row[MODE == ANY_HALVES ? kAtOnce * kThreads * 8 : 8];
     __shared__ int lds_position[kTokens], lds_there[kTokens];
     const int tid = threadIdx.x, half = a.rot / 2;
     const unsigned group = a.parts.quotient(blockIdx.x);
@@ -129,9 +135,9 @@ void pasa_rotate_k(RotaryArgs a)
     const bool there = t < tokens;
     const unsigned token = (unsigned)(token0 + (there ? t : 0)), b = a.N.quotient(token), n = a.N.rest(token, b);
     const bool turned = item < a.turned;
-    // channels of the item's first and second part
-    const int c0 = WIDE ? 8 * item + (PAIRS || turned ? 0 : a.rot - 8 * a.turned) : !turned ? a.rot + 2 * (item - a.turned) : PAIRS ? 2 * item : item;
-    const int c1 = WIDE ? (turned ? c0 + half : c0) : turned && !PAIRS ? c0 + half : c0 + 1;
+    // channels of the item, of its second part, and behind its last one that is turned
+    const int c0 = MODE == HALVES && !turned ? a.rot + 8 * (item - a.turned) : 8 * item, c1 = turned ? c0 + half : c0;
+    const bool whole = MODE == HALVES || c0 + 8 <= a.rot;
     const unsigned short* x = a.x + (long long)b * a.xs[0] + (long long)n * a.xs[2];
     unsigned short* y = a.y + (long long)b * a.ys[0] + (long long)n * a.ys[2];
 
@@ -141,13 +147,8 @@ void pasa_rotate_k(RotaryArgs a)
         for (int j = 0; j < kAtOnce; ++j) {
             const int at = h + j * a.lanes < end ? h + j * a.lanes : h0;         // a head again, for nothing
             const unsigned short* from = x + (long long)at * a.xs[1];
-            if constexpr (WIDE) {
-                lo[j] = *reinterpret_cast<const u16x8*>(from + c0);
-                if (!PAIRS) hi[j] = *reinterpret_cast<const u16x8*>(from + c1);
-            } else {
-                lo[j][0] = from[c0];
-                hi[j][0] = from[c1];
-            }
+            lo[j] = *reinterpret_cast<const u16x8*>(from + c0);
+            if (MODE == HALVES) hi[j] = *reinterpret_cast<const u16x8*>(from + c1);
         }
     };
     load(h0 + lane);
@@ -172,35 +173,41 @@ void pasa_rotate_k(RotaryArgs a)
     __syncthreads();
     if (!there || (CACHE && lds_there[t] == 0)) return;
     float2 cs[CS];
+    int other[MODE == ANY_HALVES ? 8 : 1];               // where the other channel of the pair is, from the thread's first one on
 #pragma unroll
-    for (int i = 0; i < CS; ++i) cs[i] = lds_cs[t * kMaxPairs + (turned ? CS * item + i : 0)];
+    for (int i = 0; i < CS; ++i) {
+        const int c = c0 + i;                            // ANY_HALVES
+        const int pair = MODE == HALVES ? c0 + i : MODE == PAIRS ? c0 / 2 + i : c < half ? c : c - half;
+        cs[i] = lds_cs[t * kMaxPairs + (turned && pair < half ? pair : 0)];
+        if (MODE == ANY_HALVES) {
+            other[i] = c >= a.rot ? i : c < half ? i + half : i - half;
+            if (c < half) cs[i].y = -cs[i].y;            // y = x cos -+ other sin
+        }
+    }
     auto store = [&](unsigned short* at, u4 v) {
         if (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<u4*>(at));
         else *reinterpret_cast<u4*>(at) = v;
     };
     for (int h = h0 + lane; h < end; h += kAtOnce * a.lanes) {
         if (h != h0 + lane) load(h);
+        if constexpr (MODE == ANY_HALVES) {
+            __builtin_amdgcn_wave_barrier();             // a wavefront's LDS accesses are done in order
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) *reinterpret_cast<u16x8*>(lds_row + (j * kThreads + tid) * 8) = lo[j];
+            __builtin_amdgcn_wave_barrier();
+            asm volatile("" ::: "memory");
+        }
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
             if (h + j * a.lanes >= end) break;
             unsigned short* to = y + (long long)(h + j * a.lanes) * a.ys[1];
-            if constexpr (!WIDE) {
-                const float p = widen(lo[j][0], a.io_bf16), q = widen(hi[j][0], a.io_bf16);
-                const unsigned out = pack(__builtin_fmaf(p, cs[0].x, -(q * cs[0].y)), __builtin_fmaf(q, cs[0].x, p * cs[0].y), a.io_bf16);
-                to[c0] = turned ? (unsigned short)out : lo[j][0];
-                to[c1] = turned ? (unsigned short)(out >> 16) : hi[j][0];
-            } else if (!turned) {
-                store(to + c0, __builtin_bit_cast(u4, lo[j]));
-            } else if constexpr (PAIRS) {
-                u4 out;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float p = widen(lo[j][2 * e], a.io_bf16), q = widen(lo[j][2 * e + 1], a.io_bf16);
-                    out[e] = pack(__builtin_fmaf(p, cs[e].x, -(q * cs[e].y)), __builtin_fmaf(q, cs[e].x, p * cs[e].y), a.io_bf16);
-                }
-                store(to + c0, out);
-            } else {
-                u4 out[2];
+            if (!turned) {
+                if (!a.in_place) store(to + c0, __builtin_bit_cast(u4, lo[j]));
+                continue;
+            }
+            u4 out[2];
+            if constexpr (MODE == HALVES) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float p[2], q[2];
@@ -213,9 +220,38 @@ void pasa_rotate_k(RotaryArgs a)
                     out[0][e] = pack(p[0], p[1], a.io_bf16);
                     out[1][e] = pack(q[0], q[1], a.io_bf16);
                 }
-                store(to + c0, out[0]);
                 store(to + c1, out[1]);
+            } else if constexpr (MODE == PAIRS) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p = widen(lo[j][2 * e], a.io_bf16), q = widen(lo[j][2 * e + 1], a.io_bf16);
+                    out[0][e] = pack(__builtin_fmaf(p, cs[e].x, -(q * cs[e].y)), __builtin_fmaf(q, cs[e].x, p * cs[e].y), a.io_bf16);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float p[2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float u = widen(lo[j][2 * e + i], a.io_bf16), v = widen(lds_row[(j * kThreads + tid) * 8 + other[2 * e + i]], a.io_bf16);
+                        p[i] = __builtin_fmaf(u, cs[2 * e + i].x, v * cs[2 * e + i].y);
+                    }
+                    out[0][e] = pack(p[0], p[1], a.io_bf16);
+                }
             }
+            // channels from rot on: as they were, or left alone
+            u16x8 made = __builtin_bit_cast(u16x8, out[0]);
+            if (MODE != HALVES && !whole) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) made[e] = c0 + e < a.rot ? made[e] : lo[j][e];
+            }
+            if (MODE == HALVES || whole || !a.in_place) {
+                store(to + c0, __builtin_bit_cast(u4, made));
+                continue;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (c0 + e < a.rot) to[c0 + e] = made[e];
         }
     }
 }
@@ -242,10 +278,10 @@ int launch(RotaryArgs& a, const pasa_rotary* r, int d, int transposed, int io_dt
     a.magnitude = r->magnitude;
     for (int i = 0; i < a.rot / 2; ++i) a.freq[i] = r->freq[i];
     const bool pairs = r->layout == PASA_ROTARY_PAIRS, cache = a.row_start != nullptr;
-    // Items of eight channels where pairs keep to them.
-    const bool wide = a.rot % (pairs ? 8 : 16) == 0;
-    a.turned = !wide ? a.rot / 2 : pairs ? a.rot / 8 : a.rot / 16;
-    a.items = a.turned + (in_place ? 0 : (d - a.rot) / (wide ? 8 : 2));
+    const int mode = pairs ? PAIRS : a.rot % 16 == 0 ? HALVES : ANY_HALVES;
+    a.turned = mode == HALVES ? a.rot / 16 : (a.rot + 7) / 8;
+    a.items = mode == ANY_HALVES ? d / 8 : a.turned + (in_place ? 0 : mode == HALVES ? (d - a.rot) / 8 : d / 8 - a.turned);
+    a.in_place = in_place;
     // Heads at a time: so that a thread takes two or three of them, where there are workgroups enough for that, and few threads are left over; one each otherwise.
     const int groups = kThreads / a.items;
     const long long threads = (long long)a.tokens * a.heads * a.items;
@@ -273,16 +309,16 @@ int launch(RotaryArgs& a, const pasa_rotary* r, int d, int transposed, int io_dt
     a.of_pair = fast_div((unsigned)a.rot / 2);
     a.parts = fast_div((unsigned)parts);
     auto go = [&](auto kernel) { kernel<<<(unsigned)grid, kThreads, 0, stream>>>(a); };
-    auto of_layout = [&](auto p, auto w) {
-        constexpr bool P = decltype(p)::value, W = decltype(w)::value;
-        if (cache) go(pasa_rotate_k<P, W, true, false>);
-        else if (W && threads * (P ? 16 : 32) > kStreamBytes) go(pasa_rotate_k<P, W, false, W>);
-        else go(pasa_rotate_k<P, W, false, false>);
+    const bool stream_out = threads * (mode == HALVES ? 32 : 16) > kStreamBytes;
+    auto of_mode = [&](auto m) {
+        constexpr int M = decltype(m)::value;
+        if (cache) go(pasa_rotate_k<M, true, false>);
+        else if (stream_out) go(pasa_rotate_k<M, false, true>);
+        else go(pasa_rotate_k<M, false, false>);
     };
-    using yes = std::true_type;
-    using no = std::false_type;
-    if (pairs) wide ? of_layout(yes{}, yes{}) : of_layout(yes{}, no{});
-    else wide ? of_layout(no{}, yes{}) : of_layout(no{}, no{});
+    if (mode == HALVES) of_mode(std::integral_constant<int, HALVES>{});
+    else if (mode == PAIRS) of_mode(std::integral_constant<int, PAIRS>{});
+    else of_mode(std::integral_constant<int, ANY_HALVES>{});
     return hipGetLastError() == hipSuccess ? PASA_OK : PASA_ELAUNCH;
 }
 
