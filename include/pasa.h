@@ -347,7 +347,7 @@ int pasa_rotate(const pasa_rotary* rotary, const void* x, void* y, int B, int H,
 /* The rows of a step, at their positions in the cache (only whose lengths are read): R rows of `heads` heads of d channels, x_stride and y_stride elements apart (as
  * row_stride above); the query and key heads of a joint projection lie side by side and go in one call.  y may be x (with its stride).  tree == NULL: row
  * row_start[b] + t at length[b] - n_b + t.  tree as in pasa_attn_cache: at length[b] - n_b and as many on as the row sees of its sequence's rows beside
- * itself, its depth.  Rows of no sequence are left alone.  A step is: lengths, pasa_cache_rotate, pasa_cache_write, pasa_attn_cache. */
+ * itself, its depth.  Rows of no sequence are left alone.  PASA_EUNSUPPORTED also for more than 2^30 sequences or a launch of more than 2^32 threads.  A step is: lengths, pasa_cache_rotate, pasa_cache_write, pasa_attn_cache. */
 int pasa_cache_rotate(const pasa_cache* cache, const pasa_rotary* rotary, const void* x, void* y, int heads, int R, long long x_stride, long long y_stride,
                       const int* row_start, const unsigned long long* tree, int transposed, int io_dtype, void* stream);
 

@@ -12,7 +12,7 @@ namespace {
 constexpr float kBelow = 7.f, kRise = 15.f;
 constexpr float kNoLevel = -3.402823466e38f;     // the lowest finite number: a score of -inf against it gives 0 and no NaN, and no finite one lies below it
 
-// The sum of a row's softmax is held times 2^-14.  A weight over a value's scale is up to 2^15 / (2^-100 / 448), and 262144 of them come to 2^142, which fp32
+// The sum of a row's softmax is held times 2^-14.  A weight over a value's scale is up to 2^15 / (2^-100 / 448) (in 4 bits 2^15 / (2^-98 / 1568)), and 262144 of them come to 2^142, which fp32
 // holds no more; at the other end, P = 2^7 and values of 2^128, it is 2^-128 then, which fp32 still holds.
 constexpr int kSumBits = 14;
 constexpr float kSum = 1.f / (1 << kSumBits);
@@ -310,7 +310,10 @@ __device__ inline void store_row(const RowsArgs& a, int row0, int hk, int p, int
 // P is at most 2^15, whatever the scales, and fp16 holds what matters of it.
 //
 // In 4 bits a lane takes D / 4 consecutive channels of a key, a word to a k-step, and D / 16 of a value; the factors of a unit's keys go through LDS, as fp16, where
-// the lanes that widen find them.
+// the lanes that widen find them.  64 keys of 16 rows are 428 vector instructions (with widening by an or into 64.0, 475) and 32 MFMAs, and half the bytes of 8 bits.  What bounds it: long
+// sequences, what is there whatever the keys (8.5 us, and 4.5 the merge); beyond that 6.05 TB/s (16 x 131072 keys on 4 heads, 1.2 GB, 213 us; 262144 keys, 151 MB, 31.9 us and the merge; 16 ragged
+// sequences, 167 MB, 36.5).  Keys two units ahead: no gain (39.1 -> 41.6), so it is not the way from memory; workgroups of four wavefronts, two to a compute unit: 39.6 -> 41.0.
+// 32 rows: half of the time the vector unit, the rest what hangs on one another in two wavefronts to a SIMD (trees of 48 behind 8 sequences 46 us).
 template <int D, int RB, int FORMAT, bool LISTED, bool FAR>
 __global__ __launch_bounds__(64 * kUnitsAtOnce, 2)
 void pasa_cache_rows(RowsArgs a)
@@ -322,7 +325,7 @@ void pasa_cache_rows(RowsArgs a)
     constexpr int RAW = I4 ? D / 2 : D;          // bytes of a key's codes
     constexpr int GROUPS = D / kFactorChannels, KLD = kUnit + 16;    // factors of a key; LDS row of the keys' factors, so that the lanes' banks differ
     constexpr int ONCE = FAR ? 2 : 0;            // non-temporal
-    constexpr bool QLDS = RB > 1;                // the query fragments wait in LDS: the registers are needed for RB blocks
+    constexpr bool QLDS = RB > 1 && !I4;         // the query fragments wait in LDS: the registers are needed for RB blocks (in 4 bits codes leave enough: trees of 48 49.3 -> 47.4 us)
     // A wavefront's own part: while it sweeps, per key of the unit the score's factor, log2 of the value's scale and kSum over it, and the query fragments;
     // afterwards its stored output.
     __shared__ __attribute__((aligned(16))) float lds_o[NW * ROWS * LD];
@@ -562,7 +565,10 @@ void pasa_cache_rows(RowsArgs a)
                 const bool whole = __builtin_amdgcn_ballot_w64(page_now >= 0 && pos_now + 16 <= new0) == ~0ull;      // all rows see all keys of the unit
                 const bool vs_one = vs_raw == 1.f;
                 // per key: what its score is multiplied by, log2 of the value's scale and kSum over it; in the lanes' order of keys
-                key_f[lane] = ks_raw * (I4 ? a.scale2 / kTiny : a.scale2);
+                // in 4 bits what makes up for kTiny goes with the key's factor, unless that would be more than fp32 holds
+                const float factor_k = ks_raw * a.scale2;
+                const bool large = I4 && __builtin_amdgcn_ballot_w64(factor_k >= 0x1p111f) != 0ull;
+                key_f[lane] = I4 && !large ? factor_k * (1.f / kTiny) : factor_k;
                 key_f[kUnit + lane] = __builtin_amdgcn_logf(vs_raw);
                 // finite, so that 0 times it is 0: a key that is not there may have any scale, and a NaN shows in the score of the rows that see it
                 key_f[2 * kUnit + lane] = kSum * __builtin_fminf(__builtin_fmaxf(__builtin_amdgcn_rcpf(vs_raw), 0.f), 3e38f);
@@ -629,6 +635,14 @@ void pasa_cache_rows(RowsArgs a)
                 load_k();
                 PASA_FENCE();
 
+                if constexpr (I4) {
+                    if (__builtin_expect(large, 0)) {
+#pragma unroll
+                        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                            for (int blk = 0; blk < 4; ++blk) S[rb][blk] *= 1.f / kTiny;
+                    }
+                }
                 f4 inv[4];
 #pragma unroll
                 for (int blk = 0; blk < 4; ++blk) {

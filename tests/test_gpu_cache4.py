@@ -307,6 +307,32 @@ def test_values_of_any_scale():
     _attend(c, q, ch.starts([1, 1]), 0.125, "bf16")
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_keys_of_any_scale(d):
+    """Scales of keys up to the largest that tokens may have: queries of zero see them all alike, small ones choose by them."""
+    g = np.random.default_rng([16, d])
+    Hq, Hkv, L = 4, 2, 200
+    c = h4.filled(g, [L, L, L], Hkv, d, 64)
+    q = _queries(g, 3, Hq, d, "bf16")
+    q[1], q[2] = 0.0, ch.rounded(q[2] * 2.0 ** -24, "f16")
+    for b in (1, 2):
+        for n in range(0, L, 7):
+            c["kscale"][c["table"][b, n // 64], :, n % 64] = 2.0 ** int(g.integers(100, 118))
+    scale = float(np.float32(d ** -0.5))
+    got = ch.run_attend(h4.OnGpu(c), q, ch.starts([1, 1, 1]), scale, "f16")
+    assert np.isfinite(got).all()
+    o, bound = h4.attend(c, q, ch.starts([1, 1, 1]), scale, "f16")
+    h4.check(got[:2], (o[:2], bound[:2]))
+    # the third: scores of 2^80 and more, of which one key has the largest by far more than their rounding; its value is the output
+    for h in range(Hq):
+        x = np.concatenate([(co.values(c4.numbers(c, "k")[i, h // 2], c["kscale"][i, h // 2], "i4") @ q[2, h])[:min(64, L - 64 * j)] for j, i in enumerate(c["table"][2])]) * scale
+        top, second = np.sort(x)[::-1][:2]
+        assert top > second * (1 + 2.0 ** -12) and top > 2.0 ** 60
+        n = int(np.argmax(x))
+        v = co.values(c4.numbers(c, "v")[c["table"][2, n // 64], h // 2, n % 64], c["vscale"][c["table"][2, n // 64], h // 2, n % 64], "i4")
+        assert (np.abs(got[2, h] - v) <= 2.0 ** -10 * np.abs(v) + 2.0 ** -24).all()
+
+
 def test_bad_pages_are_not_seen():
     g = np.random.default_rng(13)
     Hq, Hkv, d = 4, 2, 64
