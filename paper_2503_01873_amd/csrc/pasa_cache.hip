@@ -132,12 +132,15 @@ __device__ inline unsigned encode4(const float (&x)[8], float top, float of_grou
             q[i] = held[i] + shift;
         }
     }
-    unsigned word = 0u;
+    // the low bytes, numbers + 8, of the even ones and of the odd ones side by side, and these between those
+    unsigned half[2];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        word |= (__float_as_uint(q[i]) & 15u) << (4 * i);
-        held[i] *= m;
-    }
+    for (int h = 0; h < 2; ++h)
+        half[h] = __builtin_amdgcn_perm(__float_as_uint(q[2 + h]), __float_as_uint(q[h]), 0x0c0c0400u) |
+                  __builtin_amdgcn_perm(__float_as_uint(q[6 + h]), __float_as_uint(q[4 + h]), 0x04000c0cu);
+    unsigned word = half[0] | half[1] << 4;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) held[i] *= m;
     if (!finite) {
         word = 0x88888888u;
 #pragma unroll
