@@ -205,16 +205,16 @@ int pasa_shift_keys_matrix_mfma(const void* k, void* kprime, int B, int Hkv, int
 int pasa_shift_keys_direct(const void* k, void* kprime, void* k0, int B, int Hkv, int N, int d,
                            double beta, double kscale, void* stream);
 
-/* ---- A cache of keys and values in 8 bits, in pages, and attention that reads it ----
+/* ---- A cache of keys and values in 8 bits or 4, in pages, and attention that reads it ----
  *
  * For servers whose sequences grow token by token and differ in length: S sequences share a pool of `pages` pages of `page`
  * tokens each; table[b][i] is the page in the pool that holds the tokens i * page .. i * page + page - 1 of sequence b (sequences
- * may share pages that neither writes).  A token takes d bytes and a scale for its key and for its value, per KV head; what is
- * held stands for code * scale.  Scales belong to a token and head, so a token that enters changes nothing that is there.  (What is
+ * may share pages that neither writes).  A token takes d bytes (in 4 bits d / 2, and d / 32 factors) and a scale for its key and for its value, per KV head; what is
+ * held stands for code * scale (code * factor * scale).  Scales belong to a token and head, so a token that enters changes nothing that is there.  (What is
  * brought into the buffers by other means than pasa_cache_write keeps its rules: scales 2^-109 at least, no NaN among the codes.)
  *
  * Eq. (9) of the paper: a vector taken from every key leaves softmax unchanged.  kshift is such a vector per KV head (the bias
- * of the key projection, or a mean over a prompt): it is taken off before keys are rounded to 8 bits, which then need not cover
+ * of the key projection, or a mean over a prompt): it is taken off before keys are rounded to so few bits, which then need not cover
  * the bias, and attention and the choice of pages never add it back; pasa_cache_read does.
  *
  * kmean holds the mean of the tokens' (shifted, rounded) keys of every page and head: by Eq. (12) a query's product with it is
@@ -258,14 +258,14 @@ typedef struct {
 /* Tokens enter the cache.  k, v: rows of [Hkv][d] (fp16 or bf16, see pasa_io_dtype), `row_stride` elements apart (at least
  * Hkv * d, a multiple of 8: slices of a joint projection are taken as they are), 16-byte aligned, R rows in all.  Per token and head:
  * scale = fp32(largest magnitude / 127 or 448), 1 where that magnitude is below 2^-100, and codes the nearest of
- * value / scale (ties to even), exactly.  A token with a value that is not finite gets the scale NaN, and so does whoever sees it.
+ * value / scale (ties to even), exactly (in 4 bits as PASA_CACHE_I4 says).  A token with a value that is not finite gets the scale NaN, and so does whoever sees it.
  * kmean != NULL: the means of the pages that are written to are made again, over all their tokens below length[b].
  * PASA_EINVAL also for R <= 0; PASA_EUNSUPPORTED also for 2^23 or more pages (of all heads) that may be written to. */
 int pasa_cache_write(const pasa_cache* cache, const void* k, const void* v, int R, long long row_stride, const int* row_start,
                      int io_dtype, void* stream);
 
 /* Positions first[b] .. first[b] + N - 1 of every sequence (first: DEVICE [S], NULL: zeros) as fp16 or bf16 in k, v:
- * [S, Hkv, N, d], 16-byte aligned, what pasa_prepare_kv takes with B = S: a long chunk of a prompt is attended to that way.  code * scale
+ * [S, Hkv, N, d], 16-byte aligned, what pasa_prepare_kv takes with B = S: a long chunk of a prompt is attended to that way.  What is held
  * + kshift, rounded to fp32 and then to the type.  Zeros where a sequence has no such position.  PASA_EUNSUPPORTED also where the
  * stretches of 64 tokens (of all sequences and heads) come to 2^24. */
 int pasa_cache_read(const pasa_cache* cache, void* k, void* v, const int* first, int N, int io_dtype, void* stream);

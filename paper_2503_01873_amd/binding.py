@@ -43,7 +43,7 @@ class pasa_opts(ctypes.Structure):
 
 
 class pasa_cache(ctypes.Structure):
-    """A paged 8-bit cache: where its buffers are and what they hold, kept by the caller from call to call.  Buffers are tensors or addresses, as in
+    """A paged cache: where its buffers are and what they hold, kept by the caller from call to call.  Buffers are tensors or addresses, as in
     the calls; tensors are held on to."""
     _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "kscale", "vscale", "kmean", "kshift", "table", "length")] + \
                [(n, ctypes.c_int) for n in ("S", "Hkv", "d", "page", "pages", "table_width", "format")]

@@ -1,4 +1,4 @@
-// Attention of a few rows per sequence over the paged 8-bit cache: pasa_cache_rows, and the merge of what its workgroups leave.
+// Attention of a few rows per sequence over the paged cache: pasa_cache_rows, and the merge of what its workgroups leave.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include <type_traits>

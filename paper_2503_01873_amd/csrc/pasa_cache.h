@@ -1,4 +1,4 @@
-// Internal interface of the paged 8-bit cache: what its host layer and its kernels share.  Not installed.
+// Internal interface of the paged cache: what its host layer and its kernels share.  Not installed.
 #ifndef PASA_CACHE_H
 #define PASA_CACHE_H
 

@@ -1,4 +1,4 @@
-// The paged 8-bit cache: tokens enter (write), come back (read), and pages are chosen by their pseudo-averages (score, pick).
+// The paged cache in 8 bits or 4: tokens enter (write), come back (read), and pages are chosen by their pseudo-averages (score, pick).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include <type_traits>

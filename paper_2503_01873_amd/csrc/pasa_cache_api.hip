@@ -1,4 +1,4 @@
-// Host layer of the paged 8-bit cache: the entry points of include/pasa.h that take a pasa_cache.  Argument validation and dispatch.
+// Host layer of the paged cache: the entry points of include/pasa.h that take a pasa_cache.  Argument validation and dispatch.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>

@@ -101,6 +101,13 @@ Tables tables_of(const pasa_cache& c, int* refs)
 __device__ inline bool in_pool(const Tables& t, int page) { return page >= 0 && page < t.pages; }
 __device__ inline int length_of(const Tables& t, int b) { return clamp_int(t.length[b], 0, t.width << t.page_log2); }
 
+// What a workgroup's threads have read, written and counted in memory is done before any of them goes on.
+__device__ inline void memory_barrier()
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
 // What sequences that go on as others will hold, beside the tables; they let go of what they hold.
 __global__ __launch_bounds__(kCacheThreads)
 void pasa_fork_out_k(Tables t, const int* __restrict__ source, int* __restrict__ table_next, int* __restrict__ length_next, FastDiv chunks)
@@ -153,7 +160,7 @@ void pasa_fork_small_k(Tables t, const int* __restrict__ source, FastDiv width)
         old[i] = t.table[at[i]];
         if (ends) length[i] = 0;
     }
-    __syncthreads();                             // all have read
+    memory_barrier();                            // all have read
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         if (i * kPlanThreads + (int)threadIdx.x >= entries || from[i] == b[i]) continue;
@@ -271,7 +278,7 @@ void pasa_room_k(RoomArgs a)
         if (in_lds) lds_begin[t.S] = (int)total;
         else a.begin[t.S] = (int)total;
     }
-    __syncthreads();
+    memory_barrier();
 
     struct Place {
         int b, first;                            // sequence, its first new token
@@ -305,6 +312,7 @@ void pasa_room_k(RoomArgs a)
         const Place p = place_at(i);
         if (p.page < 0 || atomicSub(t.refs + p.page, 1) != 1) alone = false;
     }
+    // what was returned has arrived, so all of them have let go
     if (__syncthreads_and(alone)) {
         for (unsigned i = tid; i < total; i += NT) t.refs[place_at(i).page] = 1;
         if (tid == 0 && a.lacking != nullptr) *a.lacking = 0;
@@ -314,7 +322,7 @@ void pasa_room_k(RoomArgs a)
         const Place p = place_at(i);
         if (p.page >= 0 && holders(t.refs, p.page) <= 0) atomicMin(t.refs + p.page, -(p.b + 1));
     }
-    __syncthreads();
+    memory_barrier();
     auto needs = [&](const Place& p) { return p.page < 0 || holders(t.refs, p.page) != -(p.b + 1); };
     bool my_need = false;                        // where there are few: looked up once, before anything is written
     if (few && (unsigned)tid < total) my_need = needs(mine);
@@ -336,7 +344,7 @@ void pasa_room_k(RoomArgs a)
         found += all;
     }
     if (found > enough) found = enough;
-    __syncthreads();
+    memory_barrier();
     unsigned given = 0;
     for (unsigned i0 = 0; i0 < total; i0 += NT) {
         const unsigned i = i0 + tid;
