@@ -247,7 +247,7 @@ void pasa_room_k(RoomArgs a)
 {
     constexpr int NT = kPlanThreads;
     __shared__ unsigned sums[NT / 64];
-    __shared__ int lds_begin[NT + 1], lds_first[NT];
+    __shared__ int lds_begin[NT + 1], lds_first[NT], lds_free[NT];
     const int tid = threadIdx.x;
     const Tables& t = a.t;
     const int most = t.width << t.page_log2;
@@ -326,25 +326,30 @@ void pasa_room_k(RoomArgs a)
     auto needs = [&](const Place& p) { return p.page < 0 || holders(t.refs, p.page) != -(p.b + 1); };
     bool my_need = false;                        // where there are few: looked up once, before anything is written
     if (few && (unsigned)tid < total) my_need = needs(mine);
-    unsigned wanted = 0;
+    unsigned wanted = 0, my_rank = 0;
     for (unsigned i0 = 0; i0 < total; i0 += NT) {
         const unsigned i = i0 + tid;
         unsigned all;
-        scan_workgroup<NT>(i < total && (few ? my_need : needs(place_at(i))) ? 1u : 0u, sums, all);
+        my_rank = scan_workgroup<NT>(i < total && (few ? my_need : needs(place_at(i))) ? 1u : 0u, sums, all);
         wanted += all;
     }
     unsigned found = 0;
     const unsigned enough = wanted < (unsigned)a.most_free ? wanted : (unsigned)a.most_free;
+    const bool list_in_lds = enough <= NT;
     for (int p0 = 0; p0 < t.pages && found < enough; p0 += kSpan) {
         const int p = p0 + tid * kEach;
         const int there = t.pages - p < kEach ? t.pages - p : kEach;             // pages of this thread
         unsigned free = there > 0 ? ~in_use(t, p) & ((1u << there) - 1u) : 0u;
         unsigned all, rank = found + scan_workgroup<NT>((unsigned)__builtin_popcount(free), sums, all);
-        for (; free != 0 && rank < enough; free &= free - 1) a.free_pages[rank++] = p + __builtin_ctz(free);
+        for (; free != 0 && rank < enough; free &= free - 1, ++rank) {
+            if (list_in_lds) lds_free[rank] = p + __builtin_ctz(free);
+            else a.free_pages[rank] = p + __builtin_ctz(free);
+        }
         found += all;
     }
     if (found > enough) found = enough;
-    memory_barrier();
+    if (list_in_lds) __syncthreads();
+    else memory_barrier();
     unsigned given = 0;
     for (unsigned i0 = 0; i0 < total; i0 += NT) {
         const unsigned i = i0 + tid;
@@ -354,15 +359,15 @@ void pasa_room_k(RoomArgs a)
             p = place_at(i);
             need = few ? my_need : needs(p);
         }
-        unsigned all;
-        const unsigned rank = given + scan_workgroup<NT>(need ? 1u : 0u, sums, all);
+        unsigned all = 0;
+        const unsigned rank = few ? my_rank : given + scan_workgroup<NT>(need ? 1u : 0u, sums, all);
         given += all;
         if (i >= total) continue;
         if (!need) {
             t.refs[p.page] = 1;                  // all others have let go
             continue;
         }
-        const int fresh = rank < found ? a.free_pages[rank] : -1;
+        const int fresh = rank < found ? (list_in_lds ? lds_free[rank] : a.free_pages[rank]) : -1;
         t.table[p.at] = fresh;
         if (fresh < 0) continue;
         t.refs[fresh] = 1;
