@@ -67,29 +67,43 @@ __device__ inline void turn(double turns, double& c, double& s)
 }
 
 // Position of row r of a step, the same in all lanes of a wavefront; false where the row belongs to no sequence.  The sequence is found by 64 entries
-// of row_start at a time.
+// of row_start at a time; up to 63 sequences have all that is to be known of them on its way at once.
 __device__ inline bool place_of_row(const RotaryArgs& a, int r, int& position)
 {
     const int lane = threadIdx.x & 63;
-    int low = 0, size = a.S + 1;                 // the last entry that is not above r is among `size` from `low` on
-    while (size > 1) {
-        const int step = (size + 63) / 64, at = low + lane * step;
-        const bool not_above = lane * step < size && clamp_int(a.row_start[at <= a.S ? at : a.S], 0, a.tokens) <= r;
-        const int n = __builtin_ctzll(~__builtin_amdgcn_ballot_w64(not_above) | 1ull << 63);
-        const int first = lane == 63 && n == 63 && not_above ? 64 : n;           // all 64 of them
-        const int count = __builtin_amdgcn_readlane(first, 63);
-        if (count == 0) return false;
-        low += (count - 1) * step;
-        size = size - (count - 1) * step < step ? size - (count - 1) * step : step;
+    unsigned long long sees = a.tree != nullptr ? a.tree[r] : 0ull;
+    // how many of the 64 entries, from the first on, are not above r
+    auto leading = [&](bool not_above) {
+        const unsigned long long above = ~__builtin_amdgcn_ballot_w64(not_above);
+        return above == 0ull ? 64 : __builtin_ctzll(above);
+    };
+    Sequence s;
+    if (__builtin_expect(a.S < 64, 1)) {
+        const int start = clamp_int(a.row_start[lane <= a.S ? lane : a.S], 0, a.tokens);
+        const int length = clamp_int(a.length[lane < a.S ? lane : a.S - 1], 0, a.most);
+        const int n = leading(lane <= a.S && start <= r);
+        if (n == 0 || n > a.S) return false;
+        s.row0 = __builtin_amdgcn_readlane(start, n - 1);
+        const int end = __builtin_amdgcn_readlane(start, n);
+        s.rows = end > s.row0 ? end - s.row0 : 0;
+        s.length = __builtin_amdgcn_readlane(length, n - 1);
+    } else {
+        int low = 0, size = a.S + 1;             // the last entry that is not above r is among `size` from `low` on
+        while (size > 1) {
+            const int step = (size + 63) / 64, at = low + lane * step;
+            const int n = leading(lane * step < size && clamp_int(a.row_start[at <= a.S ? at : a.S], 0, a.tokens) <= r);
+            if (n == 0) return false;
+            low += (n - 1) * step;
+            size = size - (n - 1) * step < step ? size - (n - 1) * step : step;
+        }
+        low = __builtin_amdgcn_readfirstlane(low);
+        if (low >= a.S) return false;
+        s = sequence_at(a.length, a.row_start, low, a.tokens, a.most);
     }
-    low = __builtin_amdgcn_readfirstlane(low);
-    if (low >= a.S) return false;
-    const Sequence s = sequence_at(a.length, a.row_start, low, a.tokens, a.most);
     const int t = r - s.row0;
     if (t < 0 || t >= s.rows) return false;
     position = s.length - s.rows + t;
     if (a.tree != nullptr) {                     // behind the older tokens, as many as it sees of the others
-        unsigned long long sees = a.tree[r];
         if (s.rows < 64) sees &= (1ull << s.rows) - 1ull;
         if (t < 64) sees &= ~(1ull << t);
         position = s.length - s.rows + __builtin_popcountll(sees);
