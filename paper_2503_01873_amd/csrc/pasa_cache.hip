@@ -269,7 +269,8 @@ __device__ inline Place find_place(const int* __restrict__ length, const int* __
 // token again corrects it.  Partial sums of the lanes that share channels are added in a fixed order.
 // What bounds it: a step, what is waited for in turn (lengths, the table's entry, tokens: 16 tokens 4.3 us); prompts, the vector unit (10 to 16 instructions a
 // value) and memory: 32768 tokens on 8 heads, integers, 201 MB, 45 us, 4.5 TB/s; 13924 on 4, e4m3, 43.5 MB, 16.3 us, 2.7 TB/s, with few workgroups to a
-// compute unit.  In 4 bits the same 13924 tokens on 4 heads take 15.0 us (tokens one or four at a time 15.3 and 16.3, stores past the L2s 18.4).
+// compute unit.  In 4 bits the same 13924 tokens on 4 heads take 14.2 us (tokens one or four at a time 0.3 and 1.3 more, stores past the L2s 3.4, keys and
+// values by workgroups of their own 2.1).
 template <int D, int FORMAT, int NT>
 __global__ __launch_bounds__(NT)
 void pasa_cache_write_k(pasa_cache c, const unsigned short* __restrict__ k, const unsigned short* __restrict__ v, int R, long long row_stride,

@@ -136,7 +136,7 @@ void pasa_fork_in_k(Tables t, const int* __restrict__ source, const int* __restr
     if (in_pool(t, page)) atomicAdd(t.refs + page, 1);
 }
 
-// Both in one launch of one workgroup, for tables of few entries: 64 x 65 in 4.7 us (in two launches 2.9 and 2.5, and the host's 3.5 for one more).
+// Both in one launch of one workgroup, for tables of few entries: 64 x 65 in 4.9 us (in two launches 2.9 and 2.5, and the host's 3.5 for one more).
 constexpr long long kForkEntries = 8 * kPlanThreads;
 __global__ __launch_bounds__(kPlanThreads)
 void pasa_fork_small_k(Tables t, const int* __restrict__ source, FastDiv width)
@@ -241,7 +241,7 @@ struct RoomArgs {
     int R, most_free;
 };
 // In most steps nobody needs a page: every place has one, whose count was 1 when it was let go of.  That is known after one trip to the counts.
-// What bounds it: one trip to memory after the other.  16 sequences, none of which needs a page, 3.6 us; 64, of which 24 take one, 7.6, and 3.2 for the copies of 24 pages of 37 KB.
+// What bounds it: one trip to memory after the other.  16 sequences, none of which needs a page, 4.0 us; 64, of which 24 take one, 8.4, and 3.0 for the copies of 24 pages of 37 KB.
 __global__ __launch_bounds__(kPlanThreads)
 void pasa_room_k(RoomArgs a)
 {
