@@ -491,7 +491,7 @@ int launched() { return hipGetLastError() == hipSuccess ? PASA_OK : PASA_ELAUNCH
 
 constexpr long long kMaxThreads = 0xffffffff;    // of a launch: the hardware counts them in 32 bits
 constexpr int kMaxPages = 1 << 30;               // page numbers and those of a workgroup behind them fit 31 bits
-constexpr long long kMaxChunks = 1LL << 25;      // of a copy: 32-bit threads of a launch, also where a chunk is a workgroup
+constexpr long long kMaxChunks = 1LL << 25;      // of a copy by lists: 32-bit threads of a launch
 unsigned copy_grid(long long chunks) { return (unsigned)((chunks + kCopyAtOnce - 1) / kCopyAtOnce); }
 // units of a page are counted in 32 bits
 bool page_fits(const pasa_cache& c) { return (long long)c.Hkv * c.page * c.d <= 1LL << 30 && c.pages <= kMaxPages; }
@@ -608,7 +608,7 @@ int pasa_cache_compact(const pasa_cache* cache, int* refs, int* used, void* work
     if (st != PASA_OK) return st;
     if (!aligned(used, 4)) return PASA_EINVAL;
     const CopyArgs c = copy_args(*cache, *cache);
-    if ((long long)cache->pages / 2 * c.chunks.d > kMaxChunks) return PASA_EUNSUPPORTED;     // half of the pages move at most
+    if ((long long)cache->pages / 2 * c.chunks.d > INT_MAX) return PASA_EUNSUPPORTED;        // half of the pages move at most
     st = check_workspace(workspace, workspace_bytes, pack_bytes(*cache));
     if (st != PASA_OK) return st;
     PackArgs a;

@@ -86,6 +86,13 @@ def test_workspaces():
     assert fork(c, workspace_bytes=255) == 4 and room(c, workspace_bytes=255) == 4 and compact(c, workspace_bytes=255) == 4
 
 
+def test_copies_beyond_what_a_launch_counts_are_refused():
+    # of this cache a page is 2 + 2 + 1 + 1 + 1 stretches of 4 KiB
+    assert copy(cache(), n=(1 << 25) // 7 + 1) == 2
+    assert room(cache(S=(1 << 25) // 7 + 1, Hkv=2), workspace_bytes=1 << 40) == 2
+    assert compact(cache(pages=620_000_000)) == 2 and compact(cache(pages=600_000_000)) == 4
+
+
 def test_errors_name_the_entry_point():
     for name, call in (("copy", lambda: copy(cache(), n=0, check=True)), ("fork", lambda: fork(cache(), check=True)), ("room", lambda: room(cache(), check=True)),
                        ("compact", lambda: compact(cache(), check=True)), ("free", lambda: P.pasa_cache_free(cache(), None))):
