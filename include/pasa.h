@@ -340,14 +340,14 @@ int pasa_rotary_set(pasa_rotary* rotary, int layout, int rot, double base, int s
  * row to the next (host arrays of three, multiples of 8, not negative; of y at least d where there is more than one), or NULL: contiguous [B, H, N, d].  So queries
  * and keys are taken out of a joint projection and laid out for pasa_attn_fwd as they are turned.  y may be x (with its strides; channels from
  * rot on are left alone then) and must not overlap it otherwise, nor must its heads overlap.  Positions: positions (DEVICE [B][N]), or, where that is NULL, row0 + n.
- * transposed != 0: turned back, sin by -sin: for a y's gradient as x, the gradient of x.  PASA_EUNSUPPORTED also where B * N or the launch does not fit 31 and 32 bits. */
+ * transposed != 0: turned back, sin by -sin: for a y's gradient as x, the gradient of x.  PASA_EUNSUPPORTED also for more than 2^24 heads, or where B * N or the launch does not fit 31 and 32 bits. */
 int pasa_rotate(const pasa_rotary* rotary, const void* x, void* y, int B, int H, int N, int d, const long long* x_strides, const long long* y_strides,
                 const int* positions, int row0, int transposed, int io_dtype, void* stream);
 
 /* The rows of a step, at their positions in the cache (only whose lengths are read): R rows of `heads` heads of d channels, x_stride and y_stride elements apart (as
  * row_stride above); the query and key heads of a joint projection lie side by side and go in one call.  y may be x (with its stride).  tree == NULL: row
  * row_start[b] + t at length[b] - n_b + t.  tree as in pasa_attn_cache: at length[b] - n_b and as many on as the row sees of its sequence's rows beside
- * itself, its depth.  Rows of no sequence are left alone.  PASA_EUNSUPPORTED also for more than 2^30 sequences or a launch of more than 2^32 threads.  A step is: lengths, pasa_cache_rotate, pasa_cache_write, pasa_attn_cache. */
+ * itself, its depth.  Rows of no sequence are left alone.  PASA_EUNSUPPORTED also for more than 2^30 sequences, 2^24 heads or a launch of more than 2^32 threads.  A step is: lengths, pasa_cache_rotate, pasa_cache_write, pasa_attn_cache. */
 int pasa_cache_rotate(const pasa_cache* cache, const pasa_rotary* rotary, const void* x, void* y, int heads, int R, long long x_stride, long long y_stride,
                       const int* row_start, const unsigned long long* tree, int transposed, int io_dtype, void* stream);
 

@@ -12,6 +12,7 @@ namespace {
 
 constexpr int kMaxPairs = 64;
 constexpr int kThreads = 256;
+constexpr int kMaxHeads = 1 << 24;               // so that sums of them and of threads fit 31 bits
 constexpr int kTokens = 32;                      // of a workgroup at most
 constexpr long long kStreamBytes = 32 << 20;     // of y: more than the L2s would keep
 constexpr int kAtOnce = 2;                       // heads of a thread that are on their way together
@@ -277,7 +278,7 @@ bool buffer(const void* p, uintptr_t a) { return p != nullptr && aligned(p, a); 
 int check_rotary(const pasa_rotary* r, int d, int transposed, int io_dtype)
 {
     if (r == nullptr || (r->layout != PASA_ROTARY_HALVES && r->layout != PASA_ROTARY_PAIRS)) return PASA_EINVAL;
-    if (r->rot < 2 || r->rot % 2 != 0 || r->rot > d || !isfinite(r->magnitude)) return PASA_EINVAL;
+    if (r->rot < 2 || r->rot % 2 != 0 || r->rot > d || r->rot > 2 * kMaxPairs || !isfinite(r->magnitude)) return PASA_EINVAL;
     if ((transposed != 0 && transposed != 1) || (io_dtype != PASA_IO_F16 && io_dtype != PASA_IO_BF16)) return PASA_EINVAL;
     for (int i = 0; i < r->rot / 2; ++i)
         if (!isfinite(r->freq[i])) return PASA_EINVAL;
@@ -398,7 +399,7 @@ int pasa_rotate(const pasa_rotary* rotary, const void* x, void* y, int B, int H,
         for (int i = 0; i < 3; ++i)
             if (size[i] > 1 && a.xs[i] != a.ys[i]) return PASA_EINVAL;
     if (positions == nullptr && (long long)row0 + N - 1 > INT_MAX) return PASA_EINVAL;
-    if ((long long)B * N > INT_MAX) return PASA_EUNSUPPORTED;
+    if ((long long)B * N > INT_MAX || H > kMaxHeads) return PASA_EUNSUPPORTED;
     a.x = static_cast<const unsigned short*>(x);
     a.y = static_cast<unsigned short*>(y);
     a.positions = positions;
@@ -419,7 +420,7 @@ int pasa_cache_rotate(const pasa_cache* cache, const pasa_rotary* rotary, const 
     if (st != PASA_OK) return st;
     const long long least = (long long)heads * cache->d;
     if (x_stride < least || y_stride < least || x_stride % 8 != 0 || y_stride % 8 != 0 || (x == y && x_stride != y_stride)) return PASA_EINVAL;
-    if (R > INT_MAX - 1 || cache->S > 1 << 30) return PASA_EUNSUPPORTED;
+    if (R > INT_MAX - 1 || cache->S > 1 << 30 || heads > kMaxHeads) return PASA_EUNSUPPORTED;
     RotaryArgs a = {};
     a.x = static_cast<const unsigned short*>(x);
     a.y = static_cast<unsigned short*>(y);

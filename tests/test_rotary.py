@@ -62,6 +62,12 @@ def _bad_layout():
     return r
 
 
+def _too_long():
+    r = _rotary(rot=128)
+    r.rot = 256                                                           # more pairs than there are frequencies
+    return r
+
+
 def _bad_frequency():
     r = _rotary()
     r.freq[31] = math.inf
@@ -74,6 +80,7 @@ def _bad_frequency():
     (dict(rotary=_rotary(rot=128)), 1), (dict(rotary=_rotary(layout=0, rot=64), d=63), 1), (dict(rotary=_bad_layout()), 1),
     (dict(rotary=_rotary(magnitude=math.nan)), 1), (dict(rotary=_bad_frequency()), 1),
     (dict(x_strides=(8, 8, 4)), 1), (dict(x_strides=(-8, 8, 8)), 1), (dict(y_strides=(1000, 64, 56)), 1), (dict(y_strides=(1000, 0, 64)), 1),
+    (dict(rotary=_too_long(), d=256), 1), (dict(H=0x7FFFFFFF, N=1, B=1), 2), (dict(H=(1 << 24) + 1, N=1, B=1), 2),
     (dict(y=A, x_strides=(640, 64, 128)), 1), (dict(row0=0x7FFFFFFF), 1), (dict(B=1 << 16, N=1 << 15), 2), (dict(H=1 << 20, N=1 << 20), 2),
 ])
 def test_calls_that_are_refused(kw, status):
@@ -85,7 +92,7 @@ def test_calls_that_are_refused(kw, status):
     (dict(cache=None), 1), (dict(cache=refusals.cache(d=96)), 2), (dict(cache=refusals.cache(length=None)), 1), (dict(rotary=None), 1), (dict(x=None), 1),
     (dict(y=2 * A + 8), 1), (dict(row_start=None), 1), (dict(row_start=3 * A + 1), 1), (dict(tree=4 * A + 4), 1), (dict(heads=0), 1), (dict(R=0), 1),
     (dict(x_stride=127), 1), (dict(x_stride=120), 1), (dict(y_stride=132), 1), (dict(y=A, y_stride=256), 1), (dict(rotary=_rotary(rot=66)), 1),
-    (dict(io_dtype=-1), 1), (dict(transposed=-1), 1), (dict(R=0x7FFFFFFF), 2), (dict(cache=refusals.cache(S=0x7FFFFFFF, Hkv=1)), 2), (dict(heads=1 << 24, x_stride=1 << 30, y_stride=1 << 30, R=1 << 26), 2),
+    (dict(io_dtype=-1), 1), (dict(transposed=-1), 1), (dict(R=0x7FFFFFFF), 2), (dict(cache=refusals.cache(S=0x7FFFFFFF, Hkv=1)), 2), (dict(heads=(1 << 24) + 1, x_stride=1 << 40, y_stride=1 << 40), 2), (dict(heads=1 << 24, x_stride=1 << 30, y_stride=1 << 30, R=1 << 26), 2),
 ])
 def test_steps_that_are_refused(kw, status):
     a = dict(cache=refusals.cache(), rotary=_rotary(), x=A, y=2 * A, heads=2, R=3, x_stride=128, y_stride=128, row_start=3 * A, check=False)
