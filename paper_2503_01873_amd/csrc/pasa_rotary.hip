@@ -14,7 +14,9 @@ constexpr int kMaxPairs = 64;
 constexpr int kThreads = 256;
 constexpr int kMaxHeads = 1 << 24;               // so that sums of them and of threads fit 31 bits
 constexpr int kTokens = 32;                      // of a workgroup at most
-constexpr long long kStreamBytes = 32 << 20;     // of y: more than the L2s would keep
+// Of y: more is stored past the L2s, which would have to bring it to memory before the kernel ends (33 MB of keys 14.2 us, through them 17.2; 15 MB 7.6 / 8.6); the smallest
+// outputs stay there for who reads them next.
+constexpr long long kStreamBytes = 4 << 20;
 constexpr int kAtOnce = 2;                       // heads of a thread that are on their way together
 
 // Where a call's tokens are and what their positions are made of.  A token is a row of `heads` heads; b its batch entry, n its number there.
@@ -129,7 +131,7 @@ enum { HALVES = 0, PAIRS = 1, ANY_HALVES = 2 };
 // CACHE: rows of a step.  STREAM: y is stored past the L2s.
 // What bounds it: memory; 2 x 16384 rows of 28 heads, bf16, out of a joint projection, 470 MB, 86.4 us, 5.4 TB/s (one head at a time 84.0, four 94.5; through the L2s 5 us more; four heads
 // and small workgroups for all 103); 14 x 2305 rows of 5 heads of 64, a quarter of the channels, 41 MB, 9.5 us.  A step of 16 rows of 32 heads, 4.2 us: lengths,
-// then angles, then stores.  (cos and sin with the smaller terms of their series in fp32: nothing gained, prompts 108.6 -> 108.2.)
+// then angles, then stores.  (cos and sin with the smaller terms of their series in fp32: nothing gained.)
 template <int MODE, bool CACHE, bool STREAM>
 __global__ __launch_bounds__(kThreads)
 void pasa_rotate_k(RotaryArgs a)

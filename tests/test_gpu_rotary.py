@@ -85,7 +85,8 @@ def test_scaled_frequencies(scaling):
 
 
 @pytest.mark.parametrize("B,H,N,d,rot,layout", [(1, 1, 1, 64, 64, 0), (1, 40, 1, 128, 128, 1), (3, 1, 1000, 64, 20, 0), (1, 36, 1500, 128, 128, 0), (2, 7, 1301, 128, 64, 1),
-                                                (1, 500, 9, 64, 64, 0), (700, 2, 3, 64, 18, 1)])
+                                                (1, 500, 9, 64, 64, 0), (700, 2, 3, 64, 18, 1),
+                                                (2, 9, 1100, 128, 126, 0)])
 def test_numbers_of_tokens_and_heads(B, H, N, d, rot, layout):
     """One token a workgroup and four, heads shared out over several, positions of its own for every token, strides with gaps."""
     import torch
