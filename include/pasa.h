@@ -266,7 +266,8 @@ int pasa_cache_write(const pasa_cache* cache, const void* k, const void* v, int 
 
 /* Positions first[b] .. first[b] + N - 1 of every sequence (first: DEVICE [S], NULL: zeros) as fp16 or bf16 in k, v:
  * [S, Hkv, N, d], 16-byte aligned, what pasa_prepare_kv takes with B = S: a long chunk of a prompt is attended to that way.  What is held
- * + kshift, rounded to fp32 and then to the type.  Zeros where a sequence has no such position.  PASA_EUNSUPPORTED also where the
+ * + kshift, rounded to fp32 and then to the type (to its largest number where that is exceeded by no more than a code may be off: finite tokens come
+ * back finite).  Zeros where a sequence has no such position.  PASA_EUNSUPPORTED also where the
  * stretches of 64 tokens (of all sequences and heads) come to 2^24. */
 int pasa_cache_read(const pasa_cache* cache, void* k, void* v, const int* first, int N, int io_dtype, void* stream);
 

@@ -17,6 +17,8 @@ inline int log2_of(int page)
     return n;
 }
 
+constexpr float kMostF16 = 65504.f, kMostBf16 = 0x1.fep127f;     // the largest numbers of the types of tokens
+
 // In 4 bits a page of a head is its codes, two to a byte, and behind them a factor per token and kFactorChannels channels.
 constexpr int kFactorChannels = 32;
 __host__ __device__ constexpr int token_bytes4(int d) { return d / 2 + d / kFactorChannels; }

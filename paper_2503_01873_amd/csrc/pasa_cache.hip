@@ -402,6 +402,8 @@ void pasa_cache_write_k(pasa_cache c, const unsigned short* __restrict__ k, cons
 // STREAM: outputs of which the eight L2s would keep nothing are stored past them (two sequences of 32768 tokens on 4 heads, 134 MB of output:
 // 31.9 us, 6.4 TB/s; through the L2s 42.4); smaller ones stay there for the one who reads them next (14 x 5 heads, d = 64, 2304 tokens, 21 MB each: 11.5 us, past
 // them 11.9).  Out of 4 bits, four sequences of 8192 tokens on 4 heads, 75 MB: 14.5 us.
+// Numbers of the type come back as such: one that rounding to its code, or the vector taken off it, leaves beyond the type's largest, by no more than a code
+// may be off, is the largest.  A code is off by half a step (of 16 scales among the largest e4m3 codes), with 4 bits also where a factor's rounding, up to 3.5 scales, cuts the largest.
 constexpr int kReadBatch = 4;
 constexpr int read_tokens(int d) { return kReadBatch * kCacheThreads / (d / 8); }
 constexpr size_t kStreamBytes = (size_t)32 << 20;
@@ -413,6 +415,7 @@ void pasa_cache_read_k(pasa_cache c, unsigned short* __restrict__ k, unsigned sh
 {
     constexpr bool E4M3 = FORMAT == PASA_CACHE_E4M3, I4 = FORMAT == PASA_CACHE_I4;
     constexpr int LT = D / 8, AT = kCacheThreads / LT, BATCH = kReadBatch;
+    const float most = io_bf16 ? kMostBf16 : kMostF16;
     const int tid = threadIdx.x, lt = tid % LT, t0 = tid / LT;
     const unsigned up = chunks.quotient(blockIdx.x);
     const int n1 = (int)chunks.rest(blockIdx.x, up) * read_tokens(D);
@@ -473,6 +476,14 @@ void pasa_cache_read_k(pasa_cache c, unsigned short* __restrict__ k, unsigned sh
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[i] = pos[j] >= 0 ? __builtin_fmaf(x[i], scale[j][which], which == 0 ? shift[h][i] : 0.f) : 0.f;
+                const float top = __builtin_fmaxf(__builtin_fmaxf(__builtin_fabsf(x[0]), __builtin_fabsf(x[1])), __builtin_fmaxf(__builtin_fabsf(x[2]), __builtin_fabsf(x[3])));
+                if (__builtin_expect(top > most, 0)) {
+                    // 2^-20: the roundings of the difference from kshift and of the sum with it
+                    const float off = (I4 ? 0.5f * (float)code[j][which].y + 3.5f : E4M3 ? 16.f : 0.5f) * scale[j][which], reach = most + 0x1p-20f * most + off;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (__builtin_fabsf(x[i]) <= reach) x[i] = __builtin_amdgcn_fmed3f(x[i], -most, most);
+                }
                 out[2 * h] = io_bf16 ? pack_bf16(x[0], x[1]) : pack_f16(x[0], x[1]);
                 out[2 * h + 1] = io_bf16 ? pack_bf16(x[2], x[3]) : pack_f16(x[2], x[3]);
             }
