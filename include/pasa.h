@@ -293,7 +293,7 @@ int pasa_cache_choose(const pasa_cache* cache, const void* q, int R, long long r
  * Scores, statistics and output are held in fp32, P times the value's scale is rounded to fp16 (all its bits from 2^-21 of the row's
  * largest on; the scales of the values that a row sees are meant to lie within 2^80 of each other, where a token whose value is all
  * zeros and has the scale 1 counts as 2^-60), bf16 queries are converted to fp16
- * as they are loaded.  A row that sees no key, or whose scores (times log2(e), in fp32) are all -inf, is zeros.
+ * as they are loaded.  Outputs that roundings alone take beyond the type's largest number (by up to 2^-7 of it) are that number.  A row that sees no key, or whose scores (times log2(e), in fp32) are all -inf, is zeros.
  * Meant for rows up to some hundred per sequence; more are correct, but long chunks are faster through pasa_cache_read.
  * workspace: DEVICE, 256-byte aligned, pasa_attn_cache_workspace() bytes (which are enough for fewer rows too); calls that share one
  * must not overlap in time.

@@ -66,6 +66,7 @@ struct RowsArgs {
     float scale2;                                // scale * log2(e)
     int R, Hq, count, io_bf16, page_log2, never_cut;
     FastDiv G;
+    float most, reach;                           // of an output: the largest that its type holds, and what is taken as that
 };
 
 // What the workgroups share out is units of 64 keys, over sequences, KV heads and blocks of rows.  A multiple of what a workgroup sweeps at once:
@@ -275,16 +276,21 @@ __device__ inline unsigned logical_workgroup(unsigned idx, unsigned grid)
 }
 
 // Eight channels of a row's output, divided by the sum of its softmax: by its mantissa, then by the power of two, as fp32 may not hold what is
-// between (one over a sum below 2^-126)
+// between (one over a sum below 2^-126).  A mean of the type's numbers is no larger than its largest: what goes beyond that is the rounding of codes (2^-8.7
+// in 4 bits), of P (2^-11, which the sum does not have) and of long sums, together less than 2^-7, and is taken off.  (For bf16 2^-7 more is infinity in fp32.)
 __device__ inline void store_row(const RowsArgs& a, int row0, int hk, int p, int D, int c8, const f4 (&acc)[2], float sum)
 {
     const float f = sum == 0.f ? 0.f : 1.f / __builtin_amdgcn_frexp_mantf(sum);
     const int bits = -kSumBits - __builtin_amdgcn_frexp_expf(sum);
     const int t = (int)a.G.quotient((unsigned)p), h = (int)a.G.rest((unsigned)p, (unsigned)t);
+    auto value = [&](int i) {
+        const float y = __builtin_ldexpf(acc[i >> 2][i & 3] * f, bits);
+        return __builtin_fabsf(y) <= a.reach ? __builtin_amdgcn_fmed3f(y, -a.most, a.most) : y;
+    };
     unsigned out[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float y0 = __builtin_ldexpf(acc[i >> 1][2 * (i & 1)] * f, bits), y1 = __builtin_ldexpf(acc[i >> 1][2 * (i & 1) + 1] * f, bits);
+        const float y0 = value(2 * i), y1 = value(2 * i + 1);
         out[i] = a.io_bf16 ? pack_bf16(y0, y1) : pack_f16(y0, y1);
     }
     *reinterpret_cast<uint4*>(a.o + ((size_t)(row0 + t) * a.Hq + hk * (int)a.G.d + h) * D + c8) = make_uint4(out[0], out[1], out[2], out[3]);
@@ -1015,6 +1021,8 @@ hipError_t pasa_launch_attn_cache(const pasa_cache& c, const void* q, void* o, i
     a.never_cut = plan.never_cut;
     a.page_log2 = log2_of(c.page);
     a.G = fast_div((unsigned)(Hq / c.Hkv));
+    a.most = io_bf16 ? kMostBf16 : kMostF16;
+    a.reach = a.most * (1.f + 0x1p-7f);
     auto one = [&](auto rows, auto merge, auto merge_each) {
         rows<<<plan.grid, 64 * kUnitsAtOnce, 0, stream>>>(a);
         const hipError_t e = hipGetLastError();

@@ -1,4 +1,4 @@
-"""Tokens of the largest numbers of their type: they come back finite, whatever a code's rounding adds."""
+"""Tokens of the largest numbers of their type: they come back finite, and so does attention over them, whatever a code's or a weight's rounding adds."""
 import numpy as np
 import pytest
 
@@ -87,3 +87,53 @@ def test_what_no_number_of_the_type_is_held_as_comes_back_infinite(format):
     gpu = _on_gpu(c)
     k, v = _read(gpu, 1, 1, 20, 64, "f16")
     assert (np.delete(k, 3, 3) == -np.inf).all() and (np.delete(v, 40, 3) == np.inf).all() and not k[..., 3].any() and not v[..., 40].any()
+    o = ch.run_attend(gpu, np.zeros((1, 2, 64)), [0, 1], 0.125, "f16")
+    assert (np.delete(o, 40, 2) == np.inf).all() and not o[..., 40].any()
+
+
+def _bound(c, q, row_start, scale, dtype, keys):
+    if c["format"] == "i4":
+        return h4.attend(c, q, row_start, scale, dtype)
+    ref = co.attend(c, q, row_start, scale)
+    return ref[0], ch.attend_bound(c, ref, dtype, keys)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("L", [1, 64, 3000])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("format", FORMATS)
+def test_attention_over_the_largest_values_is_finite(format, d, L, dtype):
+    """Long sequences are merged from parts."""
+    g = np.random.default_rng([d, L])
+    Hq, Hkv = 4, 2
+    c = _empty(g, format, 1, Hkv, d, 64, -(-L // 64) + 20, mean=False)
+    c["length"][:] = L
+    k = ch.rounded(g.standard_normal((L, Hkv, d)), dtype)
+    v = _tokens(g, max(L, 2), Hkv, d, dtype)[:L]
+    v[:, 0, :8], v[:, 1, d - 8:] = MOST[dtype], -MOST[dtype]             # of all tokens, so that the output is such a number
+    _write(c, k, v, ch.starts([L]))
+    q = ch.rounded(g.standard_normal((1, Hq, d)), dtype).astype(np.float64)
+    got = ch.run_attend(_on_gpu(c), q, [0, 1], float(np.float32(d ** -0.5)), dtype)
+    o, bound = _bound(c, q, [0, 1], float(np.float32(d ** -0.5)), dtype, L)
+    assert np.isfinite(got).all()
+    assert not (np.abs(got - np.clip(o, -MOST[dtype], MOST[dtype])) > bound).any()
+
+
+@pytest.mark.parametrize("format", FORMATS)
+def test_weights_that_round_upwards_do_not_make_the_largest_values_infinite(format):
+    """One key of weight 2^7 and 63 whose weights lie just above the middle between two fp16 numbers: rounded, they come to 1 + 2^-11.2 times their sum."""
+    g = np.random.default_rng(3)
+    d, L, Hq = 64, 64, 2
+    c = _empty(g, format, 1, 1, d, 64, 1, mean=False)
+    c["length"][:] = L
+    k, v = np.zeros((L, 1, d), np.float32), np.full((L, 1, d), 65504, np.float32)
+    k[1:, 0, 0] = -1.0
+    v[:, 0, 1::2] *= -1
+    _write(c, k, v, ch.starts([L]))
+    q = np.zeros((1, Hq, d))
+    q[..., 0] = 1.0
+    held = co.read(_plain(c), None, 2)[0][0, 0, 1, 0]
+    scale = float(np.float32(np.log(128 / 64.035) / -held))
+    o, bound = _bound(c, q, [0, 1], scale, "f16", L)
+    got = ch.run_attend(_on_gpu(c), q, [0, 1], scale, "f16")
+    assert np.isfinite(got).all() and not (np.abs(got - np.clip(o, -65504, 65504)) > bound).any()
