@@ -359,8 +359,8 @@ int pasa_cache_rotate(const pasa_cache* cache, const pasa_rotary* rotary, const 
  * say, all of it on the device and in the order of the stream, so that a captured graph follows; they do the same whatever the order of its threads.  Other callers of
  * these buffers have to wait meanwhile.  Where refs are not the counts, pages may be given out twice or never; nothing outside the buffers is touched.
  * pasa_cache_write does not look at refs: pasa_cache_room first gives every row a page that its sequence does not share.
- * PASA_EUNSUPPORTED also for more than 2^30 pages, pages of more than 2^30 codes, tables of 2^31 entries, and, counted in stretches of 4 KiB (a page has five at least), copies of more
- * than 2^25 (pasa_cache_copy, and pasa_cache_room with a page for every sequence) and pools of more than 2^32 (pasa_cache_compact). */
+ * PASA_EUNSUPPORTED also for more than 2^30 pages, pages of more than 2^30 codes, tables of 2^31 entries, and, counted in stretches of 4 KiB (a page has four at least, five with a mean), copies
+ * of more than 2^25 - 2 (pasa_cache_copy, and pasa_cache_room with a page for every sequence) and pools of more than 2^32 (pasa_cache_compact). */
 
 /* Contents of pages from_pages[i] of one pool to to_pages[i] of another, or of the same (DEVICE [n] each): codes, scales and, where `to` keeps them, means.  The pools
  * have the same Hkv, d, page and format.  Pairs with a page outside its pool are passed over.  No page may be written twice, or written and read, in a call. */

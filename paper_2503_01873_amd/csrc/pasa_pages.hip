@@ -491,8 +491,9 @@ int launched() { return hipGetLastError() == hipSuccess ? PASA_OK : PASA_ELAUNCH
 
 constexpr long long kMaxThreads = 0xffffffff;    // of a launch: the hardware counts them in 32 bits
 constexpr int kMaxPages = 1 << 30;               // page numbers and those of a workgroup behind them fit 31 bits
-constexpr long long kMaxChunks = 1LL << 25;      // of a copy by lists: 32-bit threads of a launch
-unsigned copy_grid(long long chunks) { return (unsigned)((chunks + kCopyAtOnce - 1) / kCopyAtOnce); }
+// Workgroups of a copy by lists, and whether a launch has as many
+long long copy_grid(long long chunks) { return (chunks + kCopyAtOnce - 1) / kCopyAtOnce; }
+bool copy_fits(long long chunks) { return copy_grid(chunks) <= kMaxThreads / kCacheThreads; }
 // units of a page are counted in 32 bits
 bool page_fits(const pasa_cache& c) { return (long long)c.Hkv * c.page * c.d <= 1LL << 30 && c.pages <= kMaxPages; }
 unsigned entry_chunks(const pasa_cache& c) { return (unsigned)((c.table_width + kCacheThreads - 1) / kCacheThreads); }
@@ -534,8 +535,8 @@ int pasa_cache_copy(const pasa_cache* to, const pasa_cache* from, const int* to_
     if (!page_fits(*to) || !page_fits(*from)) return PASA_EUNSUPPORTED;
     const CopyArgs a = copy_args(*to, *from);
     const long long all = (long long)n * a.chunks.d;
-    if (all > kMaxChunks) return PASA_EUNSUPPORTED;
-    pasa_copy_pages_k<<<copy_grid(all), kCacheThreads, 0, static_cast<hipStream_t>(stream)>>>(a, from_pages, to_pages, (unsigned)all);
+    if (!copy_fits(all)) return PASA_EUNSUPPORTED;
+    pasa_copy_pages_k<<<(unsigned)copy_grid(all), kCacheThreads, 0, static_cast<hipStream_t>(stream)>>>(a, from_pages, to_pages, (unsigned)all);
     return launched();
 }
 
@@ -581,7 +582,7 @@ int pasa_cache_room(const pasa_cache* cache, int* refs, int R, const int* row_st
     if (R <= 0 || !buffer(row_start, 4) || !aligned(lacking, 4)) return PASA_EINVAL;
     const CopyArgs c = copy_args(*cache, *cache);
     const long long all = (long long)cache->S * c.chunks.d;
-    if (all > kMaxChunks) return PASA_EUNSUPPORTED;
+    if (!copy_fits(all)) return PASA_EUNSUPPORTED;
     st = check_workspace(workspace, workspace_bytes, room_bytes(*cache, R));
     if (st != PASA_OK) return st;
     RoomArgs a;
@@ -596,7 +597,7 @@ int pasa_cache_room(const pasa_cache* cache, int* refs, int R, const int* row_st
     const hipStream_t s = static_cast<hipStream_t>(stream);
     pasa_room_k<<<1, kPlanThreads, 0, s>>>(a);
     if (hipGetLastError() != hipSuccess) return PASA_ELAUNCH;
-    pasa_copy_pages_k<<<copy_grid(all), kCacheThreads, 0, s>>>(c, a.copies, a.copies + cache->S, (unsigned)all);
+    pasa_copy_pages_k<<<(unsigned)copy_grid(all), kCacheThreads, 0, s>>>(c, a.copies, a.copies + cache->S, (unsigned)all);
     return launched();
 }
 
