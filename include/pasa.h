@@ -363,7 +363,8 @@ int pasa_cache_rotate(const pasa_cache* cache, const pasa_rotary* rotary, const 
  * of more than 2^25 - 2 (pasa_cache_copy, and pasa_cache_room with a page for every sequence) and pools of more than 2^32 (pasa_cache_compact). */
 
 /* Contents of pages from_pages[i] of one pool to to_pages[i] of another, or of the same (DEVICE [n] each): codes, scales and, where `to` keeps them, means.  The pools
- * have the same Hkv, d, page and format.  Pairs with a page outside its pool are passed over.  No page may be written twice, or written and read, in a call. */
+ * have the same Hkv, d, page and format, and the same values of kshift or both none (PASA_EINVAL where one has it and the other not; values are the caller's to see
+ * to): pages hold keys without it.  Pairs with a page outside its pool are passed over.  No page may be written twice, or written and read, in a call. */
 int pasa_cache_copy(const pasa_cache* to, const pasa_cache* from, const int* to_pages, const int* from_pages, int n, void* stream);
 
 /* Afterwards sequence b is what sequence source[b] was before (DEVICE [S], source[b] == b: untouched): its length, and the pages of its tokens, which both hold from then

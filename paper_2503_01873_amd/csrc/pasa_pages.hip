@@ -532,6 +532,7 @@ int pasa_cache_copy(const pasa_cache* to, const pasa_cache* from, const int* to_
     if (!buffer(to_pages, 4) || !buffer(from_pages, 4) || n <= 0) return PASA_EINVAL;
     if (to->Hkv != from->Hkv || to->d != from->d || to->page != from->page || to->format != from->format) return PASA_EINVAL;
     if (to->kmean != nullptr && from->kmean == nullptr) return PASA_EINVAL;
+    if ((to->kshift != nullptr) != (from->kshift != nullptr)) return PASA_EINVAL;            // held keys would stand for others
     if (!page_fits(*to) || !page_fits(*from)) return PASA_EUNSUPPORTED;
     const CopyArgs a = copy_args(*to, *from);
     const long long all = (long long)n * a.chunks.d;
