@@ -358,6 +358,9 @@ int pasa_cache_rotate(const pasa_cache* cache, const pasa_rotary* rotary, const 
  * -1 (or anything outside the pool).  A caller starts with zeros and entries of -1.  The calls change tables, lengths and refs where the description's pointers
  * say, all of it on the device and in the order of the stream, so that a captured graph follows; they do the same whatever the order of its threads.  Other callers of
  * these buffers have to wait meanwhile.  Where refs are not the counts, pages may be given out twice or never; nothing outside the buffers is touched.
+ * table, length and refs belong to one pool, that of the description: contents are moved there and nowhere else, and a second call finds nothing left to move.  So layers that have a
+ * pool each have tables, lengths and refs each too, and every call is made for each of them (with the same arguments their tables stay alike); pools that shared a table
+ * would keep stale contents in all but the first.
  * pasa_cache_write does not look at refs: pasa_cache_room first gives every row a page that its sequence does not share.
  * PASA_EUNSUPPORTED also for more than 2^30 pages, pages of more than 2^30 codes, tables of 2^31 entries, and, counted in stretches of 4 KiB (a page has four at least, five with a mean), copies
  * of more than 2^25 - 2 (pasa_cache_copy, and pasa_cache_room with a page for every sequence) and pools of more than 2^32 (pasa_cache_compact). */
@@ -378,7 +381,8 @@ int pasa_cache_free(const pasa_cache* cache, int* refs, void* stream);
 /* Room for a step's rows: places that they are written to get pages of their own.  In order of sequences and places: a place without a page takes the lowest free one; one
  * whose page others hold as well lets go of it, takes the lowest free one, and, if older tokens are in the page, a copy of its contents (so the last of several
  * that go on from the same page keeps it).  Free are the pages that were so before the call.  Where none is left the place is without (rows written there are
- * lost) and counts in *lacking (DEVICE, may be NULL; it is set, also to 0): the caller ends such a sequence, or another, before the next step. */
+ * lost, and so are, to this sequence, the older tokens of a page that it shared) and counts in *lacking (DEVICE, may be NULL; it is set, also to 0): the caller ends sequences with an entry
+ * of -1 among their tokens before the next step. */
 size_t pasa_cache_room_workspace(const pasa_cache* cache, int R);
 int pasa_cache_room(const pasa_cache* cache, int* refs, int R, const int* row_start, int* lacking, void* workspace, size_t workspace_bytes, void* stream);
 
