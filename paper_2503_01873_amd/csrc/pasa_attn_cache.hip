@@ -66,7 +66,6 @@ struct RowsArgs {
     float scale2;                                // scale * log2(e)
     int R, Hq, count, io_bf16, page_log2, never_cut;
     FastDiv G;
-    float most, reach;                           // of an output: the largest that its type holds, and what is taken as that
 };
 
 // What the workgroups share out is units of 64 keys, over sequences, KV heads and blocks of rows.  A multiple of what a workgroup sweeps at once:
@@ -283,16 +282,24 @@ __device__ inline void store_row(const RowsArgs& a, int row0, int hk, int p, int
     const float f = sum == 0.f ? 0.f : 1.f / __builtin_amdgcn_frexp_mantf(sum);
     const int bits = -kSumBits - __builtin_amdgcn_frexp_expf(sum);
     const int t = (int)a.G.quotient((unsigned)p), h = (int)a.G.rest((unsigned)p, (unsigned)t);
-    auto value = [&](int i) {
-        const float y = __builtin_ldexpf(acc[i >> 2][i & 3] * f, bits);
-        return __builtin_fabsf(y) <= a.reach ? __builtin_amdgcn_fmed3f(y, -a.most, a.most) : y;
-    };
+    // as bits, which the scalar unit selects here: as floats they took two registers through the main loop, as arguments of the launch they had to be waited for
+    constexpr float beyond = kMostF16 * (1.f + 0x1p-7f);
+    const float most = __uint_as_float(a.io_bf16 ? __builtin_bit_cast(unsigned, kMostBf16) : __builtin_bit_cast(unsigned, kMostF16));
+    const float reach = __uint_as_float(a.io_bf16 ? __builtin_bit_cast(unsigned, __builtin_inff()) : __builtin_bit_cast(unsigned, beyond));
+    float y[8], top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        y[i] = __builtin_ldexpf(acc[i >> 2][i & 3] * f, bits);
+        top = __builtin_fmaxf(top, __builtin_fabsf(y[i]));
+    }
+    if (__builtin_expect(top > most, 0)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (__builtin_fabsf(y[i]) <= reach) y[i] = __builtin_amdgcn_fmed3f(y[i], -most, most);
+    }
     unsigned out[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float y0 = value(2 * i), y1 = value(2 * i + 1);
-        out[i] = a.io_bf16 ? pack_bf16(y0, y1) : pack_f16(y0, y1);
-    }
+    for (int i = 0; i < 4; ++i) out[i] = a.io_bf16 ? pack_bf16(y[2 * i], y[2 * i + 1]) : pack_f16(y[2 * i], y[2 * i + 1]);
     *reinterpret_cast<uint4*>(a.o + ((size_t)(row0 + t) * a.Hq + hk * (int)a.G.d + h) * D + c8) = make_uint4(out[0], out[1], out[2], out[3]);
 }
 
@@ -1021,8 +1028,6 @@ hipError_t pasa_launch_attn_cache(const pasa_cache& c, const void* q, void* o, i
     a.never_cut = plan.never_cut;
     a.page_log2 = log2_of(c.page);
     a.G = fast_div((unsigned)(Hq / c.Hkv));
-    a.most = io_bf16 ? kMostBf16 : kMostF16;
-    a.reach = a.most * (1.f + 0x1p-7f);
     auto one = [&](auto rows, auto merge, auto merge_each) {
         rows<<<plan.grid, 64 * kUnitsAtOnce, 0, stream>>>(a);
         const hipError_t e = hipGetLastError();
