@@ -1064,7 +1064,9 @@ hipError_t pasa_launch_attn_cache(const pasa_cache& c, const void* q, void* o, i
         return held_as(std::integral_constant<int, PASA_CACHE_I8>{});
     };
     // Keys and values that are read once and may be more than the last cache's 256 MB are read past the caches.  us, past / through them: 277 MB
-    // (262144 keys, 4 heads) 54.3 / 58.9, 305 MB 63.2 / 65.5; 68 MB, which a program that does little else finds there again, 28.0 / 24.4
+    // (262144 keys, 4 heads) 54.3 / 58.9, 305 MB 63.2 / 65.5; 68 MB, which a program that does little else finds there again, 28.0 / 24.4.
+    // In 4 bits, where that is all the program reads: 151 MB 38.3 / 35.1, 258 MB 54.4 / 49.7, 302 MB 61 / 61, 645 MB 120 / 127; where others are read in between and nothing is
+    // found again: 75 MB 25.6 / 24.5, 151 MB 37.4 / 39.1, 258 MB 54.7 / 59.4, 302 MB 62 / 66
     const long long held = (blocks != nullptr && count < c.table_width ? count : c.table_width);
     const bool far = (double)held * c.page * c.S * c.Hkv * 2 * cache_token_bytes(c) > 256e6;
     auto of_format = [&](auto d, auto rb) {

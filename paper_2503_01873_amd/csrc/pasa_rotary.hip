@@ -15,7 +15,8 @@ constexpr int kThreads = 256;
 constexpr int kMaxHeads = 1 << 24;               // so that sums of them and of threads fit 31 bits
 constexpr int kTokens = 32;                      // of a workgroup at most
 // Of y: more is stored past the L2s, which would have to bring it to memory before the kernel ends (33 MB of keys 14.2 us, through them 17.2; 15 MB 7.6 / 8.6); the smallest
-// outputs stay there for who reads them next.
+// outputs stay there for who reads them next.  With pasa_attn_fwd behind it (28 heads on 4), past / through, us: queries of 15 MB, one sequence, 63.4 / 64.0; 29 MB, 4096 rows
+// 137.0 / 136.5, 8 x 512 rows 58.8 / 57.9, 64 x 64 rows 68.5 / 65.4, where attention is short and finds less in its L2; 59 MB 435 / 435.
 constexpr long long kStreamBytes = 4 << 20;
 constexpr int kAtOnce = 2;                       // heads of a thread that are on their way together
 
